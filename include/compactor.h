@@ -16,7 +16,8 @@
  *   compress the three fused on one stream
  * and, beyond that path: the attention-based scores a themselves (Sec. 3.2), head-adaptive
  * selection across the heads of a layer (Sec. 3.3), a paged destination for the compaction,
- * and the Hadamard right-sketch of App. D.
+ * the Hadamard right-sketch of App. D, and what serving from the paged result needs: attention of
+ * new tokens to it, appending, and eviction by accumulated attention weight.
  *
  * General conventions
  *   - Every pointer marked "device" is GPU memory owned by the caller; every
@@ -318,6 +319,120 @@ int compactor_attention_workspace_size(const compactor_attn_params_t *p,
 int compactor_attention_scores(const compactor_attn_params_t *p,
                                const compactor_attn_request_t *reqs, int32_t nreq, float *attn,
                                void *workspace, size_t workspace_bytes, void *stream);
+
+/* ---- serving from the compressed cache ---------------------------------------------------- */
+/* What a program does with the retained rows once they lie in pages (compactor_compact_paged): it
+ * attends to them, appends the rows of the tokens it generates, and evicts tokens when the cache has
+ * outgrown its budget, by the attention weight that each has drawn.  For callers that serve; no part
+ * of the paper.  All calls work on one kind of cache, and all that changes from step to step lies in
+ * device memory, so that a captured graph of them can be replayed as the cache grows and shrinks. */
+
+/* The caches of nreq contexts in one pool.  Logical slot s of head (b, l, h) is slot s % page_size of
+ * page tables[b*table_stride + s / page_size]; slots 0 .. counts-1 hold its tokens, in any order.
+ * A count is taken as one of 0 .. table_len*page_size.  A table entry outside [0, num_pages) marks a
+ * page that is not there: its slots are seen by no query, written by no call and evicted first.
+ * Pages that several contexts name (a common prefix) may be attended to, but not be appended to,
+ * accumulated into or evicted from.  A cache of one layer for calls layer by layer: layers = 1 and
+ * every pointer moved to that layer. */
+typedef struct compactor_cache {
+  compactor_page_pool_t pool;
+  const int32_t *tables;  /* device, int32 [nreq][table_stride] */
+  int64_t table_stride;   /* >= table_len */
+  int32_t table_len;      /* logical pages per request, >= 1; table_len * page_size < 2^31 - 64 */
+  int32_t nreq, layers, kv_heads;
+  int32_t head_dim;       /* 128 */
+  int32_t *counts;        /* device: cached tokens of (b, l, h), at b*count_stride_b + l*count_stride_l + h */
+  int32_t *seen;          /* device, same place: tokens that the head has ever been given, which is the
+                             position of the next one */
+  int64_t count_stride_b, count_stride_l;
+  float   *mass;          /* device: accumulated attention weight of a token, at p*state_page_stride +
+                             l*state_layer_stride + h*state_head_stride + (slot in the page) */
+  int32_t *positions;     /* device, same place: position of the token in its context */
+  int64_t state_page_stride, state_layer_stride, state_head_stride;
+                          /* seen, mass and positions: all three, or all NULL for a cache that is
+                             neither admitted to, accumulated into nor evicted from */
+} compactor_cache_t;
+
+/* Makes a serving cache of what compactor_compact_paged has written (the same requests, kept_idx and
+ * kept_cnt; the block tables are the cache's): sets counts to the retained tokens, seen to n, and for
+ * retained token j of a head, in slot j, position kept_idx[j] and mass scores[kept_idx[j]] (scores in
+ * compactor_score's layout: its own, or compactor_attention_scores'; NULL, or an index outside [0, n):
+ * mass 0).  Heads that keep more than their table has room for are cut to that.  The reqs' tensors are not read, only n and ratio. */
+int compactor_cache_admit(const compactor_params_t *p, const compactor_request_t *reqs, int32_t nreq,
+                          const int32_t *kept_idx, const int32_t *kept_cnt, const float *scores,
+                          const compactor_cache_t *cache, void *stream);
+
+/* Rows of new tokens, T = tokens of them per request. */
+typedef struct compactor_cache_rows {
+  const void *k, *v;      /* device, bf16; element (b, l, t, h, c) at b*stride_b + l*stride_l + t*stride_t
+                             + h*stride_h + c; strides are multiples of 8 and the same for both */
+  int64_t stride_b, stride_l, stride_t, stride_h;
+  const int32_t *new_tokens;   /* device, int32 [nreq]: request b brings the first new_tokens[b] of its T
+                             rows (taken as one of 0 .. T), the others are padding; NULL: all T */
+  int32_t tokens;         /* T >= 1 */
+} compactor_cache_rows_t;
+
+/* Appends rows: token t of request b goes to slot counts + t of every head, with position seen + t and
+ * mass 0 (where the cache has them); counts and seen then grow by the number of tokens.  Rows that the
+ * table has no room for are dropped and the count stays at table_len * page_size (seen grows). */
+int compactor_cache_append(const compactor_cache_t *cache, const compactor_cache_rows_t *rows, void *stream);
+
+typedef struct compactor_cache_query {
+  const void *q;          /* device, bf16: query of (b, l, t, q head, c) at b*q_stride_b + l*q_stride_l +
+                             t*q_stride_t + head*q_stride_h + c; strides are multiples of 8 */
+  void *out;              /* device, bf16, addressed likewise by the out strides; not the memory of q */
+  float *lse;             /* device, fp32 [nreq][layers][tokens][q_heads], or NULL */
+  int64_t q_stride_b, q_stride_l, q_stride_t, q_stride_h;
+  int64_t out_stride_b, out_stride_l, out_stride_t, out_stride_h;
+  const int32_t *new_tokens;   /* as in compactor_cache_rows */
+  int32_t tokens;         /* T >= 1: the queries are those of the last tokens that were appended */
+  int32_t q_heads;        /* a multiple of kv_heads: query heads h*G .. h*G+G-1 share kv head h; G*T <= 64 */
+  float   scale;          /* logit scale; 0 = 1/sqrt(head_dim) */
+  float   softcap;        /* c > 0: a logit x becomes c * tanh(x / c); 0 = none */
+  int32_t accumulate;     /* not 0: adds the weights to the cache's mass */
+  int32_t max_tokens;     /* tokens that no head holds more of, 0 = what the tables hold.  Launches and
+                             workspace go by it.  A head that holds more all the same is attended to in
+                             full, but its weights are not accumulated. */
+} compactor_cache_query_t;
+
+/* Attention of the new tokens to the cache, which already holds them (append first): with n_b new tokens of request b,
+ * query (t, g) of head (b, l, h) sees the slots s < counts - (n_b - 1 - t), and
+ *   x_s = scale * q . k_s (capped by softcap),  lse = ln sum_s exp(x_s),  p_s = exp(x_s - lse),
+ *   out = sum_s p_s v_s,   mass[s] += 1/G sum over t and g of p_s   (accumulate).
+ * A query that sees nothing, and a padding row (t >= n_b), gives zeros, lse -inf and no weight, whatever the
+ * memory holds that it does not see.
+ * softmax and sums in fp32, p v with p as two bf16 planes (16 mantissa bits), out rounded once. */
+int compactor_cache_attention(const compactor_cache_t *cache, const compactor_cache_query_t *query,
+                              void *workspace, size_t workspace_bytes, void *stream);
+
+/* Bytes of 256-byte aligned device workspace for compactor_cache_attention; scratch, no state is kept.  0 where none
+ * is needed (workspace may then be NULL).  Depends on the current device's compute units.  host. */
+int compactor_cache_attention_workspace_size(const compactor_cache_t *cache,
+                                             const compactor_cache_query_t *query, size_t *bytes);
+
+typedef struct compactor_cache_evict_params {
+  int32_t budget;         /* tokens a head is brought down to, >= 0 */
+  const int32_t *budgets; /* device, int32 [nreq]: a budget per request in its place (below 0 taken as 0),
+                             or NULL */
+  int32_t sink;           /* tokens at positions below it are protected, >= 0 */
+  int32_t recent;         /* and those at positions >= seen - recent, >= 0 */
+  int32_t scope;          /* COMPACTOR_SCOPE_HEAD: every head keeps its own; COMPACTOR_SCOPE_LAYER: the H heads of
+                             a layer share H * budget (then kv_heads * table_len * page_size < 2^31 - 64) */
+  int32_t max_tokens;     /* as in compactor_cache_query; a head that holds more all the same is left as it is
+                             (layer scope: with its layer) */
+} compactor_cache_evict_params_t;
+
+/* Brings caches down to their budgets.  Of a head (layer) that holds more tokens than its budget, the
+ * first ones in this order stay: protected tokens, then larger mass first, NaN last; equal ones by
+ * lower (head, slot).  Retained tokens in slots from the new count on move, in ascending order, to the slots
+ * below it that were given up, in ascending order: K and V rows, mass and position.  All others stay
+ * where they are, and so do the contents of slots that no token is in any more. */
+int compactor_cache_evict(const compactor_cache_t *cache, const compactor_cache_evict_params_t *evict,
+                          void *workspace, size_t workspace_bytes, void *stream);
+
+/* Bytes of 256-byte aligned device workspace for compactor_cache_evict.  host. */
+int compactor_cache_evict_workspace_size(const compactor_cache_t *cache,
+                                         const compactor_cache_evict_params_t *evict, size_t *bytes);
 
 /* Context-calibrated retention (Sec. 3.4): the smallest r in (0,1] with
  * f(r) = (exp(r b - b) - exp(-b)) / (1 - exp(-b)) >= tau, b = alpha*nll + beta, i.e.

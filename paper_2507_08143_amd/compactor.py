@@ -67,7 +67,44 @@ class _PageTable(C.Structure):
     _fields_ = [("pages", C.c_void_p), ("len", C.c_int32)]
 
 
+class _Cache(C.Structure):
+    _fields_ = [("pool", _PagePool), ("tables", C.c_void_p), ("table_stride", C.c_int64),
+                ("table_len", C.c_int32), ("nreq", C.c_int32), ("layers", C.c_int32),
+                ("kv_heads", C.c_int32), ("head_dim", C.c_int32), ("counts", C.c_void_p),
+                ("seen", C.c_void_p), ("count_stride_b", C.c_int64), ("count_stride_l", C.c_int64),
+                ("mass", C.c_void_p), ("positions", C.c_void_p), ("state_page_stride", C.c_int64),
+                ("state_layer_stride", C.c_int64), ("state_head_stride", C.c_int64)]
+
+
+class _CacheRows(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("stride_b", C.c_int64), ("stride_l", C.c_int64),
+                ("stride_t", C.c_int64), ("stride_h", C.c_int64), ("new_tokens", C.c_void_p),
+                ("tokens", C.c_int32)]
+
+
+class _CacheQuery(C.Structure):
+    _fields_ = [("q", C.c_void_p), ("out", C.c_void_p), ("lse", C.c_void_p),
+                ("q_stride_b", C.c_int64), ("q_stride_l", C.c_int64), ("q_stride_t", C.c_int64),
+                ("q_stride_h", C.c_int64), ("out_stride_b", C.c_int64), ("out_stride_l", C.c_int64),
+                ("out_stride_t", C.c_int64), ("out_stride_h", C.c_int64), ("new_tokens", C.c_void_p),
+                ("tokens", C.c_int32), ("q_heads", C.c_int32), ("scale", C.c_float),
+                ("softcap", C.c_float), ("accumulate", C.c_int32), ("max_tokens", C.c_int32)]
+
+
+class _CacheEvict(C.Structure):
+    _fields_ = [("budget", C.c_int32), ("budgets", C.c_void_p), ("sink", C.c_int32),
+                ("recent", C.c_int32), ("scope", C.c_int32), ("max_tokens", C.c_int32)]
+
+
 _PP, _RP = C.POINTER(_Params), C.POINTER(_Request)
+_CP, _CQP, _CEP = C.POINTER(_Cache), C.POINTER(_CacheQuery), C.POINTER(_CacheEvict)
+_lib.compactor_cache_admit.argtypes = [_PP, _RP, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p, _CP,
+                                       C.c_void_p]
+_lib.compactor_cache_append.argtypes = [_CP, C.POINTER(_CacheRows), C.c_void_p]
+_lib.compactor_cache_attention.argtypes = [_CP, _CQP, C.c_void_p, C.c_size_t, C.c_void_p]
+_lib.compactor_cache_attention_workspace_size.argtypes = [_CP, _CQP, C.POINTER(C.c_size_t)]
+_lib.compactor_cache_evict.argtypes = [_CP, _CEP, C.c_void_p, C.c_size_t, C.c_void_p]
+_lib.compactor_cache_evict_workspace_size.argtypes = [_CP, _CEP, C.POINTER(C.c_size_t)]
 _APP, _ARP = C.POINTER(_AttnParams), C.POINTER(_AttnRequest)
 _lib.compactor_attention_workspace_size.argtypes = [_APP, _ARP, C.c_int32, C.POINTER(C.c_size_t)]
 _lib.compactor_attention_scores.argtypes = [_APP, _ARP, C.c_int32, C.c_void_p, C.c_void_p,
@@ -105,7 +142,10 @@ EXPORTS = ["compactor_default_params", "compactor_keep_count", "compactor_layout
            "compactor_compact", "compactor_compact_paged", "compactor_compress", "compactor_compress_static",
            "compactor_calibrated_ratio",
            "compactor_error_string", "compactor_version",
-           "compactor_attention_workspace_size", "compactor_attention_scores"]
+           "compactor_attention_workspace_size", "compactor_attention_scores",
+           "compactor_cache_admit", "compactor_cache_append", "compactor_cache_attention",
+           "compactor_cache_attention_workspace_size", "compactor_cache_evict",
+           "compactor_cache_evict_workspace_size"]
 
 
 STAGES = ["gram", "reduce", "solve", "score", "blend", "select", "gather"]
@@ -581,3 +621,235 @@ def compactor_attention_scores(params: AttnParams, reqs: Sequence[AttnRequest], 
     _check(_lib.compactor_attention_scores(C.byref(params.c()), arr, len(reqs), _ptr(attn),
                                            _ptr(workspace), workspace.numel(), _stream(stream)))
     return attn
+
+
+class Cache:
+    """The caches of some contexts in one page pool, for the calls that serve from them (see
+    compactor_cache_t).  Checked once, here; the tensors stay the caller's, and must not be resized
+    or moved while the Cache is in use.
+
+    k_pages, v_pages  bf16 views indexed [page, layer, slot, head, channel], as compactor_compact_paged
+                      takes them
+    tables            int32 [request, logical page]
+    counts            int32 [request, layer, head]: tokens that each head holds
+    seen              int32, same shape and strides: tokens it has ever been given
+    mass, positions   fp32 and int32 views indexed [page, layer, head, slot], slots contiguous
+    seen, mass and positions: all three, or none."""
+
+    def __init__(self, k_pages: torch.Tensor, v_pages: torch.Tensor, tables: torch.Tensor,
+                 counts: torch.Tensor, seen: Optional[torch.Tensor] = None,
+                 mass: Optional[torch.Tensor] = None, positions: Optional[torch.Tensor] = None):
+        _require(k_pages.dtype == torch.bfloat16 and v_pages.dtype == torch.bfloat16,
+                 "k_pages and v_pages must be bfloat16")
+        _require(k_pages.dim() == 5 and k_pages.stride(4) == 1 and v_pages.shape == k_pages.shape and
+                 v_pages.stride() == k_pages.stride(),
+                 "k_pages and v_pages must be [page, layer, slot, head, channel] views of equal shape and "
+                 "strides, channel contiguous")
+        pages, layers, page_size, heads, _ = k_pages.shape
+        _require(tables.dtype == torch.int32 and tables.dim() == 2 and tables.shape[0] >= 1 and
+                 tables.shape[1] >= 1 and (tables.stride(1) == 1 or tables.shape[1] == 1),
+                 "tables must be int32 [request, logical page], logical pages contiguous")
+        nreq, table_len = tables.shape
+        _require(nreq == 1 or tables.stride(0) >= table_len, "the tables of two requests must not overlap")
+        _require((seen is None) == (mass is None) == (positions is None) and (seen is None or mass is not None),
+                 "seen, mass and positions: all three, or none")
+        for name, t in (("counts", counts), ("seen", seen)):
+            if t is not None and not (t.dtype == torch.int32 and tuple(t.shape) == (nreq, layers, heads) and
+                                      (t.stride(2) == 1 or heads == 1) and t.stride() == counts.stride()):
+                _refuse("%s must be int32 [request, layer, head] = [%d, %d, %d], heads contiguous, with the "
+                        "strides of counts" % (name, nreq, layers, heads))
+        for name, t, dtype in (("mass", mass, torch.float32), ("positions", positions, torch.int32)):
+            if t is not None and not (t.dtype == dtype and tuple(t.shape) == (pages, layers, heads, page_size) and
+                                      (t.stride(3) == 1 or page_size == 1) and t.stride() == mass.stride()):
+                _refuse("%s must be %s [page, layer, head, slot] = [%d, %d, %d, %d], slots contiguous, with the "
+                        "strides of mass" % (name, dtype, pages, layers, heads, page_size))
+        for name, t in (("counts", counts), ("seen", seen), ("mass", mass), ("positions", positions)):
+            if t is not None and any(n > 1 and s == 0 for n, s in zip(t.shape, t.stride())):
+                _refuse("%s is written: its elements must not share memory" % name)
+        self.device = k_pages.device
+        for name, t in (("k_pages", k_pages), ("v_pages", v_pages), ("tables", tables), ("counts", counts),
+                        ("seen", seen), ("mass", mass), ("positions", positions)):
+            if t is not None and not t.is_cuda:
+                _refuse("%s must live on the GPU" % name)
+            if t is not None and t.device != self.device:
+                _refuse("%s must live on the GPU of the page pool" % name)
+        self.k_pages, self.v_pages, self.tables, self.counts = k_pages, v_pages, tables, counts
+        self.seen, self.mass, self.positions = seen, mass, positions
+        self.nreq, self.layers, self.kv_heads = nreq, layers, heads
+        pool = _PagePool(k_pages.data_ptr(), v_pages.data_ptr(), k_pages.stride(0), k_pages.stride(1),
+                         k_pages.stride(3), k_pages.stride(2), page_size, pages)
+        st = mass.stride() if mass is not None else (0, 0, 0)
+        self._c = _Cache(pool, tables.data_ptr(), max(tables.stride(0), table_len), table_len, nreq, layers, heads,
+                         k_pages.shape[4], counts.data_ptr(), _ptr(seen), counts.stride(0), counts.stride(1),
+                         _ptr(mass), _ptr(positions), st[0], st[1], st[2])
+        self._ref = C.byref(self._c)
+
+    def layer(self, first: int, count: int = 1) -> "Cache":
+        """The cache of `count` layers from `first` on, for calls layer by layer."""
+        _require(0 <= first and count >= 1 and first + count <= self.layers, "no such layers")
+        at = slice(first, first + count)
+        some = lambda t: None if t is None else t[:, at]      # noqa: E731
+        return Cache(self.k_pages[:, at], self.v_pages[:, at], self.tables, self.counts[:, at], some(self.seen),
+                     some(self.mass), some(self.positions))
+
+    def _new_tokens(self, t: Optional[torch.Tensor]) -> int:
+        if t is None:
+            return 0
+        if t.dtype != torch.int32 or t.dim() != 1 or t.shape[0] != self.nreq or not t.is_contiguous():
+            _refuse("new_tokens must be a contiguous int32 tensor of %d requests" % self.nreq)
+        if t.device != self.device:
+            _refuse("new_tokens must live on the GPU of the cache")
+        return t.data_ptr()
+
+    def _workspace(self, size, what, given, stream):
+        """-> (pointer, bytes), and the tensor that holds them"""
+        if given is not None:
+            _out(given, 0, torch.uint8, "workspace")
+            if given.device != self.device:
+                _refuse("the workspace must live on the GPU of the cache")
+            return given.data_ptr(), given.numel(), given
+        out = C.c_size_t(0)
+        _check(size(self._ref, what, C.byref(out)))
+        if out.value == 0:
+            return 0, 0, None
+        given = torch.empty(out.value, dtype=torch.uint8, device=self.device)
+        if stream is not None:
+            given.record_stream(stream)      # used on `stream`, see _workspace()
+        return given.data_ptr(), out.value, given
+
+    def _on(self, stream, call):
+        """call(stream handle) with the cache's GPU current."""
+        if stream is not None and stream.device != self.device:
+            _refuse("the stream belongs to another GPU than the cache")
+        if torch.cuda.current_device() == self.device.index:
+            _check(call(_stream(stream)))
+        else:
+            with torch.cuda.device(self.device):
+                _check(call(_stream(stream)))
+
+
+def compactor_cache_admit(params: Params, reqs: Sequence[Request], kept_idx: torch.Tensor,
+                          kept_cnt: torch.Tensor, cache: Cache, scores: Optional[torch.Tensor] = None,
+                          stream=None):
+    """State of the rows that compactor_compact_paged has written into the cache's pages: counts, seen,
+    positions and, from the scores, mass."""
+    pp, arr, n = call = _marshal(params, reqs, on_gpu=False)
+    so, ko, _ = _layout(*call)
+    if (n, params.layers, params.kv_heads) != (cache.nreq, cache.layers, cache.kv_heads):
+        _refuse("the cache is of [%d, %d, %d] requests, layers and heads, the call of [%d, %d, %d]"
+                % (cache.nreq, cache.layers, cache.kv_heads, n, params.layers, params.kv_heads))
+    for t, numel, dtype, name in ((kept_idx, ko[-1], torch.int32, "kept_idx"),
+                                  (kept_cnt, n * params.layers * params.kv_heads, torch.int32, "kept_cnt"),
+                                  (scores, so[-1], torch.float32, "scores")):
+        _out(t, numel, dtype, name)
+        if t is not None and t.device != cache.device:
+            _refuse("%s must live on the GPU of the cache" % name)
+    cache._on(stream, lambda st: _lib.compactor_cache_admit(pp, arr, n, _ptr(kept_idx), _ptr(kept_cnt), _ptr(scores),
+                                                            cache._ref, st))
+
+
+def compactor_cache_append(cache: Cache, k: torch.Tensor, v: torch.Tensor,
+                           new_tokens: Optional[torch.Tensor] = None, stream=None):
+    """Rows of new tokens into the cache.  k, v: bf16 [request, layer, token, kv head, channel], any
+    strides with the channel contiguous, the same for both; new_tokens: int32 [request], how many of
+    its rows each request brings (None: all)."""
+    if k.dtype != torch.bfloat16 or k.dim() != 5 or v.dtype != torch.bfloat16:
+        _refuse("k and v must be bfloat16 [request, layer, token, head, channel]")
+    B, L, T, H, d = k.shape
+    sb, sl, st_, sh, sc = k.stride()
+    if (B, L, H, d) != (cache.nreq, cache.layers, cache.kv_heads, cache._c.head_dim):
+        _refuse("k has shape %s, the cache is of [%d, %d, tokens, %d, %d]"
+                % (tuple(k.shape), cache.nreq, cache.layers, cache.kv_heads, cache._c.head_dim))
+    if sc != 1 or v.shape != k.shape or v.stride() != (sb, sl, st_, sh, sc):
+        _refuse("v must have the shape and strides of k, the channel contiguous")
+    if k.device != cache.device or v.device != cache.device:
+        _refuse("k and v must live on the GPU of the cache")
+    rows = _CacheRows(k.data_ptr(), v.data_ptr(), sb, sl, st_, sh, cache._new_tokens(new_tokens), T)
+    cache._on(stream, lambda st: _lib.compactor_cache_append(cache._ref, C.byref(rows), st))
+
+
+def _cache_query(cache: Cache, q, new_tokens, scale, softcap, accumulate, max_tokens):
+    if q.dtype != torch.bfloat16 or q.dim() != 5:
+        _refuse("q must be bfloat16 [request, layer, token, query head, channel]")
+    B, L, T, Hq, d = q.shape
+    sb, sl, st, sh, sc = q.stride()
+    if (B, L, d) != (cache.nreq, cache.layers, cache._c.head_dim) or sc != 1:
+        _refuse("q has shape %s and strides %s, the cache is of [%d, %d, tokens, query heads, %d], the channel contiguous"
+                % (tuple(q.shape), q.stride(), cache.nreq, cache.layers, cache._c.head_dim))
+    if q.device != cache.device:
+        _refuse("q must live on the GPU of the cache")
+    return _CacheQuery(q.data_ptr(), 0, 0, sb, sl, st, sh, 0, 0, 0, 0, cache._new_tokens(new_tokens), T, Hq, scale,
+                       softcap, 1 if accumulate else 0, max_tokens)
+
+
+def compactor_cache_attention_workspace_size(cache: Cache, q: torch.Tensor, accumulate: bool = False,
+                                             max_tokens: int = 0) -> int:
+    out = C.c_size_t(0)
+    query = _cache_query(cache, q, None, 0.0, 0.0, accumulate, max_tokens)
+    _check(_lib.compactor_cache_attention_workspace_size(cache._ref, C.byref(query), C.byref(out)))
+    return int(out.value)
+
+
+def compactor_cache_attention(cache: Cache, q: torch.Tensor, new_tokens: Optional[torch.Tensor] = None,
+                              scale: float = 0.0, softcap: float = 0.0, accumulate: bool = False,
+                              max_tokens: int = 0, want_lse: bool = False, out=None, lse=None,
+                              workspace=None, stream=None):
+    """Attention of the tokens appended last to the cache.  q: bf16 [request, layer, token, query head,
+    channel], any strides with the channel contiguous.  -> (out, bf16 of q's shape; lse, fp32
+    [request, layer, token, query head], or None unless asked for or given)"""
+    query = _cache_query(cache, q, new_tokens, scale, softcap, accumulate, max_tokens)
+    shape = q.shape
+    if out is None:
+        out = torch.empty(shape, dtype=torch.bfloat16, device=cache.device)
+        if stream is not None:
+            out.record_stream(stream)
+    else:
+        if out.dtype != torch.bfloat16 or out.shape != shape or out.stride(4) != 1 or out.device != cache.device:
+            _refuse("out must be bfloat16 of q's shape on the GPU of the cache, the channel contiguous")
+        if any(n > 1 and s == 0 for n, s in zip(shape, out.stride())):
+            _refuse("out is written: its elements must not share memory")
+    query.out = out.data_ptr()
+    query.out_stride_b, query.out_stride_l, query.out_stride_t, query.out_stride_h, _ = out.stride()
+    if lse is not None:
+        _out(lse, shape[0] * shape[1] * shape[2] * shape[3], torch.float32, "lse")
+        if lse.device != cache.device:
+            _refuse("lse must live on the GPU of the cache")
+    elif want_lse:
+        lse = torch.empty(shape[:4], dtype=torch.float32, device=cache.device)
+        if stream is not None:
+            lse.record_stream(stream)
+    query.lse = _ptr(lse)
+    ref = C.byref(query)
+    ptr, nbytes, _keep = cache._workspace(_lib.compactor_cache_attention_workspace_size, ref, workspace, stream)
+    cache._on(stream, lambda st: _lib.compactor_cache_attention(cache._ref, ref, ptr, nbytes, st))
+    return out, lse
+
+
+def _cache_evict(cache: Cache, budget, budgets, sink, recent, scope, max_tokens):
+    if (budget is None) == (budgets is None):
+        _refuse("either budget or budgets")
+    ptr = 0
+    if budgets is not None:
+        if budgets.dtype != torch.int32 or tuple(budgets.shape) != (cache.nreq,) or not budgets.is_contiguous():
+            _refuse("budgets must be a contiguous int32 tensor of %d requests" % cache.nreq)
+        if budgets.device != cache.device:
+            _refuse("budgets must live on the GPU of the cache")
+        ptr = budgets.data_ptr()
+    return _CacheEvict(0 if budget is None else budget, ptr, sink, recent, scope, max_tokens)
+
+
+def compactor_cache_evict_workspace_size(cache: Cache, scope: int = SCOPE_HEAD, max_tokens: int = 0) -> int:
+    out = C.c_size_t(0)
+    evict = _CacheEvict(0, 0, 0, 0, scope, max_tokens)
+    _check(_lib.compactor_cache_evict_workspace_size(cache._ref, C.byref(evict), C.byref(out)))
+    return int(out.value)
+
+
+def compactor_cache_evict(cache: Cache, budget: Optional[int] = None, budgets: Optional[torch.Tensor] = None,
+                          sink: int = 0, recent: int = 0, scope: int = SCOPE_HEAD, max_tokens: int = 0,
+                          workspace=None, stream=None):
+    """Brings every head (SCOPE_LAYER: the heads of every layer together) down to its budget: `budget`
+    tokens, or budgets[request] of an int32 device tensor."""
+    ref = C.byref(_cache_evict(cache, budget, budgets, sink, recent, scope, max_tokens))
+    ptr, nbytes, _keep = cache._workspace(_lib.compactor_cache_evict_workspace_size, ref, workspace, stream)
+    cache._on(stream, lambda st: _lib.compactor_cache_evict(cache._ref, ref, ptr, nbytes, st))

@@ -6,7 +6,7 @@
 #include <algorithm>
 #include <mutex>
 
-#include "common.h"
+#include "cache.h"
 
 using namespace cmp;
 
@@ -736,6 +736,28 @@ int compactor_compact_paged(const compactor_params_t *p, const compactor_request
       P.t[i].len = tables[T.s[i].req].len;
     }
     HIP_TRY(launch_gather_paged(T, P, kept_idx, kept_cnt, in_place != 0, st));
+    return COMPACTOR_OK;
+  });
+}
+
+int compactor_cache_admit(const compactor_params_t *p, const compactor_request_t *reqs, int32_t nreq,
+                          const int32_t *kept_idx, const int32_t *kept_cnt, const float *scores,
+                          const compactor_cache_t *cache, void *stream) {
+  int rc = check_params(p, false);
+  if (rc) return rc;
+  rc = check_requests(reqs, nreq, 0);
+  if (rc) return rc;
+  rc = check_scope(p, reqs, nreq);
+  if (rc) return rc;
+  if (!kept_idx || !kept_cnt) return COMPACTOR_EINVAL;
+  CacheView C;
+  rc = cache_view(cache, CACHE_STATE, &C);
+  if (rc) return rc;
+  if (C.nreq != nreq || C.layers != p->layers || C.kv_heads != p->kv_heads) return COMPACTOR_EINVAL;
+  hipStream_t st = static_cast<hipStream_t>(stream);
+  drop_pending_error();
+  return for_each_group(p, reqs, nreq, 1ll << 60, false, [&](const SegTable &T, long long) {
+    HIP_TRY(launch_cache_admit(T, C, kept_idx, kept_cnt, scores, st));
     return COMPACTOR_OK;
   });
 }
