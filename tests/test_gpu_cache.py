@@ -117,21 +117,20 @@ def test_attention_does_not_look_ahead(C, fill, count, T):
         P.v[p, 0, a, h] = fill
         if h == 0:
             P.k[p, 0, a, h] = fill
-    before = P.snapshot()
     out, lse = C.compactor_cache_attention(P.cache, q, accumulate=True, want_lse=True)
     torch.cuda.synchronize()
-    # all but the last token: as if the slot held zeros
+    # All but the last token against the oracle, which does not look at the slot.  (Not against a run that finds a number in it: that
+    # one multiplies the rows of later tokens in another order and with its weights in 16 bits, which the bounds allow for.)
+    qd, od, ld = U.f64(q), U.f64(out), lse.double().cpu().numpy()
     for h in range(2):
-        p, a = int(P.tables[0, (count - 1) // 16]), (count - 1) % 16
-        P.v[p, 0, a, h] = 0
-        P.k[p, 0, a, h] = 0
-    want, want_lse = C.compactor_cache_attention(P.cache, q, want_lse=True)
-    torch.cuda.synchronize()
-    assert torch.equal(U.bits(out[:, :, :T - 1]), U.bits(want[:, :, :T - 1]))
-    assert torch.equal(lse[:, :, :T - 1], want_lse[:, :, :T - 1])
-    first = U.f64(want[:, :, :T - 1])
-    assert np.isfinite(first).all()
-    del before
+        k, v, _, _, there = P.head(0, 0, h)
+        for t, see in enumerate(O.sees(count, T, T)[:T - 1]):
+            for g in range(2):
+                row = (0, 0, t, 2 * h + g)
+                want, want_lse, p = O.attend(qd[row], k, v, see, there, 128 ** -0.5, 0.0)
+                b_out, b_lse, _ = U.attention_bounds(qd[row], k, v, see, there, 128 ** -0.5, 0.0, want, p)
+                assert np.all(np.abs(od[row] - want) <= b_out), (h, t)
+                assert ld[row] == want_lse or abs(ld[row] - want_lse) <= b_lse, (h, t)
 
 
 def test_attention_values_that_are_seen_count(C):
