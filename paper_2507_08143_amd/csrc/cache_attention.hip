@@ -31,8 +31,17 @@ constexpr int ATT_TILE = 32;                 // slots a wave takes at a time
 constexpr int ATT_WAVES = 4;
 constexpr int ATT_STEP = ATT_TILE * ATT_WAVES;
 constexpr int MOST_ROWS = 64;                // query rows of a head: G * T
-constexpr int MOST_SPLITS = 256;
+constexpr int ATT_LEAST_LOG = 1;             // fewest steps of a fragment, log 2
+constexpr int ATT_ROUNDS = 4;                // fragments for every workgroup that there is room for on the chip, at most
+constexpr int ATT_ALONE = 8;                 // steps of a head up to which one workgroup takes all of it
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
+
+// A part of a head that one workgroup does.
+struct Fragment {
+  int head;                    // -1: none
+  int from, to;                // slots
+  int first, parts;            // the head's first fragment, and how many it has
+};
 
 struct Queries {
   const uint16_t *q;
@@ -43,22 +52,14 @@ struct Queries {
   const int32_t *new_tokens;
   int tokens, group;           // T, and G query heads a kv head; row t * G + g of a head
   float scale, softcap;
-  int splits, least;           // workgroups a head, and the fewest slots that one takes (whole steps)
-  float *partial;              // splits > 1: [head][split][row][D], relative to 2^m
-  float2 *stats;               // [head][split][row]: m (base 2) and the sum of 2^(x - m)
+  int frags_most, target;      // fragments that there is room for, and how many there are to be if no head were shorter; 0: one a head
+  Fragment *frags;             // [frags_most]
+  int2 *head_frags;            // [head]: its first fragment, and how many
+  float *partial;              // [frags_most][row][D], relative to 2^m
+  float2 *stats;               // [frags_most][row]: m (base 2) and the sum of 2^(x - m)
   float *logits;               // accumulate: [head][row][pitch], base 2; else null
   int most, pitch;             // slots that there is room for
 };
-
-// Slots of one workgroup of a head that holds `count`: whole steps, so that at most Q.splits of them have any.
-__device__ __forceinline__ int slots_of_split(const Queries &Q, int count) {
-  const int even = (int)(((unsigned)count + (unsigned)Q.splits - 1) / (unsigned)Q.splits);
-  const int c = (int)(((unsigned)even + ATT_STEP - 1) / ATT_STEP * ATT_STEP);
-  return c > Q.least ? c : Q.least;
-}
-__device__ __forceinline__ int splits_with_slots(int count, int chunk) {
-  return count > 0 ? (int)(((unsigned)count + (unsigned)chunk - 1) / (unsigned)chunk) : 1;
-}
 
 // What query row t of n new tokens sees of `count` slots.
 __device__ __forceinline__ int sees(int count, int n, int t) { return t < n ? max(count - (n - 1 - t), 0) : 0; }
@@ -152,13 +153,16 @@ __device__ __forceinline__ void load_rows(const uint16_t *base, const Places<PAG
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       const char *half = reinterpret_cast<const char *>(base + from_lane(P.off, 2 * tile + (i >> 2)));
-      x[i].u = load_stream16((K ? half + 64 * (i & 3) : half + (i & 3) * (long long)stride) + lane_at);
+      const char *at = (K ? half + 64 * (i & 3) : half + (i & 3) * (long long)stride) + lane_at;
+      // (the two halves of a 128-byte line of K are read by two instructions: streaming, the second would miss again)
+      x[i].u = K ? *reinterpret_cast<const uint4 *>(at) : load_stream16(at);
     }
   } else {
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       const long long off = __shfl(P.off, 16 * (i >> 2) + (K ? lane & 15 : 4 * (lane >> 4) + (i & 3)));
-      x[i].u = load_stream16(base + off + (K ? 8 * (lane >> 4) + 32 * (i & 3) : 8 * (lane & 15)));
+      const uint16_t *at = base + off + (K ? 8 * (lane >> 4) + 32 * (i & 3) : 8 * (lane & 15));
+      x[i].u = K ? *reinterpret_cast<const uint4 *>(at) : load_stream16(at);
     }
   }
 }
@@ -200,21 +204,80 @@ struct AttendLds {
   float lse2[16 * NT];
 };
 
+// Steps of ATT_STEP slots of a head: one at least, so that every head has a workgroup that writes its rows.
+__device__ __forceinline__ int steps_of(int count, int n) { return n > 0 && count > ATT_STEP ? (int)(((unsigned)count + ATT_STEP - 1) / ATT_STEP) : 1; }
+__device__ __forceinline__ int head_steps(const CacheView &C, const Queries &Q, unsigned g) {
+  const HeadOf w = head_of(C, g);
+  return steps_of(held(C, w.b, w.l, w.h), tokens_new(Q.new_tokens, w.b, Q.tokens));
+}
+
+// Sum over the lanes up to this one (row shifts, then the sums of rows and of halves of the wave handed on).
+__device__ __forceinline__ int wave_scan(int x) {
+  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);
+  return x;
+}
+
+// How long a head is only the device knows, so every workgroup finds its part by itself: heads are cut into fragments of the same
+// number of steps, a power of two so that all heads together have at most `target` of them beside the last of each head,
+// and fragments are numbered head after head.  Every wave does it alone, 64 heads at a time, without a barrier.
+// (Cutting every head into the same number of parts leaves the longest ones' parts as the last to end: 16 requests of 68 to
+// 55778 slots a head 217 us against 200.  A run of steps for every unit, across heads, is no better than parts of one size: units are not
+// equally fast.)  -> false: there is no such fragment.
+struct Part { int head, steps, step0, step1, first, parts; };
+__device__ __forceinline__ bool find_part(const CacheView &C, const Queries &Q, int fragment, Part &P) {
+  const int heads = C.nreq * C.layers * C.kv_heads, lane = threadIdx.x & 63;
+  int mine = 0, kept = 0;                           // kept: steps of head `lane`
+  for (int h = lane; h < heads; h += 64) {
+    const int x = head_steps(C, Q, (unsigned)h);
+    if (h < 64) kept = x;
+    mine += x;
+  }
+  const int total = __builtin_amdgcn_readlane(wave_scan(mine), 63);          // the host has seen to it that this fits
+  int p = ATT_LEAST_LOG;
+  while ((total - 1) >> p >= Q.target) ++p;
+  int before = 0;
+  for (int h0 = 0; h0 < heads; h0 += 64) {
+    const int h = h0 + lane, steps = h0 == 0 ? kept : h < heads ? head_steps(C, Q, (unsigned)h) : 0;
+    const int parts = (steps + (1 << p) - 1) >> p, upto = before + wave_scan(parts);
+    const unsigned long long beyond = __ballot(upto > fragment);
+    if (beyond != 0) {
+      const int at = __builtin_ctzll(beyond);
+      P.head = h0 + at;
+      P.steps = __builtin_amdgcn_readlane(steps, at);
+      P.parts = __builtin_amdgcn_readlane(parts, at);
+      P.first = __builtin_amdgcn_readlane(upto, at) - P.parts;
+      P.step0 = (fragment - P.first) << p;
+      P.step1 = min(P.step0 + (1 << p), P.steps);
+      return true;
+    }
+    before = __builtin_amdgcn_readlane(upto, 63);
+  }
+  return false;
+}
+
 template <int NT, bool PAGE16>
 __global__ __launch_bounds__(256, NT == 1 ? 3 : NT == 2 ? 2 : 1) void attend_kernel(const CacheView C, const Queries Q) {
   __shared__ AttendLds<NT> L;
-  const unsigned heads = (unsigned)C.nreq * (unsigned)C.layers * (unsigned)C.kv_heads;
-  const unsigned part = blockIdx.x / heads, g = blockIdx.x - part * heads;
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, n16 = lane & 15, j = lane >> 4;
+  const int R = Q.tokens * Q.group;
+  Part part{(int)blockIdx.x, 0, 0, 0x7fffffff, 0, 1};
+  if (Q.target > 0 && !find_part(C, Q, (int)blockIdx.x, part)) {
+    if (tid == 0) Q.frags[blockIdx.x].head = -1;
+    return;
+  }
+  const unsigned g = (unsigned)part.head;
   const HeadOf w = head_of(C, g);
   const HeadPlace hp = head_place(C, w);
   const int count = held(C, w.b, w.l, w.h), n = tokens_new(Q.new_tokens, w.b, Q.tokens);
-  const int R = Q.tokens * Q.group;
-  const int chunk = slots_of_split(Q, count);
-  const long long begin = (long long)part * chunk;
-  if (part > 0 && begin >= count) return;
-  const int end = n > 0 ? (int)min(begin + chunk, (long long)count) : 0;        // no queries: no tiles
-  const int first = (int)begin + wave * ATT_TILE;                               // of the wave's tiles, ATT_STEP apart
+  const int steps = steps_of(count, n), step0 = part.step0, step1 = min(part.step1, steps);
+  const bool complete = part.parts == 1;
+  const int end = n > 0 ? (step1 == steps ? count : step1 * ATT_STEP) : 0;      // no queries: no tiles
+  const int first = step0 * ATT_STEP + wave * ATT_TILE;                         // of the wave's tiles, ATT_STEP apart
   const int tiles = first < end ? (end - first + ATT_STEP - 1) / ATT_STEP : 0;
   const int seen_by_all = count - (n - 1);
   const uint16_t *kp = C.k + hp.rows, *vp = C.v + hp.rows;
@@ -427,7 +490,10 @@ __global__ __launch_bounds__(256, NT == 1 ? 3 : NT == 2 ? 2 : 1) void attend_ker
     }
   }
   __syncthreads();
-  const bool last = Q.splits == 1;
+  if (Q.target > 0 && tid == 0) {
+    Q.frags[blockIdx.x] = Fragment{complete ? -1 : (int)g, step0 * ATT_STEP, end, part.first, part.parts};
+    if (step0 == 0) Q.head_frags[g] = make_int2(part.first, part.parts);
+  }
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt) {
     const int r = 16 * nt + n16;
@@ -458,11 +524,11 @@ __global__ __launch_bounds__(256, NT == 1 ? 3 : NT == 2 ? 2 : 1) void attend_ker
       for (int i = 1; i < ATT_WAVES; ++i) o[c] += *reinterpret_cast<const f32x4 *>(&L.o[i][tid >> 4][ch + 4 * c]);
     }
     if (row < R) {
-      if (last) {
+      if (complete) {
         finish_row(C, Q, w, row, ch, o, mm, sum);
         if (ch == 0) L.lse2[row] = sum == 0.f ? INFINITY : mm + __builtin_amdgcn_logf(sum);
       } else {
-        const long long at = ((long long)g * Q.splits + part) * R + row;
+        const long long at = (long long)blockIdx.x * R + row;
         f32x4 *to = reinterpret_cast<f32x4 *>(Q.partial + at * D + ch);
         to[0] = o[0];
         to[1] = o[1];
@@ -470,55 +536,51 @@ __global__ __launch_bounds__(256, NT == 1 ? 3 : NT == 2 ? 2 : 1) void attend_ker
       }
     }
   }
-  if (last && store) {
+  if (complete && store) {
     __threadfence_block();
     __syncthreads();                                // the workgroup's logits and sums
     add_mass(C, Q, hp, L.lse2, logits, R, 0, count, n > 0);
   }
 }
 
-// Second launch: the workgroups of a head meet.  The first R workgroups of a head take a query row each, 16 splits side by side
-// and 8 channels a thread; the others add the weights of JOIN_SLOTS slots to the mass.
-constexpr int JOIN_SLOTS = 2048;
+// Second launch: the fragments of a head meet.  The first heads * R workgroups take a query row each, 16 fragments side by side
+// and 8 channels a thread; the others add a fragment's weights to the mass, MASS_PARTS to a fragment.
+constexpr int MASS_PARTS = 2;
 
-// Row r's maximum and sum over the splits, by all threads; every thread gets them.
-__device__ __forceinline__ float2 join_stats(const float2 *stats, int splits, float (&red)[2][4]) {
+// Maximum and sum of row r over the fragments, by the lanes of a wave.
+__device__ __forceinline__ float2 join_stats(const Queries &Q, int first, int parts, int R, int r) {
   float m = -INFINITY, l = 0.f;
-  if ((int)threadIdx.x < splits) {
-    const float2 x = stats[0];
-    m = x.x;
-    l = x.y;
+  for (int k = threadIdx.x & 63; k < parts; k += 64) {
+    const float2 x = Q.stats[(long long)(first + k) * R + r];
+    const float to = fmaxf(m, x.x);
+    l = to == -INFINITY ? 0.f : l * exp2_(m - to) + x.y * exp2_(x.x - to);
+    m = to;
   }
   float top = m;
   for (int d = 32; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
-  if ((threadIdx.x & 63) == 0) red[0][threadIdx.x >> 6] = top;
-  __syncthreads();
-  top = fmaxf(fmaxf(red[0][0], red[0][1]), fmaxf(red[0][2], red[0][3]));
   float sum = top == -INFINITY ? 0.f : l * exp2_(m - top);
   for (int d = 32; d > 0; d >>= 1) sum += __shfl_xor(sum, d);
-  if ((threadIdx.x & 63) == 0) red[1][threadIdx.x >> 6] = sum;
-  __syncthreads();
-  return make_float2(top, (red[1][0] + red[1][1]) + (red[1][2] + red[1][3]));
+  return make_float2(top, sum);
 }
 
-__global__ __launch_bounds__(256) void attend_join_kernel(const CacheView C, const Queries Q, unsigned per_head) {
-  __shared__ float red[2][4], part_o[16][D + 4], lse2[MOST_ROWS];
-  const unsigned g = blockIdx.x / per_head;
-  const int i = (int)(blockIdx.x - g * per_head), tid = threadIdx.x, R = Q.tokens * Q.group;
-  const HeadOf w = head_of(C, g);
-  const int count = held(C, w.b, w.l, w.h);
-  const int splits = splits_with_slots(count, slots_of_split(Q, count));       // at most MOST_SPLITS = the threads
-  const long long base = (long long)g * Q.splits * R;
-  if (i < R) {
-    const float2 all = join_stats(Q.stats + base + (long long)min(tid, splits - 1) * R + i, splits, red);
+__global__ __launch_bounds__(256) void attend_join_kernel(const CacheView C, const Queries Q) {
+  __shared__ float part_o[16][D + 4], lse2[MOST_ROWS];
+  const int tid = threadIdx.x, R = Q.tokens * Q.group;
+  const unsigned rows = (unsigned)C.nreq * (unsigned)C.layers * (unsigned)C.kv_heads * (unsigned)R;
+  if (blockIdx.x < rows) {
+    const unsigned g = blockIdx.x / (unsigned)R;
+    const int r = (int)(blockIdx.x - g * (unsigned)R);
+    const int2 f = Q.head_frags[g];
+    if (f.y < 2) return;                            // its only workgroup has finished it
+    const float2 all = join_stats(Q, f.x, f.y, R, r);      // (every wave)
     const int sl = tid >> 4, ch = 8 * (tid & 15);
     f32x4 o[2] = {f32x4{0.f, 0.f, 0.f, 0.f}, f32x4{0.f, 0.f, 0.f, 0.f}};
-    for (int s = sl; s < splits; s += 16) {
-      const long long at = base + (long long)s * R + i;
-      const float m = Q.stats[at].x, f = all.x == -INFINITY ? 0.f : exp2_(m - all.x);
+    for (int k = sl; k < f.y; k += 16) {
+      const long long at = (long long)(f.x + k) * R + r;
+      const float mk = Q.stats[at].x, scale = all.x == -INFINITY ? 0.f : exp2_(mk - all.x);
       const f32x4 *x = reinterpret_cast<const f32x4 *>(Q.partial + at * D + ch);
-      o[0] += x[0] * f;
-      o[1] += x[1] * f;
+      o[0] += x[0] * scale;
+      o[1] += x[1] * scale;
     }
     *reinterpret_cast<f32x4 *>(&part_o[sl][ch]) = o[0];
     *reinterpret_cast<f32x4 *>(&part_o[sl][ch + 4]) = o[1];
@@ -530,30 +592,23 @@ __global__ __launch_bounds__(256) void attend_join_kernel(const CacheView C, con
         o[0] += *reinterpret_cast<const f32x4 *>(&part_o[s][ch]);
         o[1] += *reinterpret_cast<const f32x4 *>(&part_o[s][ch + 4]);
       }
-      finish_row(C, Q, w, i, ch, o, all.x, all.y);
+      finish_row(C, Q, head_of(C, g), r, ch, o, all.x, all.y);
     }
     return;
   }
-  const int from = (i - R) * JOIN_SLOTS;
-  if (from >= count || count > Q.most) return;
-  // every wave takes rows in turn
-  for (int r = tid >> 6; r < R; r += 4) {
-    float m = -INFINITY, l = 0.f;
-    for (int s = tid & 63; s < splits; s += 64) {
-      const float2 x = Q.stats[base + (long long)s * R + r];
-      const float to = fmaxf(m, x.x);
-      l = to == -INFINITY ? 0.f : l * exp2_(m - to) + x.y * exp2_(x.x - to);
-      m = to;
-    }
-    float top = m;
-    for (int d = 32; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
-    float sum = top == -INFINITY ? 0.f : l * exp2_(m - top);
-    for (int d = 32; d > 0; d >>= 1) sum += __shfl_xor(sum, d);
-    if ((tid & 63) == 0) lse2[r] = sum == 0.f ? INFINITY : top + __builtin_amdgcn_logf(sum);
+  const unsigned i = (blockIdx.x - rows) / MASS_PARTS;
+  const int part = (int)(blockIdx.x - rows - i * MASS_PARTS);
+  const Fragment f = Q.frags[i];
+  if (f.head < 0) return;
+  const HeadOf w = head_of(C, (unsigned)f.head);
+  if (held(C, w.b, w.l, w.h) > Q.most) return;
+  for (int r = tid >> 6; r < R; r += 4) {          // every wave takes rows in turn
+    const float2 all = join_stats(Q, f.first, f.parts, R, r);
+    if ((tid & 63) == 0) lse2[r] = all.y == 0.f ? INFINITY : all.x + __builtin_amdgcn_logf(all.y);
   }
   __syncthreads();
-  const int to = count - from < JOIN_SLOTS ? count : from + JOIN_SLOTS;
-  add_mass(C, Q, head_place(C, w), lse2, Q.logits + (long long)g * R * Q.pitch, R, from, to, tokens_new(Q.new_tokens, w.b, Q.tokens) > 0);
+  const int each = (f.to - f.from + MASS_PARTS - 1) / MASS_PARTS, from = f.from + part * each;
+  add_mass(C, Q, head_place(C, w), lse2, Q.logits + (long long)f.head * R * Q.pitch, R, from, min(from + each, f.to), true);
 }
 
 static int query_check(const compactor_cache_query_t *q, const CacheView &C) {
@@ -569,9 +624,9 @@ static int query_most(const CacheView &C, const compactor_cache_query_t *q) {
 }
 
 struct AttendPlan {
-  int rows, splits, least, pitch;
-  size_t partial, stats, logits;       // bytes, in this order in the workspace
-  size_t bytes() const { return partial + stats + logits; }
+  int rows, frags_most, target, pitch;
+  size_t frags, head_frags, partial, stats, logits;       // bytes, in this order in the workspace
+  size_t bytes() const { return frags + head_frags + partial + stats + logits; }
 };
 
 static AttendPlan attend_plan(const CacheView &C, const compactor_cache_query_t *q) {
@@ -581,15 +636,20 @@ static AttendPlan attend_plan(const CacheView &C, const compactor_cache_query_t 
     cus = 256;
   AttendPlan A;
   const long long heads = (long long)C.nreq * C.layers * C.kv_heads, most = query_most(C, q);
+  const long long steps = (most + ATT_STEP - 1) / ATT_STEP;
   A.rows = q->tokens * (q->q_heads / C.kv_heads);
-  A.least = 64 * A.rows < 256 ? 256 : (64 * A.rows + ATT_STEP - 1) / ATT_STEP * ATT_STEP;
-  long long splits = 24ll * cus / heads;
-  splits = std::min(splits, (most + A.least - 1) / A.least);
-  A.splits = (int)std::min(std::max(splits, 1ll), (long long)MOST_SPLITS);
+  A.target = A.frags_most = 0;
+  if (steps > ATT_ALONE && heads * steps <= 0x7fffffffll) {
+    A.target = ATT_ROUNDS * (A.rows <= 16 ? 3 : A.rows <= 32 ? 2 : 1) * cus;
+    A.frags_most = (int)std::min((long long)A.target, ((heads * steps - 1) >> ATT_LEAST_LOG) + 1) + (int)heads;
+  }
   A.pitch = (int)((most + ATT_TILE - 1) / ATT_TILE * ATT_TILE);
   auto up = [](size_t x) { return (x + 255) / 256 * 256; };
-  A.partial = A.splits > 1 ? up((size_t)heads * A.splits * A.rows * D * sizeof(float)) : 0;
-  A.stats = A.splits > 1 ? up((size_t)heads * A.splits * A.rows * sizeof(float2)) : 0;
+  const size_t n = A.frags_most;
+  A.frags = up(n * sizeof(Fragment));
+  A.head_frags = n > 0 ? up((size_t)heads * sizeof(int2)) : 0;
+  A.partial = up(n * A.rows * D * sizeof(float));
+  A.stats = up(n * A.rows * sizeof(float2));
   A.logits = q->accumulate ? up((size_t)heads * A.rows * A.pitch * sizeof(float)) : 0;
   return A;
 }
@@ -641,8 +701,9 @@ int compactor_cache_attention(const compactor_cache_t *cache, const compactor_ca
   if (need > 0 && (!workspace || workspace_bytes < need)) return COMPACTOR_EWORKSPACE;
   if (need > 0 && (reinterpret_cast<uintptr_t>(workspace) & 255u)) return COMPACTOR_EALIGN;
   const long long heads = (long long)C.nreq * C.layers * C.kv_heads;
-  const long long parts = (long long)A.rows + (query->accumulate ? (query_most(C, query) + JOIN_SLOTS - 1) / JOIN_SLOTS : 0);
-  if (heads * A.splits > 0x7fffffffll || (A.splits > 1 && heads * parts > 0x7fffffffll)) return COMPACTOR_EINVAL;
+  const long long blocks = A.target > 0 ? A.frags_most : heads;
+  const long long join = A.target > 0 ? heads * A.rows + (query->accumulate ? (long long)MASS_PARTS * A.frags_most : 0) : 0;
+  if (blocks > 0x7fffffffll || join > 0x7fffffffll) return COMPACTOR_EINVAL;
   Queries Q;
   Q.q = static_cast<const uint16_t *>(query->q);
   Q.out = static_cast<uint16_t *>(query->out);
@@ -656,24 +717,26 @@ int compactor_cache_attention(const compactor_cache_t *cache, const compactor_ca
   Q.group = query->q_heads / C.kv_heads;
   Q.scale = query->scale > 0.f ? query->scale : 1.0f / sqrtf((float)D);
   Q.softcap = query->softcap;
-  Q.splits = A.splits;
-  Q.least = A.least;
+  Q.target = A.target;
+  Q.frags_most = A.frags_most;
   unsigned char *ws = static_cast<unsigned char *>(workspace);
-  Q.partial = reinterpret_cast<float *>(ws);
-  Q.stats = reinterpret_cast<float2 *>(ws + A.partial);
-  Q.logits = query->accumulate ? reinterpret_cast<float *>(ws + A.partial + A.stats) : nullptr;
+  Q.frags = reinterpret_cast<Fragment *>(ws);
+  Q.head_frags = reinterpret_cast<int2 *>(ws += A.frags);
+  Q.partial = reinterpret_cast<float *>(ws += A.head_frags);
+  Q.stats = reinterpret_cast<float2 *>(ws += A.partial);
+  Q.logits = query->accumulate ? reinterpret_cast<float *>(ws += A.stats) : nullptr;
   Q.most = query_most(C, query);
   Q.pitch = A.pitch;
   hipStream_t st = static_cast<hipStream_t>(stream);
   (void)hipGetLastError();   // a leftover of earlier, unrelated HIP calls is not this call's error
   // halves of tiles with one origin, and offsets inside one that fit 32 bits
   if (C.page_size % 16 == 0 && C.slot_stride <= (1 << 24))
-    launch_attend<true>(C, Q, (unsigned)(heads * A.splits), st);
+    launch_attend<true>(C, Q, (unsigned)blocks, st);
   else
-    launch_attend<false>(C, Q, (unsigned)(heads * A.splits), st);
-  if (A.splits > 1) {
+    launch_attend<false>(C, Q, (unsigned)blocks, st);
+  if (A.target > 0) {
     if (hipGetLastError() != hipSuccess) return COMPACTOR_EHIP;
-    hipLaunchKernelGGL(attend_join_kernel, dim3((unsigned)(heads * parts)), dim3(256), 0, st, C, Q, (unsigned)parts);
+    hipLaunchKernelGGL(attend_join_kernel, dim3((unsigned)join), dim3(256), 0, st, C, Q);
   }
   return hipGetLastError() == hipSuccess ? COMPACTOR_OK : COMPACTOR_EHIP;
 }
