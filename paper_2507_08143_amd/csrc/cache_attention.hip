@@ -31,8 +31,8 @@ constexpr int ATT_TILE = 32;                 // slots a wave takes at a time
 constexpr int ATT_WAVES = 4;
 constexpr int ATT_STEP = ATT_TILE * ATT_WAVES;
 constexpr int MOST_ROWS = 64;                // query rows of a head: G * T
-constexpr int ATT_LEAST_LOG = 1;             // fewest steps of a fragment, log 2
-constexpr int ATT_ROUNDS = 4;                // fragments for every workgroup that there is room for on the chip, at most
+constexpr int ATT_LEAST_LOG = 2;             // fewest steps of a fragment, log 2
+constexpr int ATT_ROUNDS = 6;                // fragments for every workgroup that there is room for on the chip, at most
 constexpr int ATT_ALONE = 8;                 // steps of a head up to which one workgroup takes all of it
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 
@@ -116,8 +116,8 @@ struct Places {
 
 template <bool PAGE16>
 __device__ __forceinline__ void places_run(const CacheView &C, const HeadPlace &p, int first, int count, int lane, Places<PAGE16> &P) {
-  // PAGE16: halves of the tiles at first, first + ATT_STEP, ...
-  const long long slot = (long long)first + (lane >> 1) * ATT_STEP + 16 * (lane & 1);
+  // PAGE16: halves of the tiles from `first` on
+  const long long slot = (long long)first + 16 * lane;
   bool ok = slot < count;
   const int i = page_number(ok ? (unsigned)slot : 0u, C.div_mul, C.div_shift);
   const int page = ok ? p.table[i] : 0;
@@ -183,23 +183,39 @@ __device__ __forceinline__ void finish_row(const CacheView &C, const Queries &Q,
         sum == 0.f ? -INFINITY : LN2 * (m + __builtin_amdgcn_logf(sum));
 }
 
-// Adds the weights of slots [from, to) to the head's mass: 1/G sum over rows of 2^(x - lse2), lse2 = inf for a row without
-// weights.
+// Adds the weights of slots [from, to), from a multiple of 4, to the head's mass: 1/G sum over rows of 2^(x - lse2), lse2 = inf for a
+// row without weights.
 __device__ __forceinline__ void add_mass(const CacheView &C, const Queries &Q, const HeadPlace &hp, const float *lse2, const float *logits,
-                                         int R, int from, int to, bool any) {
-  if (!any) return;
+                                         int R, int from, int to) {
   const float inv = 1.f / (float)Q.group;
-  for (int s = from + (int)threadIdx.x; s < to; s += 256) {
-    const SlotPlace at = slot_place(C, hp, s);
-    float x = 0.f;
-    for (int r = 0; r < R; ++r) x += lse2[r] == INFINITY ? 0.f : exp2_(logits[(long long)r * Q.pitch + s] - lse2[r]);
-    if (page_there(C, at.page)) C.mass[state_at(C, hp, at)] += x * inv;
+  for (int s = from + 4 * (int)threadIdx.x; s < to; s += 4 * 256) {
+    SlotPlace at[4];
+    float *mass[4], old[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      at[i] = slot_place(C, hp, min(s + i, to - 1));
+      mass[i] = C.mass + state_at(C, hp, SlotPlace{page_there(C, at[i].page) ? at[i].page : 0, at[i].at});
+      old[i] = *mass[i];
+    }
+    f32x4 x = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll 4
+    for (int r = 0; r < R; ++r) {
+      const f32x4 y = *reinterpret_cast<const f32x4 *>(logits + (long long)r * Q.pitch + s);
+      const float z = lse2[r];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) x[i] += z == INFINITY ? 0.f : exp2_(y[i] - z);
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (s + i < to && page_there(C, at[i].page)) *mass[i] = fmaf(x[i], inv, old[i]);
   }
 }
 
+constexpr int KEPT_FLOATS = ATT_TILE * MOST_ROWS;      // logits that a wave keeps in LDS: a tile at least
 template <int NT>
 struct AttendLds {
   float o[ATT_WAVES][16][D + 4];
+  float kept[ATT_WAVES][KEPT_FLOATS], p[ATT_WAVES][16][ATT_TILE + 1];
   float m[ATT_WAVES][16 * NT], l[ATT_WAVES][16 * NT];
   float lse2[16 * NT];
 };
@@ -261,7 +277,7 @@ __device__ __forceinline__ bool find_part(const CacheView &C, const Queries &Q, 
 }
 
 template <int NT, bool PAGE16>
-__global__ __launch_bounds__(256, NT == 1 ? 3 : NT == 2 ? 2 : 1) void attend_kernel(const CacheView C, const Queries Q) {
+__global__ __launch_bounds__(256, NT <= 2 ? 2 : 1) void attend_kernel(const CacheView C, const Queries Q) {
   __shared__ AttendLds<NT> L;
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, n16 = lane & 15, j = lane >> 4;
   const int R = Q.tokens * Q.group;
@@ -277,8 +293,9 @@ __global__ __launch_bounds__(256, NT == 1 ? 3 : NT == 2 ? 2 : 1) void attend_ker
   const int steps = steps_of(count, n), step0 = part.step0, step1 = min(part.step1, steps);
   const bool complete = part.parts == 1;
   const int end = n > 0 ? (step1 == steps ? count : step1 * ATT_STEP) : 0;      // no queries: no tiles
-  const int first = step0 * ATT_STEP + wave * ATT_TILE;                         // of the wave's tiles, ATT_STEP apart
-  const int tiles = first < end ? (end - first + ATT_STEP - 1) / ATT_STEP : 0;
+  // every wave has a run of the part's tiles
+  const int begin = step0 * ATT_STEP, each = (max(end - begin, 0) + ATT_STEP - 1) / ATT_STEP, first = begin + wave * each * ATT_TILE;
+  const int tiles = first < end ? min(each, (end - first + ATT_TILE - 1) / ATT_TILE) : 0;
   const int seen_by_all = count - (n - 1);
   const uint16_t *kp = C.k + hp.rows, *vp = C.v + hp.rows;
 
@@ -288,7 +305,7 @@ __global__ __launch_bounds__(256, NT == 1 ? 3 : NT == 2 ? 2 : 1) void attend_ker
   } else {
     places_fetch(C, hp, first, count, lane, P);
     places_take(C, P);
-    places_fetch(C, hp, (long long)first + ATT_STEP, count, lane, P);
+    places_fetch(C, hp, (long long)first + ATT_TILE, count, lane, P);
   }
   // query rows as B operands: lane l has row l & 15, channels 32 kk + 8 (l >> 4) ..
   Piece q[NT][4];
@@ -306,17 +323,16 @@ __global__ __launch_bounds__(256, NT == 1 ? 3 : NT == 2 ? 2 : 1) void attend_ker
   }
   Piece k[8], v[8];
   const unsigned stride = PAGE16 ? 2u * (unsigned)C.slot_stride : 0u, k_at = n16 * stride + 16 * j, v_at = 4 * j * stride + 16 * n16;
-  unsigned there = 0;            // bit i: slot i of the tile holds a token whose page is there
   auto tile_there = [&](int tile) {
     if (!PAGE16) return (unsigned)P.there;
     const unsigned two = (unsigned)(P.there >> (2 * (tile & 31)));
     return (two & 1u ? 0xffffu : 0u) | (two & 2u ? 0xffff0000u : 0u);
   };
-  if (tiles > 0) {
-    load_rows<PAGE16, true>(kp, P, 0, lane, k_at, stride, k);
-    load_rows<PAGE16, false>(vp, P, 0, lane, v_at, stride, v);
-    there = tile_there(0);
-  }
+  // No load of rows is under a condition, or the compiler would have to wait for V where it waits for K: behind the last tile all
+  // lanes load one piece of rows that exist.
+  load_rows<PAGE16, true>(kp, P, 0, lane, tiles > 0 ? k_at : 0u, stride, k);
+  load_rows<PAGE16, false>(vp, P, 0, lane, tiles > 0 ? v_at : 0u, stride, v);
+  unsigned there = tile_there(0);          // bit i: slot i of the tile holds a token whose page is there
 
   f32x4 acc[NT][8];
   float m[NT], l[NT];            // of query l & 15: reference of its exponents, the lane's part of their sum
@@ -331,9 +347,22 @@ __global__ __launch_bounds__(256, NT == 1 ? 3 : NT == 2 ? 2 : 1) void attend_ker
   const float to_base2 = Q.scale * LOG2E, to_tanh = capped ? 2.f * LOG2E * Q.scale / Q.softcap : 0.f, cap2 = Q.softcap * LOG2E;
   const bool store = Q.logits != nullptr && count <= Q.most;
   float *logits = Q.logits + (long long)g * R * Q.pitch;
+  // Logits wait in LDS and leave at the end, behind the last barrier, which would else wait until they have arrived (batch of 2.3 M
+  // slots, 4 rows: 229 us against 205, without them 201); where that is full, on the way.
+  float *kept = L.kept[wave];
+  const int kept_tiles = max(1, KEPT_FLOATS / (ATT_TILE * R));
+  auto leave = [&](int upto) {              // tiles up to this one
+    wave_lds_fence();
+    const int t0 = (upto - 1) / kept_tiles * kept_tiles, quads = (upto - t0) * (ATT_TILE / 4);
+    for (int row = 0; row < R; ++row)
+      for (int u = lane; u < quads; u += 64)
+        *reinterpret_cast<f32x4 *>(logits + (long long)row * Q.pitch + first + t0 * ATT_TILE + 4 * u) =
+            *reinterpret_cast<const f32x4 *>(kept + ((u >> 3) * R + row) * ATT_TILE + 4 * (u & 7));
+    wave_lds_fence();
+  };
 
   for (int tile = 0; tile < tiles; ++tile) {
-    const int s0 = first + tile * ATT_STEP;
+    const int s0 = first + tile * ATT_TILE;
     const bool more = tile + 1 < tiles;
     f32x4 s[NT][2];
 #pragma unroll
@@ -345,18 +374,16 @@ __global__ __launch_bounds__(256, NT == 1 ? 3 : NT == 2 ? 2 : 1) void attend_ker
         for (int kk = 0; kk < 4; ++kk)
           s[nt][half] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[4 * half + kk].v, q[nt][kk].v, s[nt][half], 0, 0, 0);
       }
-    // K of the next tile leaves as soon as its registers are free, V after the second product
-    unsigned there_next = 0;
-    if (more) {
-      if (PAGE16) {
-        if (((tile + 1) & 31) == 0) places_run(C, hp, s0 + ATT_STEP, count, lane, P);
-      } else {
-        places_take(C, P);
-        places_fetch(C, hp, (long long)s0 + 2 * ATT_STEP, count, lane, P);
-      }
-      load_rows<PAGE16, true>(kp, P, (tile + 1) & 31, lane, k_at, stride, k);
-      there_next = tile_there(tile + 1);
+    // K of the next tile leaves as soon as its registers are free, V after the second product.
+    if (PAGE16) {
+      if (more && ((tile + 1) & 31) == 0) places_run(C, hp, s0 + ATT_TILE, count, lane, P);
+    } else {
+      places_take(C, P);
+      places_fetch(C, hp, (long long)s0 + 2 * ATT_TILE, count, lane, P);
     }
+    const unsigned spread = more ? 0xffffffffu : 0u;
+    load_rows<PAGE16, true>(kp, P, (tile + 1) & 31, lane, k_at & spread, stride, k);
+    const unsigned there_next = tile_there(tile + 1);
     __builtin_amdgcn_sched_barrier(0);
     const int left = count - s0;
     if (left < 32) there &= (1u << left) - 1u;              // left >= 1
@@ -407,7 +434,7 @@ __global__ __launch_bounds__(256, NT == 1 ? 3 : NT == 2 ? 2 : 1) void attend_ker
         }
       }
       if (store && 16 * nt + n16 < R) {
-        float *to = logits + (long long)(16 * nt + n16) * Q.pitch + s0 + 4 * j;
+        float *to = kept + ((tile % kept_tiles) * R + 16 * nt + n16) * ATT_TILE + 4 * j;
         *reinterpret_cast<f32x4 *>(to) = f32x4{x[0], x[1], x[2], x[3]};
         *reinterpret_cast<f32x4 *>(to + 16) = f32x4{x[4], x[5], x[6], x[7]};
       }
@@ -437,7 +464,7 @@ __global__ __launch_bounds__(256, NT == 1 ? 3 : NT == 2 ? 2 : 1) void attend_ker
         lo[nt].w[i] = pack_bf16(x[2 * i] - __uint_as_float(hi[nt].w[i] << 16), x[2 * i + 1] - __uint_as_float(hi[nt].w[i] & 0xffff0000u));
       }
       if (__builtin_expect(ahead, 0)) {
-        float *mine = L.o[wave][n16];        // (of the wave alone until the waves meet)
+        float *mine = L.p[wave][n16];
         wave_lds_fence();
 #pragma unroll
         for (int i = 0; i < 8; ++i) mine[16 * (i >> 2) + 4 * j + (i & 3)] = x[i];
@@ -459,6 +486,7 @@ __global__ __launch_bounds__(256, NT == 1 ? 3 : NT == 2 ? 2 : 1) void attend_ker
         }
       }
     }
+    if (store && more && (tile + 1) % kept_tiles == 0) leave(tile + 1);
     // channels 2 d and 2 d + 1 of the lane's piece, 8 slots each
 #pragma unroll
     for (int c = 0; c < 8; ++c) {
@@ -471,7 +499,7 @@ __global__ __launch_bounds__(256, NT == 1 ? 3 : NT == 2 ? 2 : 1) void attend_ker
         acc[nt][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.v, lo[nt].v, acc[nt][c], 0, 0, 0);
       }
     }
-    if (more) load_rows<PAGE16, false>(vp, P, (tile + 1) & 31, lane, v_at, stride, v);
+    load_rows<PAGE16, false>(vp, P, (tile + 1) & 31, lane, v_at & spread, stride, v);
     there = there_next;
     __builtin_amdgcn_sched_barrier(0);
   }
@@ -536,16 +564,17 @@ __global__ __launch_bounds__(256, NT == 1 ? 3 : NT == 2 ? 2 : 1) void attend_ker
       }
     }
   }
-  if (complete && store) {
+  if (store && tiles > 0) leave(tiles);
+  if (complete && store && n > 0) {
     __threadfence_block();
     __syncthreads();                                // the workgroup's logits and sums
-    add_mass(C, Q, hp, L.lse2, logits, R, 0, count, n > 0);
+    add_mass(C, Q, hp, L.lse2, logits, R, 0, count);
   }
 }
 
 // Second launch: the fragments of a head meet.  The first heads * R workgroups take a query row each, 16 fragments side by side
 // and 8 channels a thread; the others add a fragment's weights to the mass, MASS_PARTS to a fragment.
-constexpr int MASS_PARTS = 2;
+constexpr int MASS_PARTS = 1;
 
 // Maximum and sum of row r over the fragments, by the lanes of a wave.
 __device__ __forceinline__ float2 join_stats(const Queries &Q, int first, int parts, int R, int r) {
@@ -607,8 +636,8 @@ __global__ __launch_bounds__(256) void attend_join_kernel(const CacheView C, con
     if ((tid & 63) == 0) lse2[r] = all.y == 0.f ? INFINITY : all.x + __builtin_amdgcn_logf(all.y);
   }
   __syncthreads();
-  const int each = (f.to - f.from + MASS_PARTS - 1) / MASS_PARTS, from = f.from + part * each;
-  add_mass(C, Q, head_place(C, w), lse2, Q.logits + (long long)f.head * R * Q.pitch, R, from, min(from + each, f.to), true);
+  const int each = ((f.to - f.from + MASS_PARTS - 1) / MASS_PARTS + 3) & ~3, from = f.from + part * each;
+  add_mass(C, Q, head_place(C, w), lse2, Q.logits + (long long)f.head * R * Q.pitch, R, from, min(from + each, f.to));
 }
 
 static int query_check(const compactor_cache_query_t *q, const CacheView &C) {
@@ -640,7 +669,7 @@ static AttendPlan attend_plan(const CacheView &C, const compactor_cache_query_t 
   A.rows = q->tokens * (q->q_heads / C.kv_heads);
   A.target = A.frags_most = 0;
   if (steps > ATT_ALONE && heads * steps <= 0x7fffffffll) {
-    A.target = ATT_ROUNDS * (A.rows <= 16 ? 3 : A.rows <= 32 ? 2 : 1) * cus;
+    A.target = ATT_ROUNDS * (A.rows <= 32 ? 2 : 1) * cus;
     A.frags_most = (int)std::min((long long)A.target, ((heads * steps - 1) >> ATT_LEAST_LOG) + 1) + (int)heads;
   }
   A.pitch = (int)((most + ATT_TILE - 1) / ATT_TILE * ATT_TILE);
