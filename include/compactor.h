@@ -430,7 +430,7 @@ typedef struct compactor_cache_evict_params {
 int compactor_cache_evict(const compactor_cache_t *cache, const compactor_cache_evict_params_t *evict,
                           void *workspace, size_t workspace_bytes, void *stream);
 
-/* Bytes of 256-byte aligned device workspace for compactor_cache_evict.  host. */
+/* Bytes of 256-byte aligned device workspace for compactor_cache_evict; scratch, no state is kept.  0 where none is needed.  host. */
 int compactor_cache_evict_workspace_size(const compactor_cache_t *cache,
                                          const compactor_cache_evict_params_t *evict, size_t *bytes);
 

@@ -2,6 +2,8 @@
 // of it, the state of rows that a compaction has written (admit).  The attention itself: cache_attention.hip.
 #include <string.h>
 
+#include <algorithm>
+
 #include "cache.h"
 
 namespace cmp {
@@ -205,218 +207,517 @@ hipError_t launch_cache_admit(const SegTable &T, const CacheView &C, const int32
 }
 
 // ------------------------------------------------------------------------------------------ evict
-// One workgroup per pool (a head, or the heads of a layer) finds the key of the last token that stays, by radix
-// selection on an order-preserving key (12, 12 and 8 bits), counts what every head keeps and lists its moves: the holes
-// below the new count and the retained tokens from it on, both ascending, as many of the one as of the other.  A second
-// launch moves the rows.  Sources and destinations of a head are disjoint, so the moves need no order.
-constexpr int EVICT_THREADS = 1024, EVICT_WAVES = EVICT_THREADS / 64;
-constexpr uint32_t KEY_PROTECTED = 0xffffffffu;      // above the key of +inf (0xff800000)
-constexpr int EVICT_BINS = 4096;
+// The slots of a pool (a head, or the heads of a layer) are ranked by an order-preserving 32-bit key; the key of the last one
+// that stays and how many of its equals stay (the first ones) is all that the rest needs.  A head that keeps `left` of its
+// tokens moves those in slots from `left` on into the holes below.  Both come out in order from the number `before` of retained
+// tokens in front of a slot: slot s is hole number s - before, and the retained token in slot s >= left has left - 1 - before
+// others behind it.  Sources and destinations of a head are disjoint, so the moves need no order.
+//
+// One workgroup does everything where a pool is a head of up to ALONE_SLOTS tokens; its keys stay in registers.  Longer heads and
+// layers would keep one unit busy too long (some 70 instructions a slot: 32 layers of 79000 tokens 327 us), so there the pool is cut into parts of
+// PART_SLOTS slots and every part's workgroup does the same steps in a launch each: keys and the tally of their first 12 bits,
+// the next 12, the last 8, the lists, the moves.
+constexpr uint32_t KEY_PROTECTED = 0xffffffffu;      // above the key of +inf (0xff800000); 0: NaN, or a page that is not there
 
 struct EvictPlan {
   int budget;
   const int32_t *budgets;
   int sink, recent;
   int pool_heads;              // 1 or kv_heads
-  int most;                    // tokens of a head that the lists have room for
-  int list;                    // ints from one head's lists to the next: `list / 2` destinations, then as many sources
-  int *lists, *moves;          // moves[head]: how many
+  int most;                    // tokens of a head that the launches reach
+  // parts
+  int parts;                   // of a head
+  int pitch, list;             // ints from one head's keys, and lists, to the next: `list / 2` destinations, then as many sources
+  int *hist1, *hist2, *hist3;  // [pool][4096], [pool][256]: tallies of the first, the next 12 and the last 8 bits
+  int *moves;                  // [head]: how many
+  int *left;                   // [head]: the new count, -1 where nothing changes
+  int2 *state1, *state2;       // [pool]: 12 and 24 bits of the key, and how many of those that begin so stay
+  int *above;                  // [head][part]: keys that begin with more
+  int *last;                   // [head][part][256]: a part's own tally of the last 8 bits
+  uint32_t *keys;
+  int *lists;
 };
 
-__device__ __forceinline__ uint32_t evict_key(const CacheView &C, const HeadPlace &p, int slot, const EvictPlan &E,
-                                              long long recent_from) {
-  const SlotPlace s = slot_place(C, p, slot);
-  if (!page_there(C, s.page)) return 0u;
-  const long long at = state_at(C, p, s);
-  const int pos = C.positions[at];
-  if (pos < E.sink || pos >= recent_from) return KEY_PROTECTED;
-  return score_key(C.mass[at]);
+__device__ __forceinline__ long long evict_budget(const EvictPlan &E, int b) {
+  const int asked = E.budgets != nullptr ? E.budgets[b] : E.budget;
+  return (long long)E.pool_heads * (asked > 0 ? asked : 0);
 }
 
-struct EvictLds {
-  int hist[EVICT_BINS];
-  int wave[3][EVICT_WAVES];
-  int bin, above;              // the bin that holds the last of the wanted, and how many lie in higher ones
-};
+// Keys of the 64 slots from first + 64 i on, i < N, one a lane; 0 where there is no token.  All table entries leave before the first is
+// waited for, and so do the states.
+template <int N>
+__device__ __forceinline__ void evict_keys(const CacheView &C, const HeadPlace &p, const EvictPlan &E, int first, int units, int count, long long recent_from,
+                                           uint32_t (&key)[N]) {
+  const int lane = threadIdx.x & 63;
+  int page[N], pos[N];
+  float mass[N];
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    page[i] = -1;
+    if (i < units) {                                       // uniform
+      const int slot = first + 64 * i + lane;
+      if (slot < count) page[i] = p.table[page_number((unsigned)slot, C.div_mul, C.div_shift)];
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    mass[i] = 0.f;
+    pos[i] = 0;
+    if (i < units && page_there(C, page[i])) {
+      const int slot = first + 64 * i + lane, at = slot - page_number((unsigned)slot, C.div_mul, C.div_shift) * C.page_size;
+      const long long x = page[i] * C.state_page_stride + p.state + at;
+      mass[i] = C.mass[x];
+      pos[i] = C.positions[x];
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const bool kept = pos[i] < E.sink || pos[i] >= recent_from;
+    key[i] = page_there(C, page[i]) ? (kept ? KEY_PROTECTED : score_key(mass[i])) : 0u;
+  }
+}
 
-// Sum over the workgroup, and over the waves before this one.
+__device__ __forceinline__ uint32_t wave_max(uint32_t x) {
+  for (int d = 32; d > 0; d >>= 1) {
+    const uint32_t o = __shfl_xor(x, d);
+    x = o > x ? o : x;
+  }
+  return x;
+}
+
+// Sum of the waves before this one, and of all.
+template <int WAVES>
 __device__ __forceinline__ int waves_before(const int *per_wave, int wave, int &total) {
   int before = 0;
   total = 0;
-  for (int i = 0; i < EVICT_WAVES; ++i) {
-    before += i < wave ? per_wave[i] : 0;
-    total += per_wave[i];
+#pragma unroll
+  for (int i = 0; i < WAVES; ++i) {
+    const int x = per_wave[i];
+    before += i < wave ? x : 0;
+    total += x;
   }
   return before;
 }
 
-__global__ __launch_bounds__(EVICT_THREADS) void evict_rank_kernel(const CacheView C, const EvictPlan E) {
-  __shared__ EvictLds L;
-  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
-  const int nh = E.pool_heads;
-  const unsigned g0 = blockIdx.x * (unsigned)nh;
-  const HeadOf w0 = head_of(C, g0);
-  const int asked = E.budgets != nullptr ? E.budgets[w0.b] : E.budget;
-  const long long want_all = (long long)nh * (asked > 0 ? asked : 0);
+// The bin of hist[BINS] in which the want-th largest lies, and how many lie in higher ones; by all THREADS.  per_wave and found: LDS.
+template <int BINS, int THREADS>
+__device__ __forceinline__ void find_bin(const int *hist, int want, int *per_wave, int *found) {
+  constexpr int EACH = BINS / THREADS;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  int mine[EACH], sum = 0;
+#pragma unroll
+  for (int i = 0; i < EACH; ++i) {
+    mine[i] = hist[BINS - 1 - (EACH * tid + i)];
+    sum += mine[i];
+  }
+  int upto = sum;
+  for (int d = 1; d < 64; d <<= 1) {
+    const int o = __shfl_up(upto, d);
+    if (lane >= d) upto += o;
+  }
+  if (lane == 63) per_wave[wave] = upto;
+  __syncthreads();
+  int all;
+  int before = waves_before<THREADS / 64>(per_wave, wave, all) + upto - sum;
+#pragma unroll
+  for (int i = 0; i < EACH; ++i) {
+    if (before < want && want <= before + mine[i]) {
+      found[0] = BINS - 1 - (EACH * tid + i);
+      found[1] = before;
+      found[2] = mine[i];
+    }
+    before += mine[i];
+  }
+  __syncthreads();
+}
+
+// Moves one row, its state with it, by 16 lanes.
+__device__ __forceinline__ void move_row(const CacheView &C, const HeadPlace &p, int to, int from, int lane) {
+  const SlotPlace z = slot_place(C, p, to), a = slot_place(C, p, from);
+  if (!page_there(C, z.page) || !page_there(C, a.page)) return;
+  const long long src = row_at(C, p, a) + 8 * lane, dst = row_at(C, p, z) + 8 * lane;
+  const uint4 k = *reinterpret_cast<const uint4 *>(C.k + src);
+  const uint4 v = *reinterpret_cast<const uint4 *>(C.v + src);
+  *reinterpret_cast<uint4 *>(C.k + dst) = k;
+  *reinterpret_cast<uint4 *>(C.v + dst) = v;
+  if (lane == 0) {
+    const long long x = state_at(C, p, a), y = state_at(C, p, z);
+    C.mass[y] = C.mass[x];
+    C.positions[y] = C.positions[x];
+  }
+}
+
+// ---- one workgroup a head
+constexpr int ALONE_THREADS = 1024, ALONE_WAVES = ALONE_THREADS / 64, ALONE_UNITS = 16;
+constexpr int ALONE_SLOTS = ALONE_WAVES * ALONE_UNITS * 64;
+constexpr int ALONE_BINS = 4096, ALONE_CANDS = 256;
+
+struct AloneLds {
+  int hist[ALONE_BINS];
+  int late[ALONE_SLOTS / 2 + 1], holes[ALONE_SLOTS / 2 + 1];
+  uint32_t cand[ALONE_CANDS];
+  int wave[4][ALONE_WAVES];
+  uint32_t top[2][ALONE_WAVES];
+  int found[3], cands, moves;
+  uint32_t key;
+  int ties;
+};
+
+// Key of the last token that stays: its bin among 4096 of equal width between the least and the largest key that are neither
+// protected nor 0, so that bins are even whatever the weights' range; then among the few keys of the bin, or 4096 bins within it.
+__global__ __launch_bounds__(ALONE_THREADS) void evict_alone_kernel(const CacheView C, const EvictPlan E) {
+  __shared__ AloneLds L;
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
+  const HeadOf w = head_of(C, blockIdx.x);
+  const HeadPlace p = head_place(C, w);
+  const int c = held(C, w.b, w.l, w.h);
+  const long long budget = evict_budget(E, w.b);
+  if (c <= budget || c > E.most) return;                   // uniform
+  const int left = (int)budget;
+  const long long recent_from = (long long)C.seen[count_at(C, w.b, w.l, w.h)] - E.recent;
+  const int units = ((c + 63) / 64 + ALONE_WAVES - 1) / ALONE_WAVES, first = wave * units * 64;       // of every wave
+  uint32_t key[ALONE_UNITS];
+  evict_keys(C, p, E, first, units, c, recent_from, key);
+
+  int kept = 0, plain = 0;
+  uint32_t most = 0, least = 0;                            // least: as ~key
+#pragma unroll
+  for (int i = 0; i < ALONE_UNITS; ++i)
+    if (i < units) {
+      const bool is_plain = key[i] != 0u && key[i] != KEY_PROTECTED;
+      kept += __popcll(__ballot(key[i] == KEY_PROTECTED));
+      plain += __popcll(__ballot(is_plain));
+      if (is_plain) {
+        most = key[i] > most ? key[i] : most;
+        least = ~key[i] > least ? ~key[i] : least;
+      }
+    }
+  most = wave_max(most);
+  least = wave_max(least);
+  if (lane == 0) {
+    L.wave[0][wave] = kept;
+    L.wave[1][wave] = plain;
+    L.top[0][wave] = most;
+    L.top[1][wave] = least;
+  }
+  if (tid == 0) L.moves = 0;
+  __syncthreads();
+  waves_before<ALONE_WAVES>(L.wave[0], wave, kept);
+  waves_before<ALONE_WAVES>(L.wave[1], wave, plain);
+#pragma unroll
+  for (int i = 0; i < ALONE_WAVES; ++i) {
+    most = L.top[0][i] > most ? L.top[0][i] : most;
+    least = L.top[1][i] > least ? L.top[1][i] : least;
+  }
+  uint32_t last;                                           // the key of the last one that stays
+  int ties;                                                // and how many of its equals stay
+  if (left <= kept) {
+    last = KEY_PROTECTED;
+    ties = left;
+  } else if (left - kept > plain) {
+    last = 0u;
+    ties = left - kept - plain;
+  } else {
+    uint32_t lo = ~least, hi = most;
+    int want = left - kept;
+    for (;;) {
+      const int shift = hi - lo < (uint32_t)ALONE_BINS ? 0 : 32 - __builtin_clz((hi - lo) / ALONE_BINS);
+      for (int i = tid; i < ALONE_BINS; i += ALONE_THREADS) L.hist[i] = 0;
+      if (tid == 0) L.cands = 0;
+      __syncthreads();
+#pragma unroll
+      for (int i = 0; i < ALONE_UNITS; ++i)
+        if (i < units && key[i] >= lo && key[i] <= hi) atomicAdd(&L.hist[(key[i] - lo) >> shift], 1);
+      __syncthreads();
+      find_bin<ALONE_BINS, ALONE_THREADS>(L.hist, want, L.wave[2], L.found);
+      const int bin = L.found[0], in_bin = L.found[2];
+      want -= L.found[1];
+      lo += (uint32_t)bin << shift;
+      const uint32_t end = lo + ((1u << shift) - 1u);
+      hi = end < hi ? end : hi;
+      if (shift == 0) {
+        last = lo;
+        ties = want;
+        break;
+      }
+      if (in_bin <= ALONE_CANDS) {
+#pragma unroll
+        for (int i = 0; i < ALONE_UNITS; ++i)
+          if (i < units && key[i] >= lo && key[i] <= hi) L.cand[atomicAdd(&L.cands, 1)] = key[i];
+        __syncthreads();
+        if (tid < in_bin) {
+          const uint32_t mine = L.cand[tid];
+          int more = 0, same = 0;
+          for (int i = 0; i < in_bin; ++i) {
+            const uint32_t o = L.cand[i];
+            more += o > mine;
+            same += o == mine;
+          }
+          if (more < want && want <= more + same) {        // equal candidates write the same
+            L.key = mine;
+            L.ties = want - more;
+          }
+        }
+        __syncthreads();
+        last = L.key;
+        ties = L.ties;
+        break;
+      }
+      __syncthreads();                                     // found has been read
+    }
+  }
+
+  int eq = 0, gt = 0;
+#pragma unroll
+  for (int i = 0; i < ALONE_UNITS; ++i)
+    if (i < units) {
+      const bool in = first + 64 * i + lane < c;
+      eq += __popcll(__ballot(in && key[i] == last));
+      gt += __popcll(__ballot(in && key[i] > last));
+    }
+  if (lane == 0) {
+    L.wave[0][wave] = eq;
+    L.wave[1][wave] = gt;
+  }
+  __syncthreads();
+  int all, eq_before = waves_before<ALONE_WAVES>(L.wave[0], wave, all);
+  int before = waves_before<ALONE_WAVES>(L.wave[1], wave, all) + min(eq_before, ties);
+#pragma unroll
+  for (int i = 0; i < ALONE_UNITS; ++i)
+    if (i < units) {
+      const int slot = first + 64 * i + lane;
+      const unsigned long long below = (1ull << lane) - 1, eqs = __ballot(slot < c && key[i] == last);
+      const bool stays = slot < c && (key[i] > last || (key[i] == last && eq_before + __popcll(eqs & below) < ties));
+      const unsigned long long ones = __ballot(stays);
+      const int in_front = before + __popcll(ones & below);
+      if (slot < left && !stays) L.holes[slot - in_front] = slot;
+      if (slot >= left && stays) L.late[left - 1 - in_front] = slot;
+      const int late = __popcll(__ballot(slot >= left && stays));
+      if (lane == 0 && late > 0) atomicAdd(&L.moves, late);
+      eq_before += __popcll(eqs);
+      before += __popcll(ones);
+    }
+  __syncthreads();
+  const int moves = L.moves;
+  if (tid == 0) C.counts[count_at(C, w.b, w.l, w.h)] = left;
+  for (int i = tid >> 4; i < moves; i += ALONE_THREADS / 16) move_row(C, p, L.holes[i], L.late[moves - 1 - i], tid & 15);
+}
+
+// ---- a workgroup a part
+constexpr int PART_THREADS = 256, PART_WAVES = PART_THREADS / 64, PART_UNITS = 16;
+constexpr int PART_SLOTS = PART_WAVES * PART_UNITS * 64;
+
+__global__ __launch_bounds__(256) void evict_clear_kernel(int *zero, long long ints) {
+  for (long long i = blockIdx.x * 256ll + threadIdx.x; i < ints; i += gridDim.x * 256ll) zero[i] = 0;
+}
+
+struct EvictPart {
+  unsigned g, g0;              // head, and first head of its pool
+  int pool, part, count, first;        // tokens of the head, first slot of the part
+  HeadOf w;
+  long long want;
+};
+// -> false: nothing to do for this workgroup.  A head's first part is there even if it holds nothing, for its count.
+__device__ __forceinline__ bool evict_part(const CacheView &C, const EvictPlan &E, EvictPart &P) {
+  P.g = blockIdx.x / (unsigned)E.parts;
+  P.part = (int)(blockIdx.x - P.g * (unsigned)E.parts);
+  P.pool = (int)(P.g / (unsigned)E.pool_heads);
+  P.g0 = (unsigned)P.pool * (unsigned)E.pool_heads;
+  P.w = head_of(C, P.g);
+  P.count = held(C, P.w.b, P.w.l, P.w.h);
+  P.first = P.part * PART_SLOTS;
+  P.want = evict_budget(E, P.w.b);
+  if (P.part > 0 && P.first >= P.count) return false;
+  if (E.pool_heads == 1) return P.count > P.want && P.count <= E.most;
   long long total = 0;
   bool too_long = false;
-  for (int j = 0; j < nh; ++j) {
-    const int c = held(C, w0.b, w0.l, w0.h + j);
+  for (int h = threadIdx.x & 63; h < E.pool_heads; h += 64) {
+    const int c = held(C, P.w.b, P.w.l, h);
     total += c;
     too_long |= c > E.most;
   }
-  if (total <= want_all || too_long) {                     // uniform
-    for (int j = tid; j < nh; j += EVICT_THREADS) E.moves[g0 + j] = 0;
+  for (int d = 32; d > 0; d >>= 1) total += __shfl_xor(total, d);
+  return total > P.want && !__any(too_long);
+}
+
+// Adds a part's tally to its pool's.
+__device__ __forceinline__ void add_hist(const int *mine, int *pool) {
+  for (int i = threadIdx.x; i < 4096; i += PART_THREADS)
+    if (mine[i] != 0) atomicAdd(&pool[i], mine[i]);
+}
+
+// The part's keys, as every launch but the first finds them; 0 behind the end.
+__device__ __forceinline__ void part_keys(const EvictPlan &E, const EvictPart &P, int first, uint32_t (&key)[PART_UNITS]) {
+  const uint32_t *k = E.keys + (long long)P.g * E.pitch + first + (threadIdx.x & 63);
+#pragma unroll
+  for (int i = 0; i < PART_UNITS; ++i) key[i] = k[64 * i];         // (the pitch is whole parts)
+}
+
+__global__ __launch_bounds__(PART_THREADS) void evict_keys_kernel(const CacheView C, const EvictPlan E) {
+  __shared__ int hist[4096];
+  EvictPart P;
+  if (!evict_part(C, E, P)) {
+    if (threadIdx.x == 0 && blockIdx.x % (unsigned)E.parts == 0) E.left[P.g] = -1;
     return;
   }
-  // the key of the last one that stays, and how many of its equals stay
-  uint32_t prefix = 0, mask = 0;
-  int want = (int)want_all;                                // < total < 2^31
-  if (want > 0) {
-    for (int pass = 0; pass < 3; ++pass) {
-      const int shift = pass == 0 ? 20 : pass == 1 ? 8 : 0, bins = pass == 2 ? 256 : EVICT_BINS;
-      for (int i = tid; i < EVICT_BINS; i += EVICT_THREADS) L.hist[i] = 0;
-      __syncthreads();
-      for (int j = 0; j < nh; ++j) {
-        const HeadOf w{w0.b, w0.l, w0.h + j};
-        const HeadPlace p = head_place(C, w);
-        const int c = held(C, w.b, w.l, w.h);
-        const long long from = (long long)C.seen[count_at(C, w.b, w.l, w.h)] - E.recent;
-        for (int s = tid; s < c; s += EVICT_THREADS) {
-          const uint32_t key = evict_key(C, p, s, E, from);
-          if ((key & mask) == prefix) atomicAdd(&L.hist[key >> shift & (uint32_t)(bins - 1)], 1);
-        }
-      }
-      __syncthreads();
-      // bins from the top: thread t has bins top - 4 t .. top - 4 t - 3
-      int mine[4], sum = 0;
+  for (int i = threadIdx.x; i < 4096; i += PART_THREADS) hist[i] = 0;
+  const int first = P.first + (int)(threadIdx.x >> 6) * PART_UNITS * 64, lane = threadIdx.x & 63;
+  uint32_t key[PART_UNITS];
+  evict_keys(C, head_place(C, P.w), E, first, PART_UNITS, P.count, (long long)C.seen[count_at(C, P.w.b, P.w.l, P.w.h)] - E.recent, key);
+  __syncthreads();
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        mine[i] = L.hist[EVICT_BINS - 1 - (4 * tid + i)];
-        sum += mine[i];
-      }
-      int upto = sum;
-      for (int d = 1; d < 64; d <<= 1) {
-        const int o = __shfl_up(upto, d);
-        if (lane >= d) upto += o;
-      }
-      if (lane == 63) L.wave[0][wave] = upto;
-      __syncthreads();
-      int all;
-      int before = waves_before(L.wave[0], wave, all) + upto - sum;
+  for (int i = 0; i < PART_UNITS; ++i) {
+    const int slot = first + 64 * i + lane;
+    E.keys[(long long)P.g * E.pitch + slot] = key[i];
+    if (slot < P.count) atomicAdd(&hist[key[i] >> 20], 1);
+  }
+  __syncthreads();
+  add_hist(hist, E.hist1 + (long long)P.pool * 4096);
+}
+
+__global__ __launch_bounds__(PART_THREADS) void evict_next_kernel(const CacheView C, const EvictPlan E) {
+  __shared__ int hist[4096], per_wave[PART_WAVES], found[3];
+  EvictPart P;
+  if (!evict_part(C, E, P) || P.want == 0) return;
+  find_bin<4096, PART_THREADS>(E.hist1 + (long long)P.pool * 4096, (int)P.want, per_wave, found);
+  const int bin = found[0];
+  if (threadIdx.x == 0 && P.g == P.g0 && P.part == 0) E.state1[P.pool] = make_int2(bin, (int)P.want - found[1]);
+  for (int i = threadIdx.x; i < 4096; i += PART_THREADS) hist[i] = 0;
+  const int first = P.first + (int)(threadIdx.x >> 6) * PART_UNITS * 64, lane = threadIdx.x & 63;
+  uint32_t key[PART_UNITS];
+  part_keys(E, P, first, key);
+  __syncthreads();
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        if (before < want && want <= before + mine[i]) {
-          L.bin = EVICT_BINS - 1 - (4 * tid + i);
-          L.above = before;
-        }
-        before += mine[i];
-      }
-      __syncthreads();
-      want -= L.above;
-      prefix |= (uint32_t)L.bin << shift;
-      mask |= (uint32_t)(bins - 1) << shift;
-      __syncthreads();
-    }
+  for (int i = 0; i < PART_UNITS; ++i)
+    if (first + 64 * i + lane < P.count && (int)(key[i] >> 20) == bin) atomicAdd(&hist[key[i] >> 8 & 4095], 1);
+  __syncthreads();
+  add_hist(hist, E.hist2 + (long long)P.pool * 4096);
+}
+
+__global__ __launch_bounds__(PART_THREADS) void evict_last_kernel(const CacheView C, const EvictPlan E) {
+  __shared__ int hist[256], per_wave[PART_WAVES], found[3];
+  EvictPart P;
+  if (!evict_part(C, E, P) || P.want == 0) return;
+  const int2 one = E.state1[P.pool];
+  find_bin<4096, PART_THREADS>(E.hist2 + (long long)P.pool * 4096, one.y, per_wave, found);
+  const int begins = one.x << 12 | found[0];
+  if (threadIdx.x == 0 && P.g == P.g0 && P.part == 0) E.state2[P.pool] = make_int2(begins, one.y - found[1]);
+  hist[threadIdx.x] = 0;
+  const int first = P.first + (int)(threadIdx.x >> 6) * PART_UNITS * 64, lane = threadIdx.x & 63;
+  uint32_t key[PART_UNITS];
+  part_keys(E, P, first, key);
+  __syncthreads();
+  int above = 0;
+#pragma unroll
+  for (int i = 0; i < PART_UNITS; ++i) {
+    const bool in = first + 64 * i + lane < P.count;
+    const int b = (int)(key[i] >> 8);
+    above += __popcll(__ballot(in && b > begins));
+    if (in && b == begins) atomicAdd(&hist[key[i] & 255u], 1);
   }
-  const bool none = want_all == 0;
-  // head after head: a wave has a run of consecutive slots
-  int ties = none ? 0 : want;                              // equals of `prefix` that stay, from here on
-  for (int j = 0; j < nh; ++j) {
-    const HeadOf w{w0.b, w0.l, w0.h + j};
-    const HeadPlace p = head_place(C, w);
-    const int c = held(C, w.b, w.l, w.h);
-    const long long from = (long long)C.seen[count_at(C, w.b, w.l, w.h)] - E.recent;
-    const int run = ((c + EVICT_WAVES - 1) / EVICT_WAVES + 63) / 64 * 64;
-    const int s0 = min(wave * run, c), s1 = min(s0 + run, c);
-    auto state_of = [&](int s) {                           // 0: goes, 1: equal, 2: stays
-      if (s >= s1 || none) return 0;
-      const uint32_t key = evict_key(C, p, s, E, from);
-      return key > prefix ? 2 : (key == prefix ? 1 : 0);
-    };
-    int eq = 0, gt = 0;
-    for (int s = s0; s < s1; s += 64) {
-      const int st = state_of(s + lane);
-      eq += __popcll(__ballot(st == 1));
-      gt += __popcll(__ballot(st == 2));
-    }
-    if (lane == 0) {
-      L.wave[0][wave] = eq;
-      L.wave[1][wave] = gt;
-    }
-    __syncthreads();
-    int eq_all, gt_all;
-    const int eq_before = waves_before(L.wave[0], wave, eq_all);
-    waves_before(L.wave[1], wave, gt_all);
-    const int eq_stay = min(ties, eq_all), left = gt_all + eq_stay;
-    __syncthreads();
-    // pass 0 counts a wave's holes and late tokens, pass 1 lists them
-    int hole_at = 0, late_at = 0;
-    for (int pass = 0; pass < 2; ++pass) {
-      int eq_seen = eq_before, holes = hole_at, late = late_at;
-      for (int s = s0; s < s1; s += 64) {
-        const int slot = s + lane, st = state_of(slot);
-        const unsigned long long below = (1ull << lane) - 1, eqs = __ballot(st == 1);
-        const bool stays = st == 2 || (st == 1 && eq_seen + __popcll(eqs & below) < eq_stay);
-        const bool is_hole = slot < s1 && !stays && slot < left, is_late = stays && slot >= left;
-        const unsigned long long hs = __ballot(is_hole), ls = __ballot(is_late);
-        if (pass == 1) {
-          int *list = E.lists + (long long)(g0 + j) * E.list;
-          if (is_hole) list[holes + __popcll(hs & below)] = slot;
-          if (is_late) list[E.list / 2 + late + __popcll(ls & below)] = slot;
-        }
-        eq_seen += __popcll(eqs);
-        holes += __popcll(hs);
-        late += __popcll(ls);
-      }
-      if (pass == 0) {
-        if (lane == 0) {
-          L.wave[0][wave] = holes;
-          L.wave[1][wave] = late;
-        }
-        __syncthreads();
-        int all;
-        late_at = waves_before(L.wave[1], wave, all);
-        hole_at = waves_before(L.wave[0], wave, all);
-        if (tid == 0) E.moves[g0 + j] = all;
-      }
-    }
-    if (tid == 0) C.counts[count_at(C, w.b, w.l, w.h)] = left;
-    ties -= eq_stay;
-    __syncthreads();
+  if (lane == 0) per_wave[threadIdx.x >> 6] = above;
+  __syncthreads();
+  const long long at = (long long)P.g * E.parts + P.part;
+  E.last[at * 256 + threadIdx.x] = hist[threadIdx.x];
+  if (hist[threadIdx.x] != 0) atomicAdd(&E.hist3[(long long)P.pool * 256 + threadIdx.x], hist[threadIdx.x]);
+  if (threadIdx.x == 0) E.above[at] = (per_wave[0] + per_wave[1]) + (per_wave[2] + per_wave[3]);
+}
+
+// Sum over the workgroup, to all.
+__device__ __forceinline__ int part_sum(int x, int *per_wave) {
+  for (int d = 32; d > 0; d >>= 1) x += __shfl_xor(x, d);
+  __syncthreads();
+  if ((threadIdx.x & 63) == 0) per_wave[threadIdx.x >> 6] = x;
+  __syncthreads();
+  return (per_wave[0] + per_wave[1]) + (per_wave[2] + per_wave[3]);
+}
+
+__global__ __launch_bounds__(PART_THREADS) void evict_list_kernel(const CacheView C, const EvictPlan E) {
+  __shared__ int per_wave[PART_WAVES], found[3], waves[2][PART_WAVES];
+  EvictPart P;
+  if (!evict_part(C, E, P)) return;
+  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
+  if (P.want == 0) {                                       // nothing stays, nothing moves
+    if (tid == 0 && P.part == 0) E.left[P.g] = 0;
+    return;
   }
+  const int2 two = E.state2[P.pool];
+  find_bin<256, PART_THREADS>(E.hist3 + (long long)P.pool * 256, two.y, per_wave, found);
+  const int digit = found[0], ties = two.y - found[1];
+  const uint32_t last = (uint32_t)two.x << 8 | (uint32_t)digit;
+  // equals in the heads before; equals and larger ones in the head, and in its parts before this one
+  int eq_heads = 0, eq_head = 0, eq_front = 0, gt_head = 0, gt_front = 0;
+  for (long long i = tid; i < (long long)(P.g - P.g0) * E.parts; i += PART_THREADS) {
+    const int h = (int)(i / E.parts), q = (int)(i - (long long)h * E.parts);
+    if (q == 0 || q * (long long)PART_SLOTS < held(C, P.w.b, P.w.l, h)) eq_heads += E.last[((long long)P.g0 * E.parts + i) * 256 + digit];
+  }
+  const int parts = max(1, (P.count + PART_SLOTS - 1) / PART_SLOTS);
+#pragma unroll 4
+  for (int q = 0; q < parts; ++q) {
+    const long long at = (long long)P.g * E.parts + q;
+    const int x = E.last[at * 256 + tid], a = E.above[at], e = tid == digit ? x : 0, m = (tid > digit ? x : 0) + (tid == 0 ? a : 0);
+    eq_head += e;
+    gt_head += m;
+    eq_front += q < P.part ? e : 0;
+    gt_front += q < P.part ? m : 0;
+  }
+  eq_heads = part_sum(eq_heads, per_wave);
+  eq_head = part_sum(eq_head, per_wave);
+  eq_front = part_sum(eq_front, per_wave);
+  gt_head = part_sum(gt_head, per_wave);
+  gt_front = part_sum(gt_front, per_wave);
+  const int mine = min(max(ties - eq_heads, 0), eq_head), left = gt_head + mine;      // equals that stay in the head, its new count
+  if (tid == 0 && P.part == 0) E.left[P.g] = left;
+
+  const int first = P.first + wave * PART_UNITS * 64;
+  uint32_t key[PART_UNITS];
+  part_keys(E, P, first, key);
+  int eq = 0, gt = 0;
+#pragma unroll
+  for (int i = 0; i < PART_UNITS; ++i) {
+    const bool in = first + 64 * i + lane < P.count;
+    eq += __popcll(__ballot(in && key[i] == last));
+    gt += __popcll(__ballot(in && key[i] > last));
+  }
+  if (lane == 0) {
+    waves[0][wave] = eq;
+    waves[1][wave] = gt;
+  }
+  __syncthreads();
+  int all, eq_before = eq_front + waves_before<PART_WAVES>(waves[0], wave, all);
+  int before = gt_front + waves_before<PART_WAVES>(waves[1], wave, all) + min(eq_before, mine);
+  int *list = E.lists + (long long)P.g * E.list;
+  int late_all = 0;
+#pragma unroll
+  for (int i = 0; i < PART_UNITS; ++i) {
+    const int slot = first + 64 * i + lane;
+    const unsigned long long below = (1ull << lane) - 1, eqs = __ballot(slot < P.count && key[i] == last);
+    const bool stays = slot < P.count && (key[i] > last || (key[i] == last && eq_before + __popcll(eqs & below) < mine));
+    const unsigned long long ones = __ballot(stays);
+    const int in_front = before + __popcll(ones & below);
+    if (slot < left && !stays) list[slot - in_front] = slot;
+    if (slot >= left && stays) list[E.list / 2 + left - 1 - in_front] = slot;
+    late_all += __popcll(__ballot(slot >= left && stays));
+    eq_before += __popcll(eqs);
+    before += __popcll(ones);
+  }
+  if (lane == 0 && late_all > 0) atomicAdd(&E.moves[P.g], late_all);
 }
 
 constexpr int MOVE_THREADS = 256;
 
 __global__ __launch_bounds__(MOVE_THREADS) void evict_move_kernel(const CacheView C, const EvictPlan E, int parts) {
   const unsigned g = blockIdx.x / (unsigned)parts;
-  const int part = (int)(blockIdx.x - g * (unsigned)parts), lane = threadIdx.x & 15;
+  const int part = (int)(blockIdx.x - g * (unsigned)parts);
+  const int left = E.left[g];
+  if (left < 0) return;
   const int moves = E.moves[g];
-  const HeadPlace p = head_place(C, head_of(C, g));
+  const HeadOf w = head_of(C, g);
+  if (part == 0 && threadIdx.x == 0) C.counts[count_at(C, w.b, w.l, w.h)] = left;
+  const HeadPlace p = head_place(C, w);
   const int *list = E.lists + (long long)g * E.list;
-  for (int i = part * (MOVE_THREADS / 16) + (int)(threadIdx.x >> 4); i < moves; i += parts * (MOVE_THREADS / 16)) {
-    const SlotPlace to = slot_place(C, p, list[i]), from = slot_place(C, p, list[E.list / 2 + i]);
-    if (!page_there(C, to.page) || !page_there(C, from.page)) continue;
-    const long long src = row_at(C, p, from) + 8 * lane, dst = row_at(C, p, to) + 8 * lane;
-    const uint4 k = *reinterpret_cast<const uint4 *>(C.k + src);
-    const uint4 v = *reinterpret_cast<const uint4 *>(C.v + src);
-    *reinterpret_cast<uint4 *>(C.k + dst) = k;
-    *reinterpret_cast<uint4 *>(C.v + dst) = v;
-    if (lane == 0) {
-      const long long a = state_at(C, p, from), z = state_at(C, p, to);
-      C.mass[z] = C.mass[a];
-      C.positions[z] = C.positions[a];
-    }
-  }
-}
-
-// Lists of a head: it moves at most half of its tokens (one into a slot that another left).
-static int evict_list_ints(int most) { return 2 * (most / 2 + 1); }
-
-static size_t evict_bytes(const CacheView &C, int most) {
-  const size_t heads = (size_t)C.nreq * C.layers * C.kv_heads;
-  return (heads * ((size_t)evict_list_ints(most) + 1) * sizeof(int) + 255) / 256 * 256;
+  for (int i = part * (MOVE_THREADS / 16) + (int)(threadIdx.x >> 4); i < moves; i += parts * (MOVE_THREADS / 16))
+    move_row(C, p, list[i], list[E.list / 2 + moves - 1 - i], threadIdx.x & 15);
 }
 
 static int evict_most(const CacheView &C, const compactor_cache_evict_params_t *e) {
@@ -429,6 +730,45 @@ static int evict_check(const compactor_cache_evict_params_t *e, const CacheView 
   if (e->scope != COMPACTOR_SCOPE_HEAD && e->scope != COMPACTOR_SCOPE_LAYER) return COMPACTOR_EINVAL;
   if (e->scope == COMPACTOR_SCOPE_LAYER && (long long)C.capacity * C.kv_heads > 0x7fffffffll - 64) return COMPACTOR_EINVAL;
   return COMPACTOR_OK;
+}
+
+static bool evict_alone(const CacheView &C, const compactor_cache_evict_params_t *e) {
+  return (e->scope == COMPACTOR_SCOPE_HEAD || C.kv_heads == 1) && evict_most(C, e) <= ALONE_SLOTS;
+}
+
+// Sizes and places of the parts' scratch in a workspace at `ws` (null: sizes only); returns its bytes.
+static size_t evict_scratch(const CacheView &C, const compactor_cache_evict_params_t *e, unsigned char *ws, EvictPlan *E) {
+  const size_t heads = (size_t)C.nreq * C.layers * C.kv_heads;
+  const size_t pools = e->scope == COMPACTOR_SCOPE_LAYER ? heads / C.kv_heads : heads;
+  E->most = evict_most(C, e);
+  E->parts = (int)(((long long)E->most + PART_SLOTS - 1) / PART_SLOTS);
+  const size_t pitch = (size_t)E->parts * PART_SLOTS;
+  E->list = 2 * (E->most / 2 + 1);               // a head moves at most half of its tokens (one into a slot that another left)
+  size_t at = 0;
+  auto take = [&](size_t ints) {
+    unsigned char *x = ws == nullptr ? nullptr : ws + at;
+    at += (ints * sizeof(int) + 255) / 256 * 256;
+    return x;
+  };
+  // the first four are cleared before they are used
+  E->hist1 = reinterpret_cast<int *>(take(pools * 4096));
+  E->hist2 = reinterpret_cast<int *>(take(pools * 4096));
+  E->hist3 = reinterpret_cast<int *>(take(pools * 256));
+  E->moves = reinterpret_cast<int *>(take(heads));
+  E->left = reinterpret_cast<int *>(take(heads));
+  E->state1 = reinterpret_cast<int2 *>(take(2 * pools));
+  E->state2 = reinterpret_cast<int2 *>(take(2 * pools));
+  E->above = reinterpret_cast<int *>(take(heads * E->parts));
+  E->last = reinterpret_cast<int *>(take(heads * E->parts * 256));
+  E->keys = reinterpret_cast<uint32_t *>(take(heads * pitch));
+  E->lists = reinterpret_cast<int *>(take(heads * E->list));
+  E->pitch = (int)pitch;
+  return at;
+}
+
+static size_t evict_bytes(const CacheView &C, const compactor_cache_evict_params_t *e) {
+  EvictPlan E;
+  return evict_alone(C, e) ? 0 : evict_scratch(C, e, nullptr, &E);
 }
 
 }  // namespace cmp
@@ -475,7 +815,7 @@ int compactor_cache_evict_workspace_size(const compactor_cache_t *cache, const c
   rc = evict_check(evict, C);
   if (rc) return rc;
   if (!bytes) return COMPACTOR_EINVAL;
-  *bytes = evict_bytes(C, evict_most(C, evict));
+  *bytes = evict_bytes(C, evict);
   return COMPACTOR_OK;
 }
 
@@ -492,21 +832,35 @@ int compactor_cache_evict(const compactor_cache_t *cache, const compactor_cache_
   E.budget = evict->budget; E.budgets = evict->budgets;
   E.sink = evict->sink; E.recent = evict->recent;
   E.pool_heads = evict->scope == COMPACTOR_SCOPE_LAYER ? C.kv_heads : 1;
-  E.most = evict_most(C, evict);
-  E.list = evict_list_ints(E.most);
-  if (!workspace || workspace_bytes < evict_bytes(C, E.most)) return COMPACTOR_EWORKSPACE;
-  if (reinterpret_cast<uintptr_t>(workspace) & 255u) return COMPACTOR_EALIGN;
   const long long heads = (long long)C.nreq * C.layers * C.kv_heads;
-  E.moves = static_cast<int *>(workspace);
-  E.lists = E.moves + heads;
-  long long parts = 2048 / heads;
-  parts = parts < 1 ? 1 : (parts > 128 ? 128 : parts);
-  if (heads * parts > 0x7fffffffll) return COMPACTOR_EINVAL;
   hipStream_t st = static_cast<hipStream_t>(stream);
+  if (evict_alone(C, evict)) {
+    E.most = evict_most(C, evict);
+    (void)hipGetLastError();
+    hipLaunchKernelGGL(evict_alone_kernel, dim3((unsigned)heads), dim3(ALONE_THREADS), 0, st, C, E);
+    return hipGetLastError() == hipSuccess ? COMPACTOR_OK : COMPACTOR_EHIP;
+  }
+  if (!workspace || workspace_bytes < evict_bytes(C, evict)) return COMPACTOR_EWORKSPACE;
+  if (reinterpret_cast<uintptr_t>(workspace) & 255u) return COMPACTOR_EALIGN;
+  evict_scratch(C, evict, static_cast<unsigned char *>(workspace), &E);
+  long long movers = 2048 / heads;
+  movers = movers < 1 ? 1 : (movers > 128 ? 128 : movers);
+  if (heads * E.parts > 0x7fffffffll) return COMPACTOR_EINVAL;
+  const dim3 grid((unsigned)(heads * E.parts)), block(PART_THREADS);
+  const long long clear = (reinterpret_cast<unsigned char *>(E.left) - reinterpret_cast<unsigned char *>(E.hist1)) / (long long)sizeof(int);
+  const unsigned clear_wgs = (unsigned)std::min((clear + 1023) / 1024, 1024ll);
   (void)hipGetLastError();
-  hipLaunchKernelGGL(evict_rank_kernel, dim3((unsigned)(heads / E.pool_heads)), dim3(EVICT_THREADS), 0, st, C, E);
+  hipLaunchKernelGGL(evict_clear_kernel, dim3(clear_wgs), dim3(256), 0, st, E.hist1, clear);
   if (hipGetLastError() != hipSuccess) return COMPACTOR_EHIP;
-  hipLaunchKernelGGL(evict_move_kernel, dim3((unsigned)(heads * parts)), dim3(MOVE_THREADS), 0, st, C, E, (int)parts);
+  hipLaunchKernelGGL(evict_keys_kernel, grid, block, 0, st, C, E);
+  if (hipGetLastError() != hipSuccess) return COMPACTOR_EHIP;
+  hipLaunchKernelGGL(evict_next_kernel, grid, block, 0, st, C, E);
+  if (hipGetLastError() != hipSuccess) return COMPACTOR_EHIP;
+  hipLaunchKernelGGL(evict_last_kernel, grid, block, 0, st, C, E);
+  if (hipGetLastError() != hipSuccess) return COMPACTOR_EHIP;
+  hipLaunchKernelGGL(evict_list_kernel, grid, block, 0, st, C, E);
+  if (hipGetLastError() != hipSuccess) return COMPACTOR_EHIP;
+  hipLaunchKernelGGL(evict_move_kernel, dim3((unsigned)(heads * movers)), dim3(MOVE_THREADS), 0, st, C, E, (int)movers);
   return hipGetLastError() == hipSuccess ? COMPACTOR_OK : COMPACTOR_EHIP;
 }
 

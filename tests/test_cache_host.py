@@ -126,23 +126,27 @@ def test_the_workspace_follows_max_tokens(B):
         assert B._lib.compactor_cache_attention_workspace_size(C.byref(_cache(B)), C.byref(q), C.byref(n)) == 0
         sizes.append(n.value)
     assert sizes == sorted(sizes) and sizes[2] == sizes[3] == sizes[4]
-    n = [C.c_size_t(0) for _ in range(3)]
-    for out, most in zip(n, (10, 100, 0)):
-        e = _evict(B, max_tokens=most)
-        assert B._lib.compactor_cache_evict_workspace_size(C.byref(_cache(B)), C.byref(e), C.byref(out)) == 0
-    assert 0 < n[0].value < n[1].value < n[2].value
+    # a head alone needs none up to 16384 tokens, a layer always does
+    for scope, tokens, some in ((0, (10, 16384), False), (0, (16385, 40000, 0), True), (1, (10, 9000, 0), True)):
+        n = [C.c_size_t(7) for _ in tokens]
+        for out, most in zip(n, tokens):
+            e = _evict(B, max_tokens=most, scope=scope)
+            cache = _cache(B, table_len=4000, table_stride=4000)
+            assert B._lib.compactor_cache_evict_workspace_size(C.byref(cache), C.byref(e), C.byref(out)) == 0
+        sizes = [x.value for x in n]
+        assert sizes == sorted(sizes) and (sizes[0] > 0 and len(set(sizes)) == len(sizes) if some else set(sizes) == {0})
 
 
 def test_bad_evictions(B):
     cache, n = _cache(B), C.c_size_t(0)
-    assert B._lib.compactor_cache_evict_workspace_size(C.byref(cache), C.byref(_evict(B)), C.byref(n)) == 0
+    assert B._lib.compactor_cache_evict_workspace_size(C.byref(cache), C.byref(_evict(B, scope=1)), C.byref(n)) == 0
     assert _evicts(B, cache, None) == B.EINVAL
     for kw in (dict(budget=-1), dict(sink=-1), dict(recent=-1), dict(scope=2), dict(max_tokens=-5)):
         assert _evicts(B, cache, _evict(B, **kw), wsb=n.value) == B.EINVAL, kw
     assert _evicts(B, cache, _evict(B, budgets=0x2), wsb=n.value) == B.EALIGN
-    assert _evicts(B, cache, _evict(B), ws=0, wsb=n.value) == B.EWORKSPACE
-    assert _evicts(B, cache, _evict(B), wsb=n.value - 1) == B.EWORKSPACE
-    assert _evicts(B, cache, _evict(B), ws=0x1000080, wsb=n.value) == B.EALIGN
+    assert _evicts(B, cache, _evict(B, scope=1), ws=0, wsb=n.value) == B.EWORKSPACE
+    assert _evicts(B, cache, _evict(B, scope=1), wsb=n.value - 1) == B.EWORKSPACE
+    assert _evicts(B, cache, _evict(B, scope=1), ws=0x1000080, wsb=n.value) == B.EALIGN
     wide = _cache(B, table_len=1 << 20, table_stride=1 << 20, kv_heads=256)
     assert _evicts(B, wide, _evict(B, scope=1), wsb=1 << 50) == B.EINVAL
 

@@ -417,6 +417,30 @@ def test_evict_all_weights_equal(C):
 
 
 @pytest.mark.parametrize("scope", [0, 1])
+@pytest.mark.parametrize("spread", [0.0, 1e-7, 1e-4])
+def test_evict_weights_that_crowd(C, scope, spread):
+    """Weights within a few steps of each other beside some that are far away: the threshold lies in the crowd."""
+    P = U.Paged(C, DEV, _counts(1, 2, 2, 5000, 700, 300, 9000), page=16)
+    P.fill_positions()
+    g = torch.Generator(device=DEV)
+    g.manual_seed(8)
+    P.mass.copy_(1.0 + spread * torch.rand(P.mass.shape, generator=g, device=DEV))
+    far = torch.rand(P.mass.shape, generator=g, device=DEV)
+    P.mass[far < 0.01] = 1e30
+    P.mass[far > 0.99] = -1e-30
+    for budget in (4000, 2500, 299, 20):
+        _check_evict(C, P, [budget], 2, 30, scope, what=str(budget))
+
+
+def test_evict_pools_of_many_heads(C):
+    counts = [[[(7 * h) % 40 for h in range(300)]]]
+    P = U.Paged(C, DEV, counts, page=8)
+    P.fill_positions()
+    _check_evict(C, P, [11], 1, 4, 1)
+    _check_evict(C, P, [11], 1, 4, 0)
+
+
+@pytest.mark.parametrize("scope", [0, 1])
 def test_evict_protects_more_than_the_budget(C, scope):
     P = U.Paged(C, DEV, _counts(1, 2, 3, 90, 70, 100), page=16)
     P.fill_positions()
@@ -442,14 +466,15 @@ def test_evict_more_tokens_than_promised(C):
 
 
 @pytest.mark.parametrize("counts,budget,scope", [([[[40000, 33000, 100]]], 30000, 0), ([[[70001]]], 12345, 0),
-                                                 ([[[32768, 32769, 5000]]], 20000, 1), ([[[16384, 16385], [16000, 20000]]], 16000, 0)])
+                                                 ([[[32768, 32769, 5000]]], 20000, 1), ([[[16384, 16385], [16000, 20000]]], 16000, 0),
+                                                 ([[[16384, 16000, 15, 9000]]], 8191, 0), ([[[4096, 4097, 8192, 0]], [[0, 0, 0, 12289]]], 3001, 1)])
 def test_evict_long_heads(C, counts, budget, scope):
     P = U.Paged(C, DEV, counts, page=64)
     P.seen.fill_(100000)
     P.positions.copy_(torch.randint(0, 100000, P.positions.shape, device=DEV, dtype=torch.int32))
     # weights on a coarse grid too: many ties at the threshold
     P.mass.copy_((torch.rand_like(P.mass) * 4000).floor() / 4000)
-    _check_evict(C, P, [budget], 4, 700, scope)
+    _check_evict(C, P, [budget] * P.B, 4, 700, scope)
 
 
 # ------------------------------------------------------------------------------------------ admission and together
