@@ -733,8 +733,17 @@ def compactor_cache_admit(params: Params, reqs: Sequence[Request], kept_idx: tor
                           stream=None):
     """State of the rows that compactor_compact_paged has written into the cache's pages: counts, seen,
     positions and, from the scores, mass."""
-    pp, arr, n = call = _marshal(params, reqs, on_gpu=False)
-    so, ko, _ = _layout(*call)
+    n = len(reqs)
+    _require(n >= 1, "at least one request is needed")
+    arr = (_Request * n)()                     # n and ratio are all that is looked at
+    for i, r in enumerate(reqs):
+        L, H, arr[i].n, _d = r.k_score.shape
+        if L != params.layers or H != params.kv_heads:
+            _refuse("k_score has shape %s, the parameters say [%d, %d, n, %d]"
+                    % (tuple(r.k_score.shape), params.layers, params.kv_heads, params.head_dim))
+        arr[i].ratio = r.ratio
+    pp = C.byref(params.c(False))
+    so, ko, _ = _layout(pp, arr, n)
     if (n, params.layers, params.kv_heads) != (cache.nreq, cache.layers, cache.kv_heads):
         _refuse("the cache is of [%d, %d, %d] requests, layers and heads, the call of [%d, %d, %d]"
                 % (cache.nreq, cache.layers, cache.kv_heads, n, params.layers, params.kv_heads))
@@ -800,7 +809,9 @@ def compactor_cache_attention(cache: Cache, q: torch.Tensor, new_tokens: Optiona
     query = _cache_query(cache, q, new_tokens, scale, softcap, accumulate, max_tokens)
     shape = q.shape
     if out is None:
-        out = torch.empty(shape, dtype=torch.bfloat16, device=cache.device)
+        out = torch.empty_like(q)      # (half of what torch.empty with a device takes)
+        if out.stride(4) != 1:
+            out = torch.empty(shape, dtype=torch.bfloat16, device=cache.device)
         if stream is not None:
             out.record_stream(stream)
     else:
@@ -815,7 +826,7 @@ def compactor_cache_attention(cache: Cache, q: torch.Tensor, new_tokens: Optiona
         if lse.device != cache.device:
             _refuse("lse must live on the GPU of the cache")
     elif want_lse:
-        lse = torch.empty(shape[:4], dtype=torch.float32, device=cache.device)
+        lse = q.new_empty(shape[:4], dtype=torch.float32)
         if stream is not None:
             lse.record_stream(stream)
     query.lse = _ptr(lse)

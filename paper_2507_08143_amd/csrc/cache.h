@@ -12,7 +12,8 @@ struct CacheView {
   const int32_t *tables;
   long long table_stride;
   int page_size, num_pages, capacity;        // capacity: slots that a table names
-  unsigned div_mul, div_shift;               // slot / page_size, see page_number()
+  unsigned div_mul, div_shift;               // slot / page_size, see invariant_quotient()
+  unsigned req_mul, req_shift, layer_mul, layer_shift;      // head / (layers * kv_heads), head / kv_heads
   int nreq, layers, kv_heads;
   int32_t *counts, *seen;
   long long count_stride_b, count_stride_l;
@@ -21,14 +22,14 @@ struct CacheView {
   long long state_page_stride, state_layer_stride, state_head_stride;
 };
 
-// slot / page_size for 0 <= slot < 2^31, by the multiplicative inverse of an invariant divisor (Granlund and
-// Montgomery 1994): with 2^(shift-1) < d <= 2^shift and mul = floor(2^32 (2^shift - d) / d) + 1 the quotient is
-// (mulhi(slot, mul) + slot) >> shift, and the sum stays below 2^32 because mulhi(slot, mul) <= slot.
-__host__ __device__ __forceinline__ int page_number(unsigned slot, unsigned mul, unsigned shift) {
-  const unsigned hi = (unsigned)(((unsigned long long)slot * mul) >> 32);
-  return (int)((hi + slot) >> shift);
+// x / d for 0 <= x < 2^31, by the multiplicative inverse of an invariant divisor (Granlund and Montgomery 1994): with
+// 2^(shift-1) < d <= 2^shift and mul = floor(2^32 (2^shift - d) / d) + 1 the quotient is (mulhi(x, mul) + x) >> shift, and the
+// sum stays below 2^32 because mulhi(x, mul) <= x.  (A division takes some 30 instructions before a first load.)
+__host__ __device__ __forceinline__ int invariant_quotient(unsigned x, unsigned mul, unsigned shift) {
+  const unsigned hi = (unsigned)(((unsigned long long)x * mul) >> 32);
+  return (int)((hi + x) >> shift);
 }
-inline void page_divisor(int d, unsigned *mul, unsigned *shift) {
+inline void invariant_divisor(int d, unsigned *mul, unsigned *shift) {
   unsigned s = 0;
   while ((1ull << s) < (unsigned long long)d) ++s;
   *shift = s;
@@ -38,26 +39,24 @@ inline void page_divisor(int d, unsigned *mul, unsigned *shift) {
 __device__ __forceinline__ long long count_at(const CacheView &C, int b, int l, int h) {
   return b * C.count_stride_b + l * C.count_stride_l + h;
 }
+__device__ __forceinline__ int clamp_to(int x, int most) { return x < 0 ? 0 : (x < most ? x : most); }
 __device__ __forceinline__ int held(const CacheView &C, int b, int l, int h) {
-  const int c = C.counts[count_at(C, b, l, h)];
-  return c < 0 ? 0 : (c < C.capacity ? c : C.capacity);
+  return clamp_to(C.counts[count_at(C, b, l, h)], C.capacity);
 }
 // New tokens of a request, of T rows.
 __device__ __forceinline__ int tokens_new(const int32_t *new_tokens, int b, int T) {
   if (new_tokens == nullptr) return T;
-  const int n = new_tokens[b];
-  return n < 0 ? 0 : (n < T ? n : T);
+  return clamp_to(new_tokens[b], T);
 }
 __device__ __forceinline__ bool page_there(const CacheView &C, int page) { return (unsigned)page < (unsigned)C.num_pages; }
 
 // Head (b, l, h) of launch-wide number g.
 struct HeadOf { int b, l, h; };
 __device__ __forceinline__ HeadOf head_of(const CacheView &C, unsigned g) {
-  const unsigned LH = (unsigned)C.layers * (unsigned)C.kv_heads;
   HeadOf w;
-  w.b = (int)(g / LH);
-  const unsigned r = g - (unsigned)w.b * LH;
-  w.l = (int)(r / (unsigned)C.kv_heads);
+  w.b = invariant_quotient(g, C.req_mul, C.req_shift);
+  const unsigned r = g - (unsigned)w.b * ((unsigned)C.layers * (unsigned)C.kv_heads);
+  w.l = invariant_quotient(r, C.layer_mul, C.layer_shift);
   w.h = (int)(r - (unsigned)w.l * (unsigned)C.kv_heads);
   return w;
 }
@@ -74,7 +73,7 @@ __device__ __forceinline__ HeadPlace head_place(const CacheView &C, const HeadOf
 // A slot's page (may not be there) and place in it.
 struct SlotPlace { int page, at; };
 __device__ __forceinline__ SlotPlace slot_place(const CacheView &C, const HeadPlace &p, int slot) {
-  const int i = page_number((unsigned)slot, C.div_mul, C.div_shift);
+  const int i = invariant_quotient((unsigned)slot, C.div_mul, C.div_shift);
   return SlotPlace{p.table[i], slot - i * C.page_size};
 }
 __device__ __forceinline__ long long row_at(const CacheView &C, const HeadPlace &p, const SlotPlace &s) {

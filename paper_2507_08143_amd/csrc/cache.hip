@@ -40,7 +40,9 @@ int cache_view(const compactor_cache_t *c, CacheNeed need, CacheView *view) {
   v.tables = c->tables; v.table_stride = c->table_stride;
   v.page_size = p.page_size; v.num_pages = p.num_pages;
   v.capacity = c->table_len * p.page_size;
-  page_divisor(p.page_size, &v.div_mul, &v.div_shift);
+  invariant_divisor(p.page_size, &v.div_mul, &v.div_shift);
+  invariant_divisor(c->layers * c->kv_heads, &v.req_mul, &v.req_shift);
+  invariant_divisor(c->kv_heads, &v.layer_mul, &v.layer_shift);
   v.nreq = c->nreq; v.layers = c->layers; v.kv_heads = c->kv_heads;
   v.counts = c->counts; v.seen = c->seen;
   v.count_stride_b = c->count_stride_b; v.count_stride_l = c->count_stride_l;
@@ -129,8 +131,33 @@ __global__ __launch_bounds__(256) void append_counts_kernel(const CacheView C, c
 
 // ------------------------------------------------------------------------------------------ admit
 // State of the rows of a compaction, in the order of kept_idx: a selection pool (one head, or the heads of a layer) is
-// pool_heads * k_keep entries, ADMIT_ROWS of them per workgroup.
+// pool_heads * k_keep entries, ADMIT_ROWS of them per workgroup.  Bound by the latency of the chain index, score (table entry): a
+// thread's four entries leave together.
 constexpr int ADMIT_ROWS = 1024;
+
+// Entries [lo, hi) of a head's list, at most ADMIT_ROWS of them.
+__device__ __forceinline__ void admit_rows(const CacheView &C, const HeadPlace &p, const int32_t *kept_idx, const float *scores, int n, int lo, int hi) {
+  constexpr int N = ADMIT_ROWS / 256;
+  int tok[N], page[N], at[N];
+  float mass[N];
+#pragma unroll
+  for (int u = 0; u < N; ++u) {
+    const int i = min(lo + 256 * u + (int)threadIdx.x, hi - 1);
+    tok[u] = kept_idx[i];
+    const SlotPlace s = slot_place(C, p, i);
+    page[u] = s.page;
+    at[u] = s.at;
+  }
+#pragma unroll
+  for (int u = 0; u < N; ++u) mass[u] = scores != nullptr && (unsigned)tok[u] < (unsigned)n ? scores[tok[u]] : 0.f;
+#pragma unroll
+  for (int u = 0; u < N; ++u)
+    if (lo + 256 * u + (int)threadIdx.x < hi && page_there(C, page[u])) {
+      const long long x = state_at(C, p, SlotPlace{page[u], at[u]});
+      C.positions[x] = tok[u];
+      C.mass[x] = mass[u];
+    }
+}
 
 __global__ __launch_bounds__(256) void admit_kernel(const SegTable T, const CacheView C, const int32_t *__restrict__ kept_idx,
                                                     const int32_t *__restrict__ kept_cnt, const float *__restrict__ scores) {
@@ -145,52 +172,47 @@ __global__ __launch_bounds__(256) void admit_kernel(const SegTable T, const Cach
     local -= nb;
   }
   const Seg &s = T.s[seg];
-  const int nh = pool_heads(T, s), pool = (int)(local / parts), part = (int)(local - (unsigned)pool * parts);
-  const int head0 = s.head_begin + pool * nh;              // l * H + h of the pool's first head
+  const int nh = pool_heads(T, s), pool = (int)(local / parts), part = (int)(local - (unsigned)pool * parts), lane = threadIdx.x & 63;
+  const int head0 = s.head_begin + pool * nh, layer = head0 / s.H;       // l * H + h of the pool's first head
   const long long entries = (long long)nh * s.k_keep, first = s.kept_off + (long long)head0 * s.k_keep;
-  const int32_t *cnt = kept_cnt + s.ghead0 + head0;
-  // what head j of the pool keeps, of the entries that are left
-  auto kept = [&](int j, long long left) {
-    if (!T.layer_scope) return (long long)s.k_keep;
-    const long long c = cnt[j];
-    return c < 0 ? 0 : (c < left ? c : left);
-  };
   const long long e0 = (long long)part * ADMIT_ROWS, e1 = e0 + ADMIT_ROWS < entries ? e0 + ADMIT_ROWS : entries;
-  long long base = 0;                                      // entries of the heads before
-  for (int j = 0; j < nh && base < e1; ++j) {
-    const long long c = kept(j, entries - base);
-    const int l = (head0 + j) / s.H, h = (head0 + j) - l * s.H;
-    const HeadOf w{s.req, l, h};
-    const HeadPlace p = head_place(C, w);
-    const long long room = c < C.capacity ? c : C.capacity;
-    const long long lo = e0 > base ? e0 - base : 0, hi = e1 - base < room ? e1 - base : room;
-    for (long long i = lo + threadIdx.x; i < hi; i += 256) {
-      const int tok = kept_idx[first + base + i];
-      const SlotPlace at = slot_place(C, p, (int)i);
-      if (!page_there(C, at.page)) continue;
-      const long long x = state_at(C, p, at);
-      C.positions[x] = tok;
-      C.mass[x] = scores != nullptr && tok >= 0 && tok < s.n ? scores[s.score_off + (long long)(head0 + j) * s.n + tok] : 0.f;
-    }
-    base += c;
+  auto head = [&](int j, long long base, long long kept) {             // the pool's j-th head has entries [base, base + kept); uniform
+    const HeadOf w{s.req, layer, head0 + j - layer * s.H};
+    const int room = (int)(kept < C.capacity ? kept : C.capacity);
+    const int lo = (int)(e0 > base ? e0 - base : 0), hi = (int)(e1 - base < room ? e1 - base : room);
+    if (lo < hi)
+      admit_rows(C, head_place(C, w), kept_idx + first + base,
+                 scores == nullptr ? nullptr : scores + s.score_off + (long long)(head0 + j) * s.n, s.n, lo, hi);
+  };
+  auto note = [&](int j, long long kept) {
+    const long long at = count_at(C, s.req, layer, head0 + j - layer * s.H);
+    C.counts[at] = (int)(kept < C.capacity ? kept : C.capacity);
+    C.seen[at] = s.n;
+  };
+  if (!T.layer_scope) {
+    head(0, 0, s.k_keep);
+    if (part == 0 && threadIdx.x == 0) note(0, s.k_keep);
+    return;
   }
-  if (part == 0) {
-    if (!T.layer_scope) {
-      if (threadIdx.x == 0) {
-        const int l = head0 / s.H;
-        const long long at = count_at(C, s.req, l, head0 - l * s.H);
-        C.counts[at] = s.k_keep < C.capacity ? s.k_keep : C.capacity;
-        C.seen[at] = s.n;
-      }
-    } else if (threadIdx.x == 0) {
-      long long left = entries;
-      for (int j = 0; j < nh; ++j) {
-        const long long c = kept(j, left), at = count_at(C, s.req, head0 / s.H, j);
-        left -= c;
-        C.counts[at] = (int)(c < C.capacity ? c : C.capacity);
-        C.seen[at] = s.n;
-      }
+  // 64 heads at a time: a lane has one, and where its entries begin (a count that does not fit the layer's entries is cut to them)
+  long long before = 0;
+  for (int j0 = 0; j0 < nh && (before < e1 || part == 0); j0 += 64) {
+    const int c = j0 + lane < nh ? kept_cnt[s.ghead0 + head0 + j0 + lane] : 0;
+    long long upto = c < 0 ? 0 : c;
+    for (int d = 1; d < 64; d <<= 1) {
+      const long long o = __shfl_up(upto, d);
+      if (lane >= d) upto += o;
     }
+    upto = before + upto < entries ? before + upto : entries;
+    long long base = __shfl_up(upto, 1);
+    if (lane == 0) base = before;
+    if (part == 0 && threadIdx.x < 64 && j0 + lane < nh) note(j0 + lane, upto - base);
+    for (unsigned long long mine = __ballot(base < e1 && upto > e0 && j0 + lane < nh); mine != 0; mine &= mine - 1) {
+      const int at = __builtin_ctzll(mine);
+      const long long b = __shfl(base, at);
+      head(j0 + at, b, __shfl(upto, at) - b);
+    }
+    before = __shfl(upto, 63);
   }
 }
 
@@ -226,8 +248,9 @@ struct EvictPlan {
   int pool_heads;              // 1 or kv_heads
   int most;                    // tokens of a head that the launches reach
   // parts
-  int parts;                   // of a head
-  int pitch, list;             // ints from one head's keys, and lists, to the next: `list / 2` destinations, then as many sources
+  int parts;                   // of a head, at most
+  long long pitch;             // ints from one head's keys to the next
+  int list;                    // and its lists: `list / 2` destinations, then as many sources
   int *hist1, *hist2, *hist3;  // [pool][4096], [pool][256]: tallies of the first, the next 12 and the last 8 bits
   int *moves;                  // [head]: how many
   int *left;                   // [head]: the new count, -1 where nothing changes
@@ -256,7 +279,7 @@ __device__ __forceinline__ void evict_keys(const CacheView &C, const HeadPlace &
     page[i] = -1;
     if (i < units) {                                       // uniform
       const int slot = first + 64 * i + lane;
-      if (slot < count) page[i] = p.table[page_number((unsigned)slot, C.div_mul, C.div_shift)];
+      if (slot < count) page[i] = p.table[invariant_quotient((unsigned)slot, C.div_mul, C.div_shift)];
     }
   }
 #pragma unroll
@@ -264,7 +287,7 @@ __device__ __forceinline__ void evict_keys(const CacheView &C, const HeadPlace &
     mass[i] = 0.f;
     pos[i] = 0;
     if (i < units && page_there(C, page[i])) {
-      const int slot = first + 64 * i + lane, at = slot - page_number((unsigned)slot, C.div_mul, C.div_shift) * C.page_size;
+      const int slot = first + 64 * i + lane, at = slot - invariant_quotient((unsigned)slot, C.div_mul, C.div_shift) * C.page_size;
       const long long x = page[i] * C.state_page_stride + p.state + at;
       mass[i] = C.mass[x];
       pos[i] = C.positions[x];
@@ -762,7 +785,7 @@ static size_t evict_scratch(const CacheView &C, const compactor_cache_evict_para
   E->last = reinterpret_cast<int *>(take(heads * E->parts * 256));
   E->keys = reinterpret_cast<uint32_t *>(take(heads * pitch));
   E->lists = reinterpret_cast<int *>(take(heads * E->list));
-  E->pitch = (int)pitch;
+  E->pitch = (long long)pitch;
   return at;
 }
 

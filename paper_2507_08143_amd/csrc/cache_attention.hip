@@ -18,6 +18,7 @@
 #include <math.h>
 
 #include <algorithm>
+#include <type_traits>
 
 #include "cache.h"
 
@@ -32,14 +33,18 @@ constexpr int ATT_WAVES = 4;
 constexpr int ATT_STEP = ATT_TILE * ATT_WAVES;
 constexpr int MOST_ROWS = 64;                // query rows of a head: G * T
 constexpr int ATT_LEAST_LOG = 2;             // fewest steps of a fragment, log 2
-constexpr int ATT_ROUNDS = 6;                // fragments for every workgroup that there is room for on the chip, at most
+constexpr int SCAN_HEADS = 512, SCAN_ROUNDS = 6;        // heads that a wave looks through, and fragments for every workgroup that
+                                             // there is room for on the chip
+constexpr int ATT_EVEN = 256, EVEN_PARTS = 4;          // units that have equal parts of heads of one length, and most parts of a head then
+constexpr int SPLIT_ALL = 4096, SPLIT_MOST = 8;        // more heads: parts of all of them, and of one, at most
 constexpr int ATT_ALONE = 8;                 // steps of a head up to which one workgroup takes all of it
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 
 // A part of a head that one workgroup does.
 struct Fragment {
-  int head;                    // -1: none
-  int from, to;                // slots
+  int head;                    // -1: there is none
+  int count, n;                // tokens that it holds, and queries
+  int step0, step1;            // steps of the part
   int first, parts;            // the head's first fragment, and how many it has
 };
 
@@ -52,11 +57,13 @@ struct Queries {
   const int32_t *new_tokens;
   int tokens, group;           // T, and G query heads a kv head; row t * G + g of a head
   float scale, softcap;
-  int frags_most, target;      // fragments that there is room for, and how many there are to be if no head were shorter; 0: one a head
-  Fragment *frags;             // [frags_most]
+  int target;                  // > 0: whole fragments that there are to be (scan_part)
+  int split;                   // else: workgroups a head (split_part)
+  bool fragments;              // false: every workgroup has a whole head
+  Fragment *frags;
   int2 *head_frags;            // [head]: its first fragment, and how many
-  float *partial;              // [frags_most][row][D], relative to 2^m
-  float2 *stats;               // [frags_most][row]: m (base 2) and the sum of 2^(x - m)
+  float *partial;              // [fragment][row][D], relative to 2^m
+  float2 *stats;               // [fragment][row]: m (base 2) and the sum of 2^(x - m)
   float *logits;               // accumulate: [head][row][pitch], base 2; else null
   int most, pitch;             // slots that there is room for
 };
@@ -119,7 +126,7 @@ __device__ __forceinline__ void places_run(const CacheView &C, const HeadPlace &
   // PAGE16: halves of the tiles from `first` on
   const long long slot = (long long)first + 16 * lane;
   bool ok = slot < count;
-  const int i = page_number(ok ? (unsigned)slot : 0u, C.div_mul, C.div_shift);
+  const int i = invariant_quotient(ok ? (unsigned)slot : 0u, C.div_mul, C.div_shift);
   const int page = ok ? p.table[i] : 0;
   ok = ok && page_there(C, page);
   P.off = ok ? page * C.page_stride + ((int)slot - i * C.page_size) * C.slot_stride : 0;
@@ -129,7 +136,7 @@ template <bool PAGE16>
 __device__ __forceinline__ void places_fetch(const CacheView &C, const HeadPlace &p, long long first, int count, int lane, Places<PAGE16> &P) {
   const long long slot = first + (lane & 31);
   P.in = slot < count;
-  const int i = page_number(P.in ? (unsigned)slot : 0u, C.div_mul, C.div_shift);
+  const int i = invariant_quotient(P.in ? (unsigned)slot : 0u, C.div_mul, C.div_shift);
   P.page = P.in ? p.table[i] : 0;
   P.at = (int)slot - i * C.page_size;
 }
@@ -183,32 +190,45 @@ __device__ __forceinline__ void finish_row(const CacheView &C, const Queries &Q,
         sum == 0.f ? -INFINITY : LN2 * (m + __builtin_amdgcn_logf(sum));
 }
 
-// Adds the weights of slots [from, to), from a multiple of 4, to the head's mass: 1/G sum over rows of 2^(x - lse2), lse2 = inf for a
-// row without weights.
-__device__ __forceinline__ void add_mass(const CacheView &C, const Queries &Q, const HeadPlace &hp, const float *lse2, const float *logits,
-                                         int R, int from, int to) {
-  const float inv = 1.f / (float)Q.group;
-  for (int s = from + 4 * (int)threadIdx.x; s < to; s += 4 * 256) {
-    SlotPlace at[4];
-    float *mass[4], old[4];
+// Weights of the head's slots s .. s + 3, s a multiple of 4, on the way to their mass: what does not depend on the rows' sums leaves
+// early (the mass, and the logits of the first MASS_ROWS rows).
+constexpr int MASS_ROWS = 4;
+struct MassQuad {
+  float *mass[4], old[4];
+  bool there[4];
+  f32x4 x[MASS_ROWS];
+};
+__device__ __forceinline__ void mass_fetch(const CacheView &C, const Queries &Q, const HeadPlace &hp, const float *logits, int R, int s, int to, MassQuad &M) {
+  SlotPlace at[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      at[i] = slot_place(C, hp, min(s + i, to - 1));
-      mass[i] = C.mass + state_at(C, hp, SlotPlace{page_there(C, at[i].page) ? at[i].page : 0, at[i].at});
-      old[i] = *mass[i];
-    }
-    f32x4 x = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll 4
-    for (int r = 0; r < R; ++r) {
-      const f32x4 y = *reinterpret_cast<const f32x4 *>(logits + (long long)r * Q.pitch + s);
-      const float z = lse2[r];
+  for (int i = 0; i < 4; ++i) at[i] = slot_place(C, hp, min(s + i, to - 1));
 #pragma unroll
-      for (int i = 0; i < 4; ++i) x[i] += z == INFINITY ? 0.f : exp2_(y[i] - z);
-    }
+  for (int r = 0; r < MASS_ROWS; ++r) M.x[r] = *reinterpret_cast<const f32x4 *>(logits + (long long)min(r, R - 1) * Q.pitch + s);
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-      if (s + i < to && page_there(C, at[i].page)) *mass[i] = fmaf(x[i], inv, old[i]);
+  for (int i = 0; i < 4; ++i) {
+    const bool there = page_there(C, at[i].page);
+    M.there[i] = s + i < to && there;
+    M.mass[i] = C.mass + state_at(C, hp, SlotPlace{there ? at[i].page : 0, at[i].at});
+    M.old[i] = *M.mass[i];
   }
+}
+// 1/G sum over rows of 2^(x - lse2), lse2 = inf for a row without weights.
+__device__ __forceinline__ void mass_add(const Queries &Q, const float *lse2, const float *logits, int R, int s, const MassQuad &M) {
+  const float inv = 1.f / (float)Q.group;
+  f32x4 sum = f32x4{0.f, 0.f, 0.f, 0.f};
+  auto row = [&](int r, const f32x4 &x) {
+    const float z = lse2[r];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) sum[i] += z == INFINITY ? 0.f : exp2_(x[i] - z);
+  };
+#pragma unroll
+  for (int r = 0; r < MASS_ROWS; ++r)
+    if (r < R) row(r, M.x[r]);
+#pragma unroll 4
+  for (int r = MASS_ROWS; r < R; ++r) row(r, *reinterpret_cast<const f32x4 *>(logits + (long long)r * Q.pitch + s));
+#pragma unroll
+  for (int i = 0; i < 4; ++i)
+    if (M.there[i]) *M.mass[i] = fmaf(sum[i], inv, M.old[i]);
 }
 
 constexpr int KEPT_FLOATS = ATT_TILE * MOST_ROWS;      // logits that a wave keeps in LDS: a tile at least
@@ -222,9 +242,10 @@ struct AttendLds {
 
 // Steps of ATT_STEP slots of a head: one at least, so that every head has a workgroup that writes its rows.
 __device__ __forceinline__ int steps_of(int count, int n) { return n > 0 && count > ATT_STEP ? (int)(((unsigned)count + ATT_STEP - 1) / ATT_STEP) : 1; }
-__device__ __forceinline__ int head_steps(const CacheView &C, const Queries &Q, unsigned g) {
+struct HeadSize { int count, n; };           // tokens held, and queries
+__device__ __forceinline__ HeadSize head_size(const CacheView &C, const Queries &Q, unsigned g) {
   const HeadOf w = head_of(C, g);
-  return steps_of(held(C, w.b, w.l, w.h), tokens_new(Q.new_tokens, w.b, Q.tokens));
+  return HeadSize{held(C, w.b, w.l, w.h), tokens_new(Q.new_tokens, w.b, Q.tokens)};
 }
 
 // Sum over the lanes up to this one (row shifts, then the sums of rows and of halves of the wave handed on).
@@ -238,42 +259,107 @@ __device__ __forceinline__ int wave_scan(int x) {
   return x;
 }
 
-// How long a head is only the device knows, so every workgroup finds its part by itself: heads are cut into fragments of the same
-// number of steps, a power of two so that all heads together have at most `target` of them beside the last of each head,
-// and fragments are numbered head after head.  Every wave does it alone, 64 heads at a time, without a barrier.
-// (Cutting every head into the same number of parts leaves the longest ones' parts as the last to end: 16 requests of 68 to
-// 55778 slots a head 217 us against 200.  A run of steps for every unit, across heads, is no better than parts of one size: units are not
-// equally fast.)  -> false: there is no such fragment.
-struct Part { int head, steps, step0, step1, first, parts; };
-__device__ __forceinline__ bool find_part(const CacheView &C, const Queries &Q, int fragment, Part &P) {
+// The largest of the lanes' numbers >= 0, in lane 63.
+__device__ __forceinline__ int wave_max_up(int x) {
+  x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false));
+  x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false));
+  x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false));
+  x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false));
+  x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false));
+  x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false));
+  return x;
+}
+
+// How long a head is only the device knows, so up to SCAN_HEADS heads every wave finds its workgroup's part by itself, without a
+// barrier: heads are cut into fragments of the same power of two of steps, numbered head after head, at most `target` of them beside
+// the last of each head.  A few rounds of workgroups keep the chip busy to the end whatever the lengths (16 requests of 68
+// to 55778 slots a head, us with fragments of any size in 1 / 2 / 3 / 4 / 6 rounds 212 / 202 / 201 / 202 / 203; 48 of 8192 to 32000 833 / 694 / 657 /
+// 652 / 643; 32 of 500 to 16000 131 / 119 / 116 / 116 / 120; cutting every head into the same number of parts 217 / 645 / -).  Heads of (nearly)
+// one length need no rounds where whole rounds of units have equal parts (256 heads of 4000: 84 against 89, 512 183 against 213).
+//
+// What a workgroup does before its first load of rows counts: under load, 26 us of the first case's 202 for 650 instructions
+// more.  A launch that plans the fragments for all costs 9 us and saves less (the cases above 210 / 666 / 123).  From SCAN_HEADS
+// heads on each is cut into the same few parts (split_part): 1024 heads of 4000, us with a scan / a plan / parts 407 / 384 / 360, of 250 to 8000
+// 249 / 237 / 232, 4096 of 2000 1045 / 786 / 692.  -> false: there is no such fragment.
+constexpr int SCAN_GROUP = 4;                // of 64 heads whose sizes are fetched together; the first stays
+__device__ __forceinline__ bool scan_part(const CacheView &C, const Queries &Q, int fragment, Fragment &F) {
   const int heads = C.nreq * C.layers * C.kv_heads, lane = threadIdx.x & 63;
-  int mine = 0, kept = 0;                           // kept: steps of head `lane`
-  for (int h = lane; h < heads; h += 64) {
-    const int x = head_steps(C, Q, (unsigned)h);
-    if (h < 64) kept = x;
-    mine += x;
+  HeadSize size[SCAN_GROUP];
+  auto fetch = [&](int h0) {
+#pragma unroll
+    for (int i = 0; i < SCAN_GROUP; ++i)
+      if (i == 0 || h0 + 64 * i < heads) size[i] = head_size(C, Q, (unsigned)min(h0 + 64 * i + lane, heads - 1));
+  };
+  auto steps_at = [&](int h0, int i) { return h0 + 64 * i + lane < heads ? steps_of(size[i].count, size[i].n) : 0; };
+#pragma unroll
+  for (int i = 0; i < SCAN_GROUP; ++i) size[i] = HeadSize{0, 0};
+  int mine = 0, longest = 0;
+  for (int h0 = (heads - 1) / (64 * SCAN_GROUP) * (64 * SCAN_GROUP); h0 >= 0; h0 -= 64 * SCAN_GROUP) {
+    fetch(h0);
+#pragma unroll
+    for (int i = 0; i < SCAN_GROUP; ++i) {
+      mine += steps_at(h0, i);
+      longest = max(longest, steps_at(h0, i));
+    }
   }
   const int total = __builtin_amdgcn_readlane(wave_scan(mine), 63);          // the host has seen to it that this fits
-  int p = ATT_LEAST_LOG;
-  while ((total - 1) >> p >= Q.target) ++p;
-  int before = 0;
-  for (int h0 = 0; h0 < heads; h0 += 64) {
-    const int h = h0 + lane, steps = h0 == 0 ? kept : h < heads ? head_steps(C, Q, (unsigned)h) : 0;
-    const int parts = (steps + (1 << p) - 1) >> p, upto = before + wave_scan(parts);
-    const unsigned long long beyond = __ballot(upto > fragment);
-    if (beyond != 0) {
-      const int at = __builtin_ctzll(beyond);
-      P.head = h0 + at;
-      P.steps = __builtin_amdgcn_readlane(steps, at);
-      P.parts = __builtin_amdgcn_readlane(parts, at);
-      P.first = __builtin_amdgcn_readlane(upto, at) - P.parts;
-      P.step0 = (fragment - P.first) << p;
-      P.step1 = min(P.step0 + (1 << p), P.steps);
-      return true;
+  longest = __builtin_amdgcn_readlane(wave_max_up(longest), 63);
+  int log = ATT_LEAST_LOG, per = 0;        // steps of a fragment: 1 << log, or `per` where that is not 0
+  while ((total - 1) >> log >= Q.target) ++log;
+  if (10ll * total >= 9ll * longest * heads)
+    for (int parts = 1; parts <= EVEN_PARTS && per == 0; ++parts) {
+      const int wgs = heads * parts, over = wgs % ATT_EVEN;
+      if (wgs <= 2 * ATT_EVEN && (over == 0 || 10 * over >= 9 * ATT_EVEN)) per = max(1 << ATT_LEAST_LOG, (int)((unsigned)(longest + parts - 1) / (unsigned)parts));
     }
-    before = __builtin_amdgcn_readlane(upto, 63);
+  int before = 0;
+  for (int h0 = 0; h0 < heads; h0 += 64 * SCAN_GROUP) {
+    if (h0 > 0) fetch(h0);
+#pragma unroll
+    for (int i = 0; i < SCAN_GROUP; ++i) {
+      if (i > 0 && h0 + 64 * i >= heads) break;
+      const int steps = steps_at(h0, i);
+      int parts = (steps + (1 << log) - 1) >> log;
+      if (per > 0) {
+        parts = 0;
+#pragma unroll
+        for (int k = 0; k < EVEN_PARTS; ++k) parts += steps > k * per;
+      }
+      const int upto = before + wave_scan(parts);
+      const unsigned long long beyond = __ballot(upto > fragment);
+      if (beyond != 0) {
+        const int at = __builtin_ctzll(beyond), each = per > 0 ? per : 1 << log;
+        F.head = h0 + 64 * i + at;
+        F.count = __builtin_amdgcn_readlane(size[i].count, at);
+        F.n = __builtin_amdgcn_readlane(size[i].n, at);
+        F.parts = __builtin_amdgcn_readlane(parts, at);
+        F.first = __builtin_amdgcn_readlane(upto, at) - F.parts;
+        F.step0 = (fragment - F.first) * each;
+        F.step1 = min(F.step0 + each, __builtin_amdgcn_readlane(steps, at));
+        return true;
+      }
+      before = __builtin_amdgcn_readlane(upto, 63);
+    }
   }
   return false;
+}
+
+// Part blockIdx.x / heads of a head.  Workgroups go round the eight XCDs, and heads often come in eights: neighbours in a group of eight
+// change places from group to group, or an XCD would have the same kv head of every request, long or short.
+__device__ __forceinline__ bool split_part(const CacheView &C, const Queries &Q, Fragment &F, int &fragment) {
+  const unsigned heads = (unsigned)C.nreq * (unsigned)C.layers * (unsigned)C.kv_heads;
+  const unsigned part = Q.split == 1 ? 0u : blockIdx.x / heads, i = blockIdx.x - part * heads;
+  F.head = (int)((i | 7u) < heads ? (i & ~7u) | ((i + (i >> 3) + part) & 7u) : i);
+  const HeadSize size = head_size(C, Q, (unsigned)F.head);
+  F.count = size.count;
+  F.n = size.n;
+  const int steps = steps_of(size.count, size.n);
+  const int per = Q.split == 1 ? steps : max(1 << ATT_LEAST_LOG, (int)((unsigned)(steps + Q.split - 1) / (unsigned)Q.split));
+  F.first = F.head * Q.split;
+  F.parts = Q.split == 1 ? 1 : (int)((unsigned)(steps + per - 1) / (unsigned)per);
+  F.step0 = (int)part * per;
+  F.step1 = min(F.step0 + per, steps);
+  fragment = F.first + (int)part;
+  return (int)part < F.parts;
 }
 
 template <int NT, bool PAGE16>
@@ -281,20 +367,24 @@ __global__ __launch_bounds__(256, NT <= 2 ? 2 : 1) void attend_kernel(const Cach
   __shared__ AttendLds<NT> L;
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, n16 = lane & 15, j = lane >> 4;
   const int R = Q.tokens * Q.group;
-  Part part{(int)blockIdx.x, 0, 0, 0x7fffffff, 0, 1};
-  if (Q.target > 0 && !find_part(C, Q, (int)blockIdx.x, part)) {
-    if (tid == 0) Q.frags[blockIdx.x].head = -1;
+  Fragment part;
+  int fragment = (int)blockIdx.x;
+  if (!(Q.target > 0 ? scan_part(C, Q, fragment, part) : split_part(C, Q, part, fragment))) {
+    if (tid == 0) Q.frags[fragment].head = -1;
     return;
+  }
+  if (Q.fragments && tid == 0) {
+    Q.frags[fragment] = part;
+    if (part.step0 == 0) Q.head_frags[part.head] = make_int2(part.first, part.parts);
   }
   const unsigned g = (unsigned)part.head;
   const HeadOf w = head_of(C, g);
   const HeadPlace hp = head_place(C, w);
-  const int count = held(C, w.b, w.l, w.h), n = tokens_new(Q.new_tokens, w.b, Q.tokens);
-  const int steps = steps_of(count, n), step0 = part.step0, step1 = min(part.step1, steps);
+  const int count = part.count, n = part.n;
   const bool complete = part.parts == 1;
-  const int end = n > 0 ? (step1 == steps ? count : step1 * ATT_STEP) : 0;      // no queries: no tiles
+  const int end = n > 0 ? min(part.step1 * ATT_STEP, count) : 0;      // no queries: no tiles
   // every wave has a run of the part's tiles
-  const int begin = step0 * ATT_STEP, each = (max(end - begin, 0) + ATT_STEP - 1) / ATT_STEP, first = begin + wave * each * ATT_TILE;
+  const int begin = part.step0 * ATT_STEP, each = (max(end - begin, 0) + ATT_STEP - 1) / ATT_STEP, first = begin + wave * each * ATT_TILE;
   const int tiles = first < end ? min(each, (end - first + ATT_TILE - 1) / ATT_TILE) : 0;
   const int seen_by_all = count - (n - 1);
   const uint16_t *kp = C.k + hp.rows, *vp = C.v + hp.rows;
@@ -328,12 +418,6 @@ __global__ __launch_bounds__(256, NT <= 2 ? 2 : 1) void attend_kernel(const Cach
     const unsigned two = (unsigned)(P.there >> (2 * (tile & 31)));
     return (two & 1u ? 0xffffu : 0u) | (two & 2u ? 0xffff0000u : 0u);
   };
-  // No load of rows is under a condition, or the compiler would have to wait for V where it waits for K: behind the last tile all
-  // lanes load one piece of rows that exist.
-  load_rows<PAGE16, true>(kp, P, 0, lane, tiles > 0 ? k_at : 0u, stride, k);
-  load_rows<PAGE16, false>(vp, P, 0, lane, tiles > 0 ? v_at : 0u, stride, v);
-  unsigned there = tile_there(0);          // bit i: slot i of the tile holds a token whose page is there
-
   f32x4 acc[NT][8];
   float m[NT], l[NT];            // of query l & 15: reference of its exponents, the lane's part of their sum
 #pragma unroll
@@ -361,9 +445,10 @@ __global__ __launch_bounds__(256, NT <= 2 ? 2 : 1) void attend_kernel(const Cach
     wave_lds_fence();
   };
 
-  for (int tile = 0; tile < tiles; ++tile) {
+  unsigned there;                // bit i: slot i of the tile holds a token whose page is there
+  auto one_tile = [&](int tile, auto another) {
+    constexpr bool more = decltype(another)::value;
     const int s0 = first + tile * ATT_TILE;
-    const bool more = tile + 1 < tiles;
     f32x4 s[NT][2];
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt)
@@ -375,15 +460,17 @@ __global__ __launch_bounds__(256, NT <= 2 ? 2 : 1) void attend_kernel(const Cach
           s[nt][half] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[4 * half + kk].v, q[nt][kk].v, s[nt][half], 0, 0, 0);
       }
     // K of the next tile leaves as soon as its registers are free, V after the second product.
-    if (PAGE16) {
-      if (more && ((tile + 1) & 31) == 0) places_run(C, hp, s0 + ATT_TILE, count, lane, P);
-    } else {
-      places_take(C, P);
-      places_fetch(C, hp, (long long)s0 + 2 * ATT_TILE, count, lane, P);
+    unsigned there_next = 0;
+    if constexpr (more) {
+      if (PAGE16) {
+        if (((tile + 1) & 31) == 0) places_run(C, hp, s0 + ATT_TILE, count, lane, P);
+      } else {
+        places_take(C, P);
+        places_fetch(C, hp, (long long)s0 + 2 * ATT_TILE, count, lane, P);
+      }
+      load_rows<PAGE16, true>(kp, P, (tile + 1) & 31, lane, k_at, stride, k);
+      there_next = tile_there(tile + 1);
     }
-    const unsigned spread = more ? 0xffffffffu : 0u;
-    load_rows<PAGE16, true>(kp, P, (tile + 1) & 31, lane, k_at & spread, stride, k);
-    const unsigned there_next = tile_there(tile + 1);
     __builtin_amdgcn_sched_barrier(0);
     const int left = count - s0;
     if (left < 32) there &= (1u << left) - 1u;              // left >= 1
@@ -499,9 +586,18 @@ __global__ __launch_bounds__(256, NT <= 2 ? 2 : 1) void attend_kernel(const Cach
         acc[nt][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.v, lo[nt].v, acc[nt][c], 0, 0, 0);
       }
     }
-    load_rows<PAGE16, false>(vp, P, (tile + 1) & 31, lane, v_at & spread, stride, v);
+    if constexpr (more) load_rows<PAGE16, false>(vp, P, (tile + 1) & 31, lane, v_at, stride, v);
     there = there_next;
     __builtin_amdgcn_sched_barrier(0);
+  };
+  // No load of rows of the loop is under a condition, or the compiler would have to wait for V where it waits for K; nor is one
+  // issued that nobody wants: the barrier below would wait for it.
+  if (tiles > 0) {
+    load_rows<PAGE16, true>(kp, P, 0, lane, k_at, stride, k);
+    load_rows<PAGE16, false>(vp, P, 0, lane, v_at, stride, v);
+    there = tile_there(0);
+    for (int tile = 0; tile + 1 < tiles; ++tile) one_tile(tile, std::true_type());
+    one_tile(tiles - 1, std::false_type());
   }
 
   // the four waves meet
@@ -518,10 +614,6 @@ __global__ __launch_bounds__(256, NT <= 2 ? 2 : 1) void attend_kernel(const Cach
     }
   }
   __syncthreads();
-  if (Q.target > 0 && tid == 0) {
-    Q.frags[blockIdx.x] = Fragment{complete ? -1 : (int)g, step0 * ATT_STEP, end, part.first, part.parts};
-    if (step0 == 0) Q.head_frags[g] = make_int2(part.first, part.parts);
-  }
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt) {
     const int r = 16 * nt + n16;
@@ -556,7 +648,7 @@ __global__ __launch_bounds__(256, NT <= 2 ? 2 : 1) void attend_kernel(const Cach
         finish_row(C, Q, w, row, ch, o, mm, sum);
         if (ch == 0) L.lse2[row] = sum == 0.f ? INFINITY : mm + __builtin_amdgcn_logf(sum);
       } else {
-        const long long at = (long long)blockIdx.x * R + row;
+        const long long at = (long long)fragment * R + row;
         f32x4 *to = reinterpret_cast<f32x4 *>(Q.partial + at * D + ch);
         to[0] = o[0];
         to[1] = o[1];
@@ -568,7 +660,11 @@ __global__ __launch_bounds__(256, NT <= 2 ? 2 : 1) void attend_kernel(const Cach
   if (complete && store && n > 0) {
     __threadfence_block();
     __syncthreads();                                // the workgroup's logits and sums
-    add_mass(C, Q, hp, L.lse2, logits, R, 0, count);
+    for (int at = 4 * tid; at < count; at += 4 * 256) {
+      MassQuad M;
+      mass_fetch(C, Q, hp, logits, R, at, count, M);
+      mass_add(Q, L.lse2, logits, R, at, M);
+    }
   }
 }
 
@@ -628,16 +724,23 @@ __global__ __launch_bounds__(256) void attend_join_kernel(const CacheView C, con
   const unsigned i = (blockIdx.x - rows) / MASS_PARTS;
   const int part = (int)(blockIdx.x - rows - i * MASS_PARTS);
   const Fragment f = Q.frags[i];
-  if (f.head < 0) return;
-  const HeadOf w = head_of(C, (unsigned)f.head);
-  if (held(C, w.b, w.l, w.h) > Q.most) return;
+  if (f.head < 0 || f.parts < 2 || f.count > Q.most) return;
+  const HeadPlace hp = head_place(C, head_of(C, (unsigned)f.head));
+  const float *logits = Q.logits + (long long)f.head * R * Q.pitch;
+  const int begin = f.step0 * ATT_STEP, end = min(f.step1 * ATT_STEP, f.count);
+  const int each = ((end - begin + MASS_PARTS - 1) / MASS_PARTS + 3) & ~3, from = begin + part * each, to = min(from + each, end);
+  if (from >= to) return;
+  MassQuad M;
+  mass_fetch(C, Q, hp, logits, R, min(from + 4 * tid, (to - 1) & ~3), to, M);
   for (int r = tid >> 6; r < R; r += 4) {          // every wave takes rows in turn
     const float2 all = join_stats(Q, f.first, f.parts, R, r);
     if ((tid & 63) == 0) lse2[r] = all.y == 0.f ? INFINITY : all.x + __builtin_amdgcn_logf(all.y);
   }
   __syncthreads();
-  const int each = ((f.to - f.from + MASS_PARTS - 1) / MASS_PARTS + 3) & ~3, from = f.from + part * each;
-  add_mass(C, Q, head_place(C, w), lse2, Q.logits + (long long)f.head * R * Q.pitch, R, from, min(from + each, f.to));
+  for (int at = from + 4 * tid; at < to; at += 4 * 256) {
+    if (at >= from + 4 * 256) mass_fetch(C, Q, hp, logits, R, at, to, M);
+    mass_add(Q, lse2, logits, R, at, M);
+  }
 }
 
 static int query_check(const compactor_cache_query_t *q, const CacheView &C) {
@@ -653,7 +756,7 @@ static int query_most(const CacheView &C, const compactor_cache_query_t *q) {
 }
 
 struct AttendPlan {
-  int rows, frags_most, target, pitch;
+  int rows, frags_most, target, split, pitch;
   size_t frags, head_frags, partial, stats, logits;       // bytes, in this order in the workspace
   size_t bytes() const { return frags + head_frags + partial + stats + logits; }
 };
@@ -667,10 +770,14 @@ static AttendPlan attend_plan(const CacheView &C, const compactor_cache_query_t 
   const long long heads = (long long)C.nreq * C.layers * C.kv_heads, most = query_most(C, q);
   const long long steps = (most + ATT_STEP - 1) / ATT_STEP;
   A.rows = q->tokens * (q->q_heads / C.kv_heads);
+  A.split = 1;
   A.target = A.frags_most = 0;
-  if (steps > ATT_ALONE && heads * steps <= 0x7fffffffll) {
-    A.target = ATT_ROUNDS * (A.rows <= 32 ? 2 : 1) * cus;
-    A.frags_most = (int)std::min((long long)A.target, ((heads * steps - 1) >> ATT_LEAST_LOG) + 1) + (int)heads;
+  if (steps > ATT_ALONE && heads <= SCAN_HEADS && heads * steps <= 0x7fffffffll) {
+    A.target = SCAN_ROUNDS * (A.rows <= 32 ? 2 : 1) * cus;
+    A.frags_most = (int)(std::max(std::min((long long)A.target, ((heads * steps - 1) >> ATT_LEAST_LOG) + 1), 2ll * ATT_EVEN) + heads);
+  } else if (steps > ATT_ALONE) {
+    A.split = (int)std::max(std::min(std::min(SPLIT_ALL / heads, (long long)SPLIT_MOST), ((steps - 1) >> ATT_LEAST_LOG) + 1), 1ll);
+    if (A.split > 1) A.frags_most = A.split * (int)heads;
   }
   A.pitch = (int)((most + ATT_TILE - 1) / ATT_TILE * ATT_TILE);
   auto up = [](size_t x) { return (x + 255) / 256 * 256; };
@@ -730,8 +837,8 @@ int compactor_cache_attention(const compactor_cache_t *cache, const compactor_ca
   if (need > 0 && (!workspace || workspace_bytes < need)) return COMPACTOR_EWORKSPACE;
   if (need > 0 && (reinterpret_cast<uintptr_t>(workspace) & 255u)) return COMPACTOR_EALIGN;
   const long long heads = (long long)C.nreq * C.layers * C.kv_heads;
-  const long long blocks = A.target > 0 ? A.frags_most : heads;
-  const long long join = A.target > 0 ? heads * A.rows + (query->accumulate ? (long long)MASS_PARTS * A.frags_most : 0) : 0;
+  const long long blocks = A.frags_most > 0 ? A.frags_most : heads;
+  const long long join = A.frags_most > 0 ? heads * A.rows + (query->accumulate ? (long long)MASS_PARTS * A.frags_most : 0) : 0;
   if (blocks > 0x7fffffffll || join > 0x7fffffffll) return COMPACTOR_EINVAL;
   Queries Q;
   Q.q = static_cast<const uint16_t *>(query->q);
@@ -747,7 +854,8 @@ int compactor_cache_attention(const compactor_cache_t *cache, const compactor_ca
   Q.scale = query->scale > 0.f ? query->scale : 1.0f / sqrtf((float)D);
   Q.softcap = query->softcap;
   Q.target = A.target;
-  Q.frags_most = A.frags_most;
+  Q.split = A.split;
+  Q.fragments = A.frags_most > 0;
   unsigned char *ws = static_cast<unsigned char *>(workspace);
   Q.frags = reinterpret_cast<Fragment *>(ws);
   Q.head_frags = reinterpret_cast<int2 *>(ws += A.frags);
@@ -763,7 +871,7 @@ int compactor_cache_attention(const compactor_cache_t *cache, const compactor_ca
     launch_attend<true>(C, Q, (unsigned)blocks, st);
   else
     launch_attend<false>(C, Q, (unsigned)blocks, st);
-  if (A.target > 0) {
+  if (A.frags_most > 0) {
     if (hipGetLastError() != hipSuccess) return COMPACTOR_EHIP;
     hipLaunchKernelGGL(attend_join_kernel, dim3((unsigned)join), dim3(256), 0, st, C, Q);
   }

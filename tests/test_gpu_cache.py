@@ -93,6 +93,16 @@ def test_attention_long(C, B, L, H, n, page, G, T):
     _attend(C, P, _queries(P, T, H * G), cap=20.0 if T > 1 else 0.0)
 
 
+@pytest.mark.parametrize("B,L,H,lengths", [(5, 2, 9, (2000, 1, 0, 1025, 700, 128, 129, 1999)), (16, 1, 8, (1300,)), (16, 1, 8, (1290, 1300, 1280)),
+                                           (43, 1, 7, (1100, 30, 0, 1500)), (37, 2, 4, (1100, 1090)), (8, 8, 8, (1030, 1024, 513, 60)),
+                                           (65, 1, 8, (1100, 5, 900, 0, 1400)), (9, 8, 9, (1200,)), (1, 513, 1, (1025,)), (200, 3, 7, (40, 1100, 0))])
+def test_attention_of_many_heads(C, B, L, H, lengths):
+    """Heads of one length and of many, up to and beyond the number whose lengths a workgroup looks through."""
+    P = U.Paged(C, DEV, _counts(B, L, H, *lengths), page=32, layout="token", seed=B)
+    new = None if B % 2 else [b % 3 for b in range(B)]
+    _attend(C, P, _queries(P, 2, H), new=new, accumulate=B != 37, what="%d heads" % (B * L * H))
+
+
 @pytest.mark.parametrize("page", [16, 24, 128])
 @pytest.mark.parametrize("fill", [float("nan"), float("inf"), -float("inf")])
 def test_attention_does_not_look_past_the_end(C, page, fill):
@@ -189,6 +199,15 @@ def _attend_given(C, P, q, out, lse):
     n = q.shape[0] * q.shape[1] * q.shape[2] * q.shape[3]
     U.check_attention(P, q, None, 128 ** -0.5, 0.0, got, s[:n].view(q.shape[:4]), before, True)
     return got, s
+
+
+def test_attention_with_tables_inside_a_larger_one(C):
+    P = U.Paged(C, DEV, _counts(3, 1, 2, 70, 200, 33), page=16)
+    wide = torch.full((3, P.per + 9), -1, dtype=torch.int32, device=DEV)
+    wide[:, 4:4 + P.per] = P.tables
+    P.tables = wide[:, 4:4 + P.per]
+    P.cache = P.handle()
+    _attend(C, P, _queries(P, 1, 8))
 
 
 def test_attention_without_state(C):
