@@ -306,6 +306,9 @@ __device__ __forceinline__ bool scan_part(const CacheView &C, const Queries &Q, 
   longest = __builtin_amdgcn_readlane(wave_max_up(longest), 63);
   int log = ATT_LEAST_LOG, per = 0;        // steps of a fragment: 1 << log, or `per` where that is not 0
   while ((total - 1) >> log >= Q.target) ++log;
+  // More than 16 query rows make a start dearer, and 64 leave room for one workgroup a unit: twice as much for each where there is enough
+  // for all (24 heads of 18000, 40 rows: 84 us with 4 steps, 64 with 8; 96 heads of 900 to 9800, 20 rows, 72 and 67).
+  if (log == ATT_LEAST_LOG && Q.tokens * Q.group > 16 && total >> (log + 1) >= ATT_EVEN) ++log;
   if (10ll * total >= 9ll * longest * heads)
     for (int parts = 1; parts <= EVEN_PARTS && per == 0; ++parts) {
       const int wgs = heads * parts, over = wgs % ATT_EVEN;
