@@ -775,9 +775,10 @@ static AttendPlan attend_plan(const CacheView &C, const compactor_cache_query_t 
   A.rows = q->tokens * (q->q_heads / C.kv_heads);
   A.split = 1;
   A.target = A.frags_most = 0;
-  if (steps > ATT_ALONE && heads <= SCAN_HEADS && heads * steps <= 0x7fffffffll) {
-    A.target = SCAN_ROUNDS * (A.rows <= 32 ? 2 : 1) * cus;
-    A.frags_most = (int)(std::max(std::min((long long)A.target, ((heads * steps - 1) >> ATT_LEAST_LOG) + 1), 2ll * ATT_EVEN) + heads);
+  // a wave adds up the steps of heads that may hold more than `most`, and their fragments have to fit all the same
+  if (steps > ATT_ALONE && heads <= SCAN_HEADS && heads * (((long long)C.capacity + ATT_STEP - 1) / ATT_STEP) <= 0x7fffffffll) {
+    A.target = (int)std::min((long long)SCAN_ROUNDS * (A.rows <= 32 ? 2 : 1) * cus, ((heads * steps - 1) >> ATT_LEAST_LOG) + 1);
+    A.frags_most = std::max(A.target, 2 * ATT_EVEN) + (int)heads;
   } else if (steps > ATT_ALONE) {
     A.split = (int)std::max(std::min(std::min(SPLIT_ALL / heads, (long long)SPLIT_MOST), ((steps - 1) >> ATT_LEAST_LOG) + 1), 1ll);
     if (A.split > 1) A.frags_most = A.split * (int)heads;

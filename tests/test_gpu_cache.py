@@ -222,6 +222,13 @@ def test_attention_of_more_tokens_than_promised(C):
     _attend(C, P, _queries(P, 2, 24), most=10 ** 6)
 
 
+@pytest.mark.parametrize("B,H,n,most", [(1, 8, 42000, 1100), (1, 1, 300000, 1100), (2, 64, 9000, 1030), (75, 8, 1500, 1100)])
+def test_attention_of_many_more_tokens_than_promised(C, B, H, n, most):
+    """Launches and workspace are made for `most` tokens a head; what is beyond them has to fit in."""
+    P = U.Paged(C, DEV, _counts(B, 1, H, n, most, n - 77, 5), page=64)
+    _attend(C, P, _queries(P, 1, 2 * H), most=most)
+
+
 def test_attention_counts_outside_the_table(C):
     P = U.Paged(C, DEV, _counts(1, 1, 3, 64, 64, 64), page=16)
     P.counts[0, 0] = torch.tensor([-5, 1000, 64], dtype=torch.int32)
