@@ -331,14 +331,14 @@ int compactor_attention_scores(const compactor_attn_params_t *p,
  * page tables[b*table_stride + s / page_size]; slots 0 .. counts-1 hold its tokens, in any order.
  * A count is taken as one of 0 .. table_len*page_size.  A table entry outside [0, num_pages) marks a
  * page that is not there: its slots are seen by no query, written by no call and evicted first.
- * Pages that several contexts name (a common prefix) may be attended to, but not be appended to,
- * accumulated into or evicted from.  A cache of one layer for calls layer by layer: layers = 1 and
+ * Pages that are named more than once (a common prefix of several contexts) may be attended to, but not be
+ * appended to, accumulated into or evicted from.  A cache of one layer for calls layer by layer: layers = 1 and
  * every pointer moved to that layer. */
 typedef struct compactor_cache {
   compactor_page_pool_t pool;
   const int32_t *tables;  /* device, int32 [nreq][table_stride] */
   int64_t table_stride;   /* >= table_len */
-  int32_t table_len;      /* logical pages per request, >= 1; table_len * page_size < 2^31 - 64 */
+  int32_t table_len;      /* logical pages per request, >= 1; table_len * page_size <= 2^30 */
   int32_t nreq, layers, kv_heads;
   int32_t head_dim;       /* 128 */
   int32_t *counts;        /* device: cached tokens of (b, l, h), at b*count_stride_b + l*count_stride_l + h */
@@ -388,7 +388,7 @@ typedef struct compactor_cache_query {
   int32_t tokens;         /* T >= 1: the queries are those of the last tokens that were appended */
   int32_t q_heads;        /* a multiple of kv_heads: query heads h*G .. h*G+G-1 share kv head h; G*T <= 64 */
   float   scale;          /* logit scale; 0 = 1/sqrt(head_dim) */
-  float   softcap;        /* c > 0: a logit x becomes c * tanh(x / c); 0 = none */
+  float   softcap;        /* c > 0: a logit x becomes c * tanh(x / c); 0 = none (scale/c, and both times log2 e, finite) */
   int32_t accumulate;     /* not 0: adds the weights to the cache's mass */
   int32_t max_tokens;     /* tokens that no head holds more of, 0 = what the tables hold.  Launches and
                              workspace go by it.  A head that holds more all the same is attended to in
@@ -425,7 +425,8 @@ typedef struct compactor_cache_evict_params {
 /* Brings caches down to their budgets.  Of a head (layer) that holds more tokens than its budget, the
  * first ones in this order stay: protected tokens, then larger mass first, NaN last; equal ones by
  * lower (head, slot).  Retained tokens in slots from the new count on move, in ascending order, to the slots
- * below it that were given up, in ascending order: K and V rows, mass and position.  All others stay
+ * below it that were given up, in ascending order: K and V rows, mass and position (into a page that is not there:
+ * nowhere).  All others stay
  * where they are, and so do the contents of slots that no token is in any more. */
 int compactor_cache_evict(const compactor_cache_t *cache, const compactor_cache_evict_params_t *evict,
                           void *workspace, size_t workspace_bytes, void *stream);

@@ -16,7 +16,8 @@ int cache_view(const compactor_cache_t *c, CacheNeed need, CacheView *view) {
   if (c->head_dim != D) return COMPACTOR_EUNSUPPORTED;
   const compactor_page_pool_t &p = c->pool;
   if (p.page_size < 1 || p.num_pages < 1 || c->table_len < 1 || c->table_stride < c->table_len) return COMPACTOR_EINVAL;
-  if ((long long)c->table_len * p.page_size > 0x7fffffffll - 64) return COMPACTOR_EINVAL;
+  // (half a TB of rows of one head; sums of a slot and a launch's steps, and a tile's end, then fit)
+  if ((long long)c->table_len * p.page_size > 1ll << 30) return COMPACTOR_EINVAL;
   if (need != CACHE_SIZES) {
     if (!p.k_pages || !p.v_pages || !c->tables || !c->counts) return COMPACTOR_EINVAL;
     if (p.page_stride < 0 || p.layer_stride < 0 || p.head_stride < 0 || p.slot_stride < D) return COMPACTOR_EINVAL;

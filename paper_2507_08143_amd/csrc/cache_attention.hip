@@ -431,11 +431,11 @@ __global__ __launch_bounds__(256, NT <= 2 ? 2 : 1) void attend_kernel(const Cach
     for (int c = 0; c < 8; ++c) acc[nt][c] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
   const bool capped = Q.softcap > 0.f;
-  const float to_base2 = Q.scale * LOG2E, to_tanh = capped ? 2.f * LOG2E * Q.scale / Q.softcap : 0.f, cap2 = Q.softcap * LOG2E;
+  const float to_base2 = Q.scale * LOG2E, to_y = capped ? Q.scale / Q.softcap : 0.f, cap2 = Q.softcap * LOG2E;
   const bool store = Q.logits != nullptr && count <= Q.most;
   float *logits = Q.logits + (long long)g * R * Q.pitch;
-  // Logits wait in LDS and leave at the end, behind the last barrier, which would else wait until they have arrived (batch of 2.3 M
-  // slots, 4 rows: 229 us against 205, without them 201); where that is full, on the way.
+  // Logits wait in LDS and leave in whole lines, a run of tiles of a row at a time (written as they come, 16 bytes a lane: 239 us for
+  // 2.3 M slots and 4 rows, so 229, without them 203; streamed, or behind the last barrier instead of before it, the same).
   float *kept = L.kept[wave];
   const int kept_tiles = max(1, KEPT_FLOATS / (ATT_TILE * R));
   auto leave = [&](int upto) {              // tiles up to this one
@@ -507,10 +507,14 @@ __global__ __launch_bounds__(256, NT <= 2 ? 2 : 1) void attend_kernel(const Cach
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
       float x[8];
-      if (capped) {                // tanh(y) = 1 - 2 / (e^2y + 1)
+      if (capped) {                // tanh(y) = 1 - 2 / (e^2y + 1); near 0, where that cancels, y times a polynomial in y^2
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-          x[i] = cap2 - 2.f * cap2 * __builtin_amdgcn_rcpf(exp2_(s[nt][i >> 2][i & 3] * to_tanh) + 1.f);
+        for (int i = 0; i < 8; ++i) {
+          const float dot = s[nt][i >> 2][i & 3], y = dot * to_y, z = y * y;
+          const float far = cap2 - 2.f * cap2 * __builtin_amdgcn_rcpf(exp2_(y * (2.f * LOG2E)) + 1.f);
+          const float slope = fmaf(z, fmaf(z, fmaf(z, fmaf(z, 62.f / 2835.f, -17.f / 315.f), 2.f / 15.f), -1.f / 3.f), 1.f);
+          x[i] = z < 1.f / 16.f ? dot * to_base2 * slope : far;
+        }
       } else {
 #pragma unroll
         for (int i = 0; i < 8; ++i) x[i] = s[nt][i >> 2][i & 3] * to_base2;
@@ -672,8 +676,7 @@ __global__ __launch_bounds__(256, NT <= 2 ? 2 : 1) void attend_kernel(const Cach
 }
 
 // Second launch: the fragments of a head meet.  The first heads * R workgroups take a query row each, 16 fragments side by side
-// and 8 channels a thread; the others add a fragment's weights to the mass, MASS_PARTS to a fragment.
-constexpr int MASS_PARTS = 1;
+// and 8 channels a thread; the others add a fragment's weights to the mass.
 
 // Maximum and sum of row r over the fragments, by the lanes of a wave.
 __device__ __forceinline__ float2 join_stats(const Queries &Q, int first, int parts, int R, int r) {
@@ -724,14 +727,11 @@ __global__ __launch_bounds__(256) void attend_join_kernel(const CacheView C, con
     }
     return;
   }
-  const unsigned i = (blockIdx.x - rows) / MASS_PARTS;
-  const int part = (int)(blockIdx.x - rows - i * MASS_PARTS);
-  const Fragment f = Q.frags[i];
+  const Fragment f = Q.frags[blockIdx.x - rows];
   if (f.head < 0 || f.parts < 2 || f.count > Q.most) return;
   const HeadPlace hp = head_place(C, head_of(C, (unsigned)f.head));
   const float *logits = Q.logits + (long long)f.head * R * Q.pitch;
-  const int begin = f.step0 * ATT_STEP, end = min(f.step1 * ATT_STEP, f.count);
-  const int each = ((end - begin + MASS_PARTS - 1) / MASS_PARTS + 3) & ~3, from = begin + part * each, to = min(from + each, end);
+  const int from = f.step0 * ATT_STEP, to = min(f.step1 * ATT_STEP, f.count);
   if (from >= to) return;
   MassQuad M;
   mass_fetch(C, Q, hp, logits, R, min(from + 4 * tid, (to - 1) & ~3), to, M);
@@ -746,11 +746,15 @@ __global__ __launch_bounds__(256) void attend_join_kernel(const CacheView C, con
   }
 }
 
+static float scale_of(const compactor_cache_query_t *q) { return q->scale > 0.f ? q->scale : 1.0f / sqrtf((float)D); }
+
 static int query_check(const compactor_cache_query_t *q, const CacheView &C) {
   if (!q) return COMPACTOR_EINVAL;
   if (q->tokens < 1 || q->q_heads < C.kv_heads || q->q_heads % C.kv_heads || q->max_tokens < 0) return COMPACTOR_EINVAL;
   if ((long long)(q->q_heads / C.kv_heads) * q->tokens > 64) return COMPACTOR_EUNSUPPORTED;
-  if (!(q->scale >= 0.f) || !isfinite(q->scale) || !(q->softcap >= 0.f) || !isfinite(q->softcap)) return COMPACTOR_EINVAL;
+  // (in base 2 too, and relative to the cap)
+  if (!(q->scale >= 0.f) || !isfinite(q->scale * LOG2E) || !(q->softcap >= 0.f) || !isfinite(q->softcap * LOG2E)) return COMPACTOR_EINVAL;
+  if (q->softcap > 0.f && !isfinite(scale_of(q) / q->softcap)) return COMPACTOR_EINVAL;
   return COMPACTOR_OK;
 }
 
@@ -842,7 +846,7 @@ int compactor_cache_attention(const compactor_cache_t *cache, const compactor_ca
   if (need > 0 && (reinterpret_cast<uintptr_t>(workspace) & 255u)) return COMPACTOR_EALIGN;
   const long long heads = (long long)C.nreq * C.layers * C.kv_heads;
   const long long blocks = A.frags_most > 0 ? A.frags_most : heads;
-  const long long join = A.frags_most > 0 ? heads * A.rows + (query->accumulate ? (long long)MASS_PARTS * A.frags_most : 0) : 0;
+  const long long join = A.frags_most > 0 ? heads * A.rows + (query->accumulate ? A.frags_most : 0) : 0;
   if (blocks > 0x7fffffffll || join > 0x7fffffffll) return COMPACTOR_EINVAL;
   Queries Q;
   Q.q = static_cast<const uint16_t *>(query->q);
@@ -855,7 +859,7 @@ int compactor_cache_attention(const compactor_cache_t *cache, const compactor_ca
   Q.new_tokens = query->new_tokens;
   Q.tokens = query->tokens;
   Q.group = query->q_heads / C.kv_heads;
-  Q.scale = query->scale > 0.f ? query->scale : 1.0f / sqrtf((float)D);
+  Q.scale = scale_of(query);
   Q.softcap = query->softcap;
   Q.target = A.target;
   Q.split = A.split;

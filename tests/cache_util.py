@@ -100,7 +100,8 @@ def attention_bounds(q, k, v, see, there, scale, cap, out, p):
     """How far one row's outputs may be off.  With u = 2^-24: a logit is a sum of d exact products, in any order
     off by (d - 1) u scale sum |q_c k_c|, its scaling and its way into the exponent's argument (two multiplications and a
     subtraction of numbers up to the largest |x|) by 6 u max |x|; a cap has slope <= 1 and is itself off by 2^-21 cap (its tanh
-    is 1 - 2 / (e + 1) with e off by a few u relative).  A weight e^(x - m) / sum is then off by 2 dx relative, by 2^-21 for the
+    is 1 - 2 / (e + 1) with e off by a few u relative), and by no more than 2^-19 |x| where x is small beside it (that form is taken from
+    tanh = 0.245 on, where 2^-21 is 2^-19 of the value; below it stands y (1 - y^2/3 + .. ), off by some 10 u).  A weight e^(x - m) / sum is then off by 2 dx relative, by 2^-21 for the
     exponentials, reciprocals and products, and by (n + 16) u for the sum; a weight that underflows is off by 2^-120.  The product with
     V takes it with 16 mantissa bits (2^-16 for the two roundings), and sums n terms (n + 16) u.  The output is rounded to bf16 once.
     -> (bound of out [d], of lse, relative bound of the weights)"""
@@ -112,7 +113,7 @@ def attention_bounds(q, k, v, see, there, scale, cap, out, p):
     x = scale * (k[at] @ q)
     dx = (D - 1) * u * scale * float(np.max(np.abs(k[at]) @ np.abs(q))) + 6 * u * float(np.max(np.abs(x)))
     if cap > 0:
-        dx += 2.0 ** -21 * cap
+        dx += min(2.0 ** -21 * cap, 2.0 ** -19 * float(np.max(np.abs(x))))
     rel = 2 * dx + 2.0 ** -21 + (n + 16) * u
     size = p[at] @ np.abs(v[at])
     b_out = size * (rel + 2.0 ** -16 + (n + 16) * u) + 2.0 ** -120 * np.abs(v[at]).sum(0)

@@ -60,6 +60,7 @@ BAD_CACHES = [
     (dict(layers=1 << 11, kv_heads=1 << 10), "EINVAL"), (dict(nreq=1 << 30, kv_heads=4), "EINVAL"),
     (dict(page_size=0), "EINVAL"), (dict(num_pages=0), "EINVAL"), (dict(table_len=0), "EINVAL"), (dict(table_stride=9), "EINVAL"),
     (dict(table_len=1 << 20, table_stride=1 << 20, page_size=1 << 11), "EINVAL"),
+    (dict(table_len=(1 << 20) + 1, table_stride=1 << 21, page_size=1 << 10), "EINVAL"),
     (dict(k_pages=0), "EINVAL"), (dict(v_pages=0), "EINVAL"), (dict(tables=0), "EINVAL"), (dict(counts=0), "EINVAL"),
     (dict(slot_stride=64), "EINVAL"), (dict(page_stride=-8), "EINVAL"), (dict(count_stride_b=-1), "EINVAL"),
     (dict(state_page_stride=-1), "EINVAL"), (dict(seen=0), "EINVAL"), (dict(mass=0), "EINVAL"), (dict(positions=0), "EINVAL"),
@@ -104,6 +105,7 @@ def test_bad_queries(B):
                      (dict(q_heads=12), B.EINVAL), (dict(tokens=17), B.EUNSUPPORTED), (dict(q_heads=520), B.EUNSUPPORTED),
                      (dict(scale=-1.0), B.EINVAL), (dict(scale=float("nan")), B.EINVAL), (dict(scale=float("inf")), B.EINVAL),
                      (dict(softcap=-1.0), B.EINVAL), (dict(softcap=float("inf")), B.EINVAL), (dict(max_tokens=-1), B.EINVAL),
+                     (dict(scale=3e38), B.EINVAL), (dict(softcap=3e38), B.EINVAL), (dict(scale=1.0, softcap=1e-39), B.EINVAL),
                      (dict(q_stride_t=-8), B.EINVAL), (dict(out_stride_h=-128), B.EINVAL), (dict(q=0x100002), B.EALIGN),
                      (dict(out=0x200008), B.EALIGN), (dict(out_stride_h=4), B.EALIGN), (dict(q_stride_b=12), B.EALIGN),
                      (dict(lse=0x3), B.EALIGN), (dict(new_tokens=0x6), B.EALIGN)):

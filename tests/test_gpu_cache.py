@@ -76,9 +76,10 @@ def test_attention_rows(C, G, T, accumulate):
     _attend(C, P, _queries(P, T, 2 * G), new=[-3, 1], accumulate=accumulate, what="G %d T %d, one token" % (G, T))
 
 
-@pytest.mark.parametrize("scale,cap,gain", [(0.0, 30.0, 1.0), (0.5, 5.0, 8.0), (0.02, 0.0, 8.0), (1.0, 0.0, 20.0), (1.0, 50.0, 20.0)])
+@pytest.mark.parametrize("scale,cap,gain", [(0.0, 30.0, 1.0), (0.5, 5.0, 8.0), (0.02, 0.0, 8.0), (1.0, 0.0, 20.0), (1.0, 50.0, 20.0),
+                                            (0.0, 1e4, 1.0), (0.3, 4e6, 8.0), (0.0, 2e38, 1.0), (0.0, 0.01, 1.0), (1.0, 1e-30, 1.0)])
 def test_attention_scales_and_caps(C, scale, cap, gain):
-    """Large logits too: one slot that takes all the weight, and caps that saturate."""
+    """Large logits too: one slot that takes all the weight, caps that saturate, and caps that no logit comes near."""
     P = U.Paged(C, DEV, _counts(2, 1, 4, 700, 33, 5, 1500), page=16, gain=gain)
     _attend(C, P, _queries(P, 2, 16), scale=scale, cap=cap)
 
