@@ -231,11 +231,14 @@ __device__ __forceinline__ void mass_add(const Queries &Q, const float *lse2, co
     if (M.there[i]) *M.mass[i] = fmaf(sum[i], inv, M.old[i]);
 }
 
-constexpr int KEPT_FLOATS = ATT_TILE * MOST_ROWS;      // logits that a wave keeps in LDS: a tile at least
+// Logits leave for the workspace 16 bytes a lane, or by way of LDS in whole lines, a run of tiles of a row at a time; up to 16 rows that pays
+// (2.3 M slots with 4 rows: 249 us and 255, without logits 221; streamed, or behind the last barrier: the same), with 20 rows 66 us and 64, with 40 158 and 102.
+constexpr int KEPT_FLOATS = 2048;            // that a wave keeps: 4 tiles of 16 rows
+template <int NT> constexpr bool kept_in_lds = NT == 1;
 template <int NT>
 struct AttendLds {
   float o[ATT_WAVES][16][D + 4];
-  float kept[ATT_WAVES][KEPT_FLOATS], p[ATT_WAVES][16][ATT_TILE + 1];
+  float kept[ATT_WAVES][kept_in_lds<NT> ? KEPT_FLOATS : 4], p[ATT_WAVES][16][ATT_TILE + 1];
   float m[ATT_WAVES][16 * NT], l[ATT_WAVES][16 * NT];
   float lse2[16 * NT];
 };
@@ -434,10 +437,8 @@ __global__ __launch_bounds__(256, NT <= 2 ? 2 : 1) void attend_kernel(const Cach
   const float to_base2 = Q.scale * LOG2E, to_y = capped ? Q.scale / Q.softcap : 0.f, cap2 = Q.softcap * LOG2E;
   const bool store = Q.logits != nullptr && count <= Q.most;
   float *logits = Q.logits + (long long)g * R * Q.pitch;
-  // Logits wait in LDS and leave in whole lines, a run of tiles of a row at a time (written as they come, 16 bytes a lane: 239 us for
-  // 2.3 M slots and 4 rows, so 229, without them 203; streamed, or behind the last barrier instead of before it, the same).
   float *kept = L.kept[wave];
-  const int kept_tiles = max(1, KEPT_FLOATS / (ATT_TILE * R));
+  const int kept_tiles = kept_in_lds<NT> ? KEPT_FLOATS / (ATT_TILE * R) : 1;
   auto leave = [&](int upto) {              // tiles up to this one
     wave_lds_fence();
     const int t0 = (upto - 1) / kept_tiles * kept_tiles, quads = (upto - t0) * (ATT_TILE / 4);
@@ -528,7 +529,7 @@ __global__ __launch_bounds__(256, NT <= 2 ? 2 : 1) void attend_kernel(const Cach
         }
       }
       if (store && 16 * nt + n16 < R) {
-        float *to = kept + ((tile % kept_tiles) * R + 16 * nt + n16) * ATT_TILE + 4 * j;
+        float *to = (kept_in_lds<NT> ? kept + ((tile % kept_tiles) * R + n16) * ATT_TILE : logits + (long long)(16 * nt + n16) * Q.pitch + s0) + 4 * j;
         *reinterpret_cast<f32x4 *>(to) = f32x4{x[0], x[1], x[2], x[3]};
         *reinterpret_cast<f32x4 *>(to + 16) = f32x4{x[4], x[5], x[6], x[7]};
       }
@@ -580,7 +581,7 @@ __global__ __launch_bounds__(256, NT <= 2 ? 2 : 1) void attend_kernel(const Cach
         }
       }
     }
-    if (store && more && (tile + 1) % kept_tiles == 0) leave(tile + 1);
+    if (kept_in_lds<NT> && store && more && (tile + 1) % kept_tiles == 0) leave(tile + 1);
     // channels 2 d and 2 d + 1 of the lane's piece, 8 slots each
 #pragma unroll
     for (int c = 0; c < 8; ++c) {
@@ -663,7 +664,7 @@ __global__ __launch_bounds__(256, NT <= 2 ? 2 : 1) void attend_kernel(const Cach
       }
     }
   }
-  if (store && tiles > 0) leave(tiles);
+  if (kept_in_lds<NT> && store && tiles > 0) leave(tiles);
   if (complete && store && n > 0) {
     __threadfence_block();
     __syncthreads();                                // the workgroup's logits and sums
