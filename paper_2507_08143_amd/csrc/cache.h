@@ -83,6 +83,28 @@ __device__ __forceinline__ long long state_at(const CacheView &C, const HeadPlac
   return s.page * C.state_page_stride + p.state + s.at;
 }
 
+// Sum over the lanes up to this one (row shifts, then the sums of rows and of halves of the wave handed on).
+__device__ __forceinline__ int wave_scan(int x) {
+  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);
+  x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);
+  return x;
+}
+
+// The largest of the lanes' numbers, in lane 63.
+__device__ __forceinline__ unsigned wave_max_up(unsigned x) {
+  x = max(x, (unsigned)__builtin_amdgcn_update_dpp(0, (int)x, 0x111, 0xf, 0xf, false));
+  x = max(x, (unsigned)__builtin_amdgcn_update_dpp(0, (int)x, 0x112, 0xf, 0xf, false));
+  x = max(x, (unsigned)__builtin_amdgcn_update_dpp(0, (int)x, 0x114, 0xf, 0xf, false));
+  x = max(x, (unsigned)__builtin_amdgcn_update_dpp(0, (int)x, 0x118, 0xf, 0xf, false));
+  x = max(x, (unsigned)__builtin_amdgcn_update_dpp(0, (int)x, 0x142, 0xa, 0xf, false));
+  x = max(x, (unsigned)__builtin_amdgcn_update_dpp(0, (int)x, 0x143, 0xc, 0xf, false));
+  return x;
+}
+
 // Checks a caller's cache (COMPACTOR_OK or an error) and makes the view of it.
 enum CacheNeed { CACHE_SIZES, CACHE_ROWS, CACHE_STATE };      // sizes only; pages and counts; and seen, mass, positions
 int cache_view(const compactor_cache_t *c, CacheNeed need, CacheView *view);

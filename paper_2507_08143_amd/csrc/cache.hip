@@ -239,7 +239,9 @@ hipError_t launch_cache_admit(const SegTable &T, const CacheView &C, const int32
 // One workgroup does everything where a pool is a head of up to ALONE_SLOTS tokens; its keys stay in registers.  Longer heads and
 // layers would keep one unit busy too long (some 70 instructions a slot: 32 layers of 79000 tokens 327 us), so there the pool is cut into parts of
 // PART_SLOTS slots and every part's workgroup does the same steps in a launch each: keys and the tally of their first 12 bits,
-// the next 12, the last 8, the lists, the moves.
+// the next 12, the last 8, the lists, the moves.  What bounds both is not the 8 bytes of state a slot but the chain of steps, and the instructions
+// of each, which are fetched as they are run for the first time (lists of 10 units a wave: 5.1 us, run a second time 2.9).  Workgroups of 8
+// waves with 8 units each: 8 heads of 26215 tokens 36 us, 32 layers of 79000 tokens 57; 4 with 16 41 and 60, 16 with 4 35 and 71.
 constexpr uint32_t KEY_PROTECTED = 0xffffffffu;      // above the key of +inf (0xff800000); 0: NaN, or a page that is not there
 
 struct EvictPlan {
@@ -267,78 +269,122 @@ __device__ __forceinline__ long long evict_budget(const EvictPlan &E, int b) {
   return (long long)E.pool_heads * (asked > 0 ? asked : 0);
 }
 
-// Keys of the 64 slots from first + 64 i on, i < N, one a lane; 0 where there is no token.  All table entries leave before the first is
-// waited for, and so do the states.
+// The first position that is protected as recent (an int: positions are).
+__device__ __forceinline__ int recent_from(const EvictPlan &E, int seen) {
+  const long long from = (long long)seen - E.recent;
+  return from < -0x80000000ll ? (int)-0x80000000ll : (int)from;
+}
+
+// Keys of the 64 slots from first + 64 i on, i < N, one a lane; 0 where there is no token.  count > 0.  `units`, uniform, of them hold
+// any.  All table entries leave before the first is waited for, and so do the states.  Four units at a time and the last token's slot
+// for what lies behind: code that runs once costs what its fetch takes.
 template <int N>
-__device__ __forceinline__ void evict_keys(const CacheView &C, const HeadPlace &p, const EvictPlan &E, int first, int units, int count, long long recent_from,
+__device__ __forceinline__ void evict_keys(const CacheView &C, const HeadPlace &p, const EvictPlan &E, int first, int units, int count, int recent,
                                            uint32_t (&key)[N]) {
   const int lane = threadIdx.x & 63;
-  int page[N], pos[N];
+  int page[N], at[N], pos[N];
   float mass[N];
 #pragma unroll
-  for (int i = 0; i < N; ++i) {
-    page[i] = -1;
-    if (i < units) {                                       // uniform
-      const int slot = first + 64 * i + lane;
-      if (slot < count) page[i] = p.table[invariant_quotient((unsigned)slot, C.div_mul, C.div_shift)];
-    }
-  }
+  for (int i0 = 0; i0 < N; i0 += 4)
+    if (i0 < units)
 #pragma unroll
-  for (int i = 0; i < N; ++i) {
-    mass[i] = 0.f;
-    pos[i] = 0;
-    if (i < units && page_there(C, page[i])) {
-      const int slot = first + 64 * i + lane, at = slot - invariant_quotient((unsigned)slot, C.div_mul, C.div_shift) * C.page_size;
-      const long long x = page[i] * C.state_page_stride + p.state + at;
-      mass[i] = C.mass[x];
-      pos[i] = C.positions[x];
-    }
-  }
+      for (int i = i0; i < i0 + 4; ++i) {
+        const int slot = min(first + 64 * i + lane, count - 1), q = invariant_quotient((unsigned)slot, C.div_mul, C.div_shift);
+        page[i] = p.table[(unsigned)q];
+        at[i] = slot - q * C.page_size;
+      }
 #pragma unroll
-  for (int i = 0; i < N; ++i) {
-    const bool kept = pos[i] < E.sink || pos[i] >= recent_from;
-    key[i] = page_there(C, page[i]) ? (kept ? KEY_PROTECTED : score_key(mass[i])) : 0u;
+  for (int i0 = 0; i0 < N; i0 += 4)
+    if (i0 < units)
+#pragma unroll
+      for (int i = i0; i < i0 + 4; ++i) {
+        const long long x = (page_there(C, page[i]) ? page[i] : 0) * C.state_page_stride + p.state + at[i];
+        mass[i] = C.mass[x];
+        pos[i] = C.positions[x];
+      }
+#pragma unroll
+  for (int i0 = 0; i0 < N; i0 += 4) {
+#pragma unroll
+    for (int i = i0; i < i0 + 4; ++i) key[i] = 0u;
+    if (i0 < units)
+#pragma unroll
+      for (int i = i0; i < i0 + 4; ++i) {
+        const uint32_t rank = pos[i] < E.sink || pos[i] >= recent ? KEY_PROTECTED : score_key(mass[i]);
+        key[i] = page_there(C, page[i]) && first + 64 * i + lane < count ? rank : 0u;
+      }
   }
 }
 
-__device__ __forceinline__ uint32_t wave_max(uint32_t x) {
-  for (int d = 32; d > 0; d >>= 1) {
-    const uint32_t o = __shfl_xor(x, d);
-    x = o > x ? o : x;
-  }
-  return x;
-}
+__device__ __forceinline__ unsigned long long lanes_below(int n) { return n <= 0 ? 0ull : (n < 64 ? (1ull << n) - 1 : ~0ull); }
 
 // Sum of the waves before this one, and of all.
 template <int WAVES>
 __device__ __forceinline__ int waves_before(const int *per_wave, int wave, int &total) {
-  int before = 0;
-  total = 0;
+  const int upto = wave_scan((int)(threadIdx.x & 63) < WAVES ? per_wave[threadIdx.x & (WAVES - 1)] : 0);
+  total = __builtin_amdgcn_readlane(upto, WAVES - 1);
+  return wave == 0 ? 0 : __builtin_amdgcn_readlane(upto, wave - 1);
+}
+
+// Equals of `last` and larger ones among a wave's keys.
+template <int N>
+__device__ __forceinline__ void count_keys(const uint32_t (&key)[N], int first, int units, int count, uint32_t last, int &equal, int &more) {
+  equal = more = 0;
 #pragma unroll
-  for (int i = 0; i < WAVES; ++i) {
-    const int x = per_wave[i];
-    before += i < wave ? x : 0;
-    total += x;
-  }
-  return before;
+  for (int i = 0; i < N; ++i)
+    if (i < units) {
+      equal += __popcll(__ballot(key[i] == last) & lanes_below(count - first - 64 * i));
+      more += __popcll(__ballot(key[i] > last));
+    }
+}
+
+// The places of a wave's tokens in the lists of their head: `equal` equals and `more` larger ones lie in front of the wave, `ties` equals
+// stay, `left` tokens in all.  -> retained tokens in slots from `left` on.
+template <int N>
+__device__ __forceinline__ int list_keys(const uint32_t (&key)[N], int first, int units, int count, uint32_t last, int equal, int more, int ties, int left,
+                                         int *holes, int *late) {
+  const int lane = threadIdx.x & 63;
+  int before = more + min(equal, ties), moves = 0;
+#pragma unroll
+  for (int i = 0; i < N; ++i)
+    if (i < units) {
+      const int base = first + 64 * i;
+      const unsigned long long in = lanes_below(count - base), low = lanes_below(left - base), eqs = __ballot(key[i] == last) & in;
+      unsigned long long stay = __ballot(key[i] > last);
+      const int n = __popcll(eqs), room = ties - equal;
+      if (n <= room) stay |= eqs;
+      else if (room > 0) stay |= eqs & __ballot((int)__builtin_amdgcn_mbcnt_hi((unsigned)(eqs >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)eqs, 0u)) < room);
+      const int in_front = (int)__builtin_amdgcn_mbcnt_hi((unsigned)(stay >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)stay, (unsigned)before));
+      if (__builtin_amdgcn_inverse_ballot_w64(in & low & ~stay)) holes[base + lane - in_front] = base + lane;
+      if (__builtin_amdgcn_inverse_ballot_w64(stay & ~low)) late[left - 1 - in_front] = base + lane;
+      moves += __popcll(stay & ~low);
+      equal += n;
+      before += __popcll(stay);
+    }
+  return moves;
 }
 
 // The bin of hist[BINS] in which the want-th largest lies, and how many lie in higher ones; by all THREADS.  per_wave and found: LDS.
 template <int BINS, int THREADS>
 __device__ __forceinline__ void find_bin(const int *hist, int want, int *per_wave, int *found) {
-  constexpr int EACH = BINS / THREADS;
+  constexpr int EACH = (BINS + THREADS - 1) / THREADS;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   int mine[EACH], sum = 0;
+  if constexpr (EACH % 4 == 0) {
 #pragma unroll
-  for (int i = 0; i < EACH; ++i) {
-    mine[i] = hist[BINS - 1 - (EACH * tid + i)];
-    sum += mine[i];
+    for (int i = 0; i < EACH; i += 4) {
+      const int4 x = *reinterpret_cast<const int4 *>(hist + BINS - 4 - (EACH * tid + i));
+      mine[i] = x.w;
+      mine[i + 1] = x.z;
+      mine[i + 2] = x.y;
+      mine[i + 3] = x.x;
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < EACH; ++i) mine[i] = EACH * tid + i < BINS ? hist[BINS - 1 - (EACH * tid + i)] : 0;
   }
-  int upto = sum;
-  for (int d = 1; d < 64; d <<= 1) {
-    const int o = __shfl_up(upto, d);
-    if (lane >= d) upto += o;
-  }
+#pragma unroll
+  for (int i = 0; i < EACH; ++i) sum += mine[i];
+  const int upto = wave_scan(sum);
   if (lane == 63) per_wave[wave] = upto;
   __syncthreads();
   int all;
@@ -377,15 +423,20 @@ constexpr int ALONE_SLOTS = ALONE_WAVES * ALONE_UNITS * 64;
 constexpr int ALONE_BINS = 4096, ALONE_CANDS = 256;
 
 struct AloneLds {
-  int hist[ALONE_BINS];
+  alignas(16) int hist[ALONE_BINS];
   int late[ALONE_SLOTS / 2 + 1], holes[ALONE_SLOTS / 2 + 1];
   uint32_t cand[ALONE_CANDS];
-  int wave[4][ALONE_WAVES];
+  int wave[3][ALONE_WAVES];
   uint32_t top[2][ALONE_WAVES];
   int found[3], cands, moves;
   uint32_t key;
   int ties;
 };
+
+__device__ __forceinline__ void clear_hist(int (&hist)[ALONE_BINS]) {
+  reinterpret_cast<int4 *>(hist)[threadIdx.x] = make_int4(0, 0, 0, 0);
+}
+static_assert(ALONE_BINS == 4 * ALONE_THREADS, "one store clears the tally");
 
 // Key of the last token that stays: its bin among 4096 of equal width between the least and the largest key that are neither
 // protected nor 0, so that bins are even whatever the weights' range; then among the few keys of the bin, or 4096 bins within it.
@@ -394,45 +445,40 @@ __global__ __launch_bounds__(ALONE_THREADS) void evict_alone_kernel(const CacheV
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
   const HeadOf w = head_of(C, blockIdx.x);
   const HeadPlace p = head_place(C, w);
-  const int c = held(C, w.b, w.l, w.h);
+  const long long here = count_at(C, w.b, w.l, w.h);
+  const int seen = C.seen[here], c = clamp_to(C.counts[here], C.capacity);        // (leave together, with the budget)
   const long long budget = evict_budget(E, w.b);
   if (c <= budget || c > E.most) return;                   // uniform
   const int left = (int)budget;
-  const long long recent_from = (long long)C.seen[count_at(C, w.b, w.l, w.h)] - E.recent;
   const int units = ((c + 63) / 64 + ALONE_WAVES - 1) / ALONE_WAVES, first = wave * units * 64;       // of every wave
   uint32_t key[ALONE_UNITS];
-  evict_keys(C, p, E, first, units, c, recent_from, key);
+  clear_hist(L.hist);                                      // while the keys come
+  evict_keys(C, p, E, first, units, c, recent_from(E, seen), key);
 
-  int kept = 0, plain = 0;
+  int both = 0;                                            // protected tokens, and 2^16 times plain ones
   uint32_t most = 0, least = 0;                            // least: as ~key
 #pragma unroll
   for (int i = 0; i < ALONE_UNITS; ++i)
     if (i < units) {
-      const bool is_plain = key[i] != 0u && key[i] != KEY_PROTECTED;
-      kept += __popcll(__ballot(key[i] == KEY_PROTECTED));
-      plain += __popcll(__ballot(is_plain));
-      if (is_plain) {
-        most = key[i] > most ? key[i] : most;
-        least = ~key[i] > least ? ~key[i] : least;
-      }
+      const bool plain = key[i] != 0u && key[i] != KEY_PROTECTED;
+      both += plain ? 1 << 16 : (key[i] != 0u ? 1 : 0);
+      most = max(most, plain ? key[i] : 0u);
+      least = max(least, plain ? ~key[i] : 0u);
     }
-  most = wave_max(most);
-  least = wave_max(least);
-  if (lane == 0) {
-    L.wave[0][wave] = kept;
-    L.wave[1][wave] = plain;
+  both = wave_scan(both);
+  most = wave_max_up(most);
+  least = wave_max_up(least);
+  if (lane == 63) {
+    L.wave[0][wave] = both;
     L.top[0][wave] = most;
     L.top[1][wave] = least;
   }
   if (tid == 0) L.moves = 0;
   __syncthreads();
-  waves_before<ALONE_WAVES>(L.wave[0], wave, kept);
-  waves_before<ALONE_WAVES>(L.wave[1], wave, plain);
-#pragma unroll
-  for (int i = 0; i < ALONE_WAVES; ++i) {
-    most = L.top[0][i] > most ? L.top[0][i] : most;
-    least = L.top[1][i] > least ? L.top[1][i] : least;
-  }
+  waves_before<ALONE_WAVES>(L.wave[0], wave, both);
+  const int kept = both & 0xffff, plain = both >> 16;
+  most = __builtin_amdgcn_readlane(wave_max_up(L.top[0][lane & (ALONE_WAVES - 1)]), 63);
+  least = __builtin_amdgcn_readlane(wave_max_up(L.top[1][lane & (ALONE_WAVES - 1)]), 63);
   uint32_t last;                                           // the key of the last one that stays
   int ties;                                                // and how many of its equals stay
   if (left <= kept) {
@@ -444,11 +490,15 @@ __global__ __launch_bounds__(ALONE_THREADS) void evict_alone_kernel(const CacheV
   } else {
     uint32_t lo = ~least, hi = most;
     int want = left - kept;
+    bool again = false;
     for (;;) {
       const int shift = hi - lo < (uint32_t)ALONE_BINS ? 0 : 32 - __builtin_clz((hi - lo) / ALONE_BINS);
-      for (int i = tid; i < ALONE_BINS; i += ALONE_THREADS) L.hist[i] = 0;
       if (tid == 0) L.cands = 0;
-      __syncthreads();
+      if (again) {
+        clear_hist(L.hist);
+        __syncthreads();
+      }
+      again = true;
 #pragma unroll
       for (int i = 0; i < ALONE_UNITS; ++i)
         if (i < units && key[i] >= lo && key[i] <= hi) atomicAdd(&L.hist[(key[i] - lo) >> shift], 1);
@@ -491,44 +541,21 @@ __global__ __launch_bounds__(ALONE_THREADS) void evict_alone_kernel(const CacheV
     }
   }
 
-  int eq = 0, gt = 0;
-#pragma unroll
-  for (int i = 0; i < ALONE_UNITS; ++i)
-    if (i < units) {
-      const bool in = first + 64 * i + lane < c;
-      eq += __popcll(__ballot(in && key[i] == last));
-      gt += __popcll(__ballot(in && key[i] > last));
-    }
-  if (lane == 0) {
-    L.wave[0][wave] = eq;
-    L.wave[1][wave] = gt;
-  }
+  int equal, more, all;
+  count_keys(key, first, units, c, last, equal, more);
+  if (lane == 0) L.wave[1][wave] = equal | more << 16;     // (a wave may still read wave[0])
   __syncthreads();
-  int all, eq_before = waves_before<ALONE_WAVES>(L.wave[0], wave, all);
-  int before = waves_before<ALONE_WAVES>(L.wave[1], wave, all) + min(eq_before, ties);
-#pragma unroll
-  for (int i = 0; i < ALONE_UNITS; ++i)
-    if (i < units) {
-      const int slot = first + 64 * i + lane;
-      const unsigned long long below = (1ull << lane) - 1, eqs = __ballot(slot < c && key[i] == last);
-      const bool stays = slot < c && (key[i] > last || (key[i] == last && eq_before + __popcll(eqs & below) < ties));
-      const unsigned long long ones = __ballot(stays);
-      const int in_front = before + __popcll(ones & below);
-      if (slot < left && !stays) L.holes[slot - in_front] = slot;
-      if (slot >= left && stays) L.late[left - 1 - in_front] = slot;
-      const int late = __popcll(__ballot(slot >= left && stays));
-      if (lane == 0 && late > 0) atomicAdd(&L.moves, late);
-      eq_before += __popcll(eqs);
-      before += __popcll(ones);
-    }
+  const int front = waves_before<ALONE_WAVES>(L.wave[1], wave, all);
+  const int late = list_keys(key, first, units, c, last, front & 0xffff, front >> 16, ties, left, L.holes, L.late);
+  if (lane == 0 && late > 0) atomicAdd(&L.moves, late);
   __syncthreads();
   const int moves = L.moves;
-  if (tid == 0) C.counts[count_at(C, w.b, w.l, w.h)] = left;
+  if (tid == 0) C.counts[here] = left;
   for (int i = tid >> 4; i < moves; i += ALONE_THREADS / 16) move_row(C, p, L.holes[i], L.late[moves - 1 - i], tid & 15);
 }
 
 // ---- a workgroup a part
-constexpr int PART_THREADS = 256, PART_WAVES = PART_THREADS / 64, PART_UNITS = 16;
+constexpr int PART_THREADS = 512, PART_WAVES = PART_THREADS / 64, PART_UNITS = 8;
 constexpr int PART_SLOTS = PART_WAVES * PART_UNITS * 64;
 
 __global__ __launch_bounds__(256) void evict_clear_kernel(int *zero, long long ints) {
@@ -537,7 +564,7 @@ __global__ __launch_bounds__(256) void evict_clear_kernel(int *zero, long long i
 
 struct EvictPart {
   unsigned g, g0;              // head, and first head of its pool
-  int pool, part, count, first;        // tokens of the head, first slot of the part
+  int pool, part, count, seen, first;        // tokens of the head now and ever, first slot of the part
   HeadOf w;
   long long want;
 };
@@ -545,23 +572,30 @@ struct EvictPart {
 __device__ __forceinline__ bool evict_part(const CacheView &C, const EvictPlan &E, EvictPart &P) {
   P.g = blockIdx.x / (unsigned)E.parts;
   P.part = (int)(blockIdx.x - P.g * (unsigned)E.parts);
-  P.pool = (int)(P.g / (unsigned)E.pool_heads);
+  P.pool = E.pool_heads == 1 ? (int)P.g : (int)(P.g / (unsigned)E.pool_heads);
   P.g0 = (unsigned)P.pool * (unsigned)E.pool_heads;
   P.w = head_of(C, P.g);
-  P.count = held(C, P.w.b, P.w.l, P.w.h);
   P.first = P.part * PART_SLOTS;
+  // one round trip for all that is asked
+  const int lane = threadIdx.x & 63;
+  const long long here = count_at(C, P.w.b, P.w.l, P.w.h), layer = count_at(C, P.w.b, P.w.l, 0);
+  P.seen = C.seen[here];
+  const int mine = C.counts[E.pool_heads == 1 ? here : layer + min(lane, E.pool_heads - 1)], own = C.counts[here];
   P.want = evict_budget(E, P.w.b);
+  P.count = clamp_to(own, C.capacity);
   if (P.part > 0 && P.first >= P.count) return false;
   if (E.pool_heads == 1) return P.count > P.want && P.count <= E.most;
-  long long total = 0;
-  bool too_long = false;
-  for (int h = threadIdx.x & 63; h < E.pool_heads; h += 64) {
-    const int c = held(C, P.w.b, P.w.l, h);
-    total += c;
-    too_long |= c > E.most;
+  int c = lane < E.pool_heads ? clamp_to(mine, C.capacity) : 0, longest = c;        // (a pool's sum fits: check_scope)
+  for (int h = lane + 64; h < E.pool_heads; h += 64) {
+    const int x = held(C, P.w.b, P.w.l, h);
+    c += x;
+    longest = max(longest, x);
   }
-  for (int d = 32; d > 0; d >>= 1) total += __shfl_xor(total, d);
-  return total > P.want && !__any(too_long);
+  for (int d = 32; d > 0; d >>= 1) {
+    c += __shfl_xor(c, d);
+    longest = max(longest, __shfl_xor(longest, d));
+  }
+  return c > P.want && longest <= E.most;
 }
 
 // Adds a part's tally to its pool's.
@@ -587,7 +621,8 @@ __global__ __launch_bounds__(PART_THREADS) void evict_keys_kernel(const CacheVie
   for (int i = threadIdx.x; i < 4096; i += PART_THREADS) hist[i] = 0;
   const int first = P.first + (int)(threadIdx.x >> 6) * PART_UNITS * 64, lane = threadIdx.x & 63;
   uint32_t key[PART_UNITS];
-  evict_keys(C, head_place(C, P.w), E, first, PART_UNITS, P.count, (long long)C.seen[count_at(C, P.w.b, P.w.l, P.w.h)] - E.recent, key);
+  // (no units of an empty head)
+  evict_keys(C, head_place(C, P.w), E, first, P.count > 0 ? PART_UNITS : 0, P.count, recent_from(E, P.seen), key);
   __syncthreads();
 #pragma unroll
   for (int i = 0; i < PART_UNITS; ++i) {
@@ -603,14 +638,13 @@ __global__ __launch_bounds__(PART_THREADS) void evict_next_kernel(const CacheVie
   __shared__ int hist[4096], per_wave[PART_WAVES], found[3];
   EvictPart P;
   if (!evict_part(C, E, P) || P.want == 0) return;
-  find_bin<4096, PART_THREADS>(E.hist1 + (long long)P.pool * 4096, (int)P.want, per_wave, found);
-  const int bin = found[0];
-  if (threadIdx.x == 0 && P.g == P.g0 && P.part == 0) E.state1[P.pool] = make_int2(bin, (int)P.want - found[1]);
-  for (int i = threadIdx.x; i < 4096; i += PART_THREADS) hist[i] = 0;
   const int first = P.first + (int)(threadIdx.x >> 6) * PART_UNITS * 64, lane = threadIdx.x & 63;
   uint32_t key[PART_UNITS];
   part_keys(E, P, first, key);
-  __syncthreads();
+  for (int i = threadIdx.x; i < 4096; i += PART_THREADS) hist[i] = 0;
+  find_bin<4096, PART_THREADS>(E.hist1 + (long long)P.pool * 4096, (int)P.want, per_wave, found);
+  const int bin = found[0];
+  if (threadIdx.x == 0 && P.g == P.g0 && P.part == 0) E.state1[P.pool] = make_int2(bin, (int)P.want - found[1]);
 #pragma unroll
   for (int i = 0; i < PART_UNITS; ++i)
     if (first + 64 * i + lane < P.count && (int)(key[i] >> 20) == bin) atomicAdd(&hist[key[i] >> 8 & 4095], 1);
@@ -622,15 +656,14 @@ __global__ __launch_bounds__(PART_THREADS) void evict_last_kernel(const CacheVie
   __shared__ int hist[256], per_wave[PART_WAVES], found[3];
   EvictPart P;
   if (!evict_part(C, E, P) || P.want == 0) return;
-  const int2 one = E.state1[P.pool];
-  find_bin<4096, PART_THREADS>(E.hist2 + (long long)P.pool * 4096, one.y, per_wave, found);
-  const int begins = one.x << 12 | found[0];
-  if (threadIdx.x == 0 && P.g == P.g0 && P.part == 0) E.state2[P.pool] = make_int2(begins, one.y - found[1]);
-  hist[threadIdx.x] = 0;
   const int first = P.first + (int)(threadIdx.x >> 6) * PART_UNITS * 64, lane = threadIdx.x & 63;
   uint32_t key[PART_UNITS];
   part_keys(E, P, first, key);
-  __syncthreads();
+  const int2 one = E.state1[P.pool];
+  if (threadIdx.x < 256) hist[threadIdx.x] = 0;
+  find_bin<4096, PART_THREADS>(E.hist2 + (long long)P.pool * 4096, one.y, per_wave, found);
+  const int begins = one.x << 12 | found[0];
+  if (threadIdx.x == 0 && P.g == P.g0 && P.part == 0) E.state2[P.pool] = make_int2(begins, one.y - found[1]);
   int above = 0;
 #pragma unroll
   for (int i = 0; i < PART_UNITS; ++i) {
@@ -642,22 +675,30 @@ __global__ __launch_bounds__(PART_THREADS) void evict_last_kernel(const CacheVie
   if (lane == 0) per_wave[threadIdx.x >> 6] = above;
   __syncthreads();
   const long long at = (long long)P.g * E.parts + P.part;
-  E.last[at * 256 + threadIdx.x] = hist[threadIdx.x];
-  if (hist[threadIdx.x] != 0) atomicAdd(&E.hist3[(long long)P.pool * 256 + threadIdx.x], hist[threadIdx.x]);
-  if (threadIdx.x == 0) E.above[at] = (per_wave[0] + per_wave[1]) + (per_wave[2] + per_wave[3]);
+  if (threadIdx.x < 256) {
+    E.last[at * 256 + threadIdx.x] = hist[threadIdx.x];
+    if (hist[threadIdx.x] != 0) atomicAdd(&E.hist3[(long long)P.pool * 256 + threadIdx.x], hist[threadIdx.x]);
+  }
+  int all;
+  waves_before<PART_WAVES>(per_wave, 0, all);
+  if (threadIdx.x == 0) E.above[at] = all;
 }
 
-// Sum over the workgroup, to all.
-__device__ __forceinline__ int part_sum(int x, int *per_wave) {
-  for (int d = 32; d > 0; d >>= 1) x += __shfl_xor(x, d);
+// Sums over the workgroup, to all.
+template <int N>
+__device__ __forceinline__ void part_sums(int (&x)[N], int (*per_wave)[PART_WAVES]) {
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const int upto = wave_scan(x[i]);
+    if ((threadIdx.x & 63) == 63) per_wave[i][threadIdx.x >> 6] = upto;
+  }
   __syncthreads();
-  if ((threadIdx.x & 63) == 0) per_wave[threadIdx.x >> 6] = x;
-  __syncthreads();
-  return (per_wave[0] + per_wave[1]) + (per_wave[2] + per_wave[3]);
+#pragma unroll
+  for (int i = 0; i < N; ++i) waves_before<PART_WAVES>(per_wave[i], 0, x[i]);
 }
 
 __global__ __launch_bounds__(PART_THREADS) void evict_list_kernel(const CacheView C, const EvictPlan E) {
-  __shared__ int per_wave[PART_WAVES], found[3], waves[2][PART_WAVES];
+  __shared__ int per_wave[PART_WAVES], found[3], waves[PART_WAVES], sums[5][PART_WAVES];
   EvictPart P;
   if (!evict_part(C, E, P)) return;
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
@@ -665,67 +706,46 @@ __global__ __launch_bounds__(PART_THREADS) void evict_list_kernel(const CacheVie
     if (tid == 0 && P.part == 0) E.left[P.g] = 0;
     return;
   }
+  const int first = P.first + wave * PART_UNITS * 64;
+  uint32_t key[PART_UNITS];
+  part_keys(E, P, first, key);
   const int2 two = E.state2[P.pool];
+  // the head's tallies of the last 8 bits, this thread's digit in every other part, in all of them and in those before this one
+  const int parts = max(1, (int)(((long long)P.count + PART_SLOTS - 1) / PART_SLOTS)), d = tid & 255;
+  int same = 0, same_front = 0, above = 0, above_front = 0;
+#pragma unroll 1
+  for (int q = tid >> 8; q < parts; q += PART_THREADS / 256) {
+    const long long at = (long long)P.g * E.parts + q;
+    const int x = E.last[at * 256 + d], a = d == 0 ? E.above[at] : 0;
+    same += x;
+    above += a;
+    same_front += q < P.part ? x : 0;
+    above_front += q < P.part ? a : 0;
+  }
   find_bin<256, PART_THREADS>(E.hist3 + (long long)P.pool * 256, two.y, per_wave, found);
   const int digit = found[0], ties = two.y - found[1];
   const uint32_t last = (uint32_t)two.x << 8 | (uint32_t)digit;
   // equals in the heads before; equals and larger ones in the head, and in its parts before this one
-  int eq_heads = 0, eq_head = 0, eq_front = 0, gt_head = 0, gt_front = 0;
-  for (long long i = tid; i < (long long)(P.g - P.g0) * E.parts; i += PART_THREADS) {
-    const int h = (int)(i / E.parts), q = (int)(i - (long long)h * E.parts);
-    if (q == 0 || q * (long long)PART_SLOTS < held(C, P.w.b, P.w.l, h)) eq_heads += E.last[((long long)P.g0 * E.parts + i) * 256 + digit];
-  }
-  const int parts = max(1, (P.count + PART_SLOTS - 1) / PART_SLOTS);
-#pragma unroll 4
-  for (int q = 0; q < parts; ++q) {
-    const long long at = (long long)P.g * E.parts + q;
-    const int x = E.last[at * 256 + tid], a = E.above[at], e = tid == digit ? x : 0, m = (tid > digit ? x : 0) + (tid == 0 ? a : 0);
-    eq_head += e;
-    gt_head += m;
-    eq_front += q < P.part ? e : 0;
-    gt_front += q < P.part ? m : 0;
-  }
-  eq_heads = part_sum(eq_heads, per_wave);
-  eq_head = part_sum(eq_head, per_wave);
-  eq_front = part_sum(eq_front, per_wave);
-  gt_head = part_sum(gt_head, per_wave);
-  gt_front = part_sum(gt_front, per_wave);
-  const int mine = min(max(ties - eq_heads, 0), eq_head), left = gt_head + mine;      // equals that stay in the head, its new count
+  enum { EQ_HEADS, EQ_HEAD, EQ_FRONT, GT_HEAD, GT_FRONT };
+  int sum[5] = {0, d == digit ? same : 0, d == digit ? same_front : 0, above + (d > digit ? same : 0), above_front + (d > digit ? same_front : 0)};
+  if (found[2] > ties)                                     // else all equals stay
+    for (long long i = tid; i < (long long)(P.g - P.g0) * E.parts; i += PART_THREADS) {
+      const int h = (int)((unsigned long long)i / (unsigned)E.parts), q = (int)(i - (long long)h * E.parts);
+      if (q == 0 || q * (long long)PART_SLOTS < held(C, P.w.b, P.w.l, h)) sum[EQ_HEADS] += E.last[((long long)P.g0 * E.parts + i) * 256 + digit];
+    }
+  part_sums(sum, sums);
+  const int mine = min(max(ties - sum[EQ_HEADS], 0), sum[EQ_HEAD]), left = sum[GT_HEAD] + mine;      // equals that stay in the head, its new count
   if (tid == 0 && P.part == 0) E.left[P.g] = left;
 
-  const int first = P.first + wave * PART_UNITS * 64;
-  uint32_t key[PART_UNITS];
-  part_keys(E, P, first, key);
-  int eq = 0, gt = 0;
-#pragma unroll
-  for (int i = 0; i < PART_UNITS; ++i) {
-    const bool in = first + 64 * i + lane < P.count;
-    eq += __popcll(__ballot(in && key[i] == last));
-    gt += __popcll(__ballot(in && key[i] > last));
-  }
-  if (lane == 0) {
-    waves[0][wave] = eq;
-    waves[1][wave] = gt;
-  }
+  int equal, more, all;
+  count_keys(key, first, PART_UNITS, P.count, last, equal, more);
+  if (lane == 0) waves[wave] = equal | more << 16;
   __syncthreads();
-  int all, eq_before = eq_front + waves_before<PART_WAVES>(waves[0], wave, all);
-  int before = gt_front + waves_before<PART_WAVES>(waves[1], wave, all) + min(eq_before, mine);
+  const int front = waves_before<PART_WAVES>(waves, wave, all);
   int *list = E.lists + (long long)P.g * E.list;
-  int late_all = 0;
-#pragma unroll
-  for (int i = 0; i < PART_UNITS; ++i) {
-    const int slot = first + 64 * i + lane;
-    const unsigned long long below = (1ull << lane) - 1, eqs = __ballot(slot < P.count && key[i] == last);
-    const bool stays = slot < P.count && (key[i] > last || (key[i] == last && eq_before + __popcll(eqs & below) < mine));
-    const unsigned long long ones = __ballot(stays);
-    const int in_front = before + __popcll(ones & below);
-    if (slot < left && !stays) list[slot - in_front] = slot;
-    if (slot >= left && stays) list[E.list / 2 + left - 1 - in_front] = slot;
-    late_all += __popcll(__ballot(slot >= left && stays));
-    eq_before += __popcll(eqs);
-    before += __popcll(ones);
-  }
-  if (lane == 0 && late_all > 0) atomicAdd(&E.moves[P.g], late_all);
+  const int late = list_keys(key, first, PART_UNITS, P.count, last, sum[EQ_FRONT] + (front & 0xffff), sum[GT_FRONT] + (front >> 16), mine, left, list,
+                             list + E.list / 2);
+  if (lane == 0 && late > 0) atomicAdd(&E.moves[P.g], late);
 }
 
 constexpr int MOVE_THREADS = 256;

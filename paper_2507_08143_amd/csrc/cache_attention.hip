@@ -251,28 +251,6 @@ __device__ __forceinline__ HeadSize head_size(const CacheView &C, const Queries 
   return HeadSize{held(C, w.b, w.l, w.h), tokens_new(Q.new_tokens, w.b, Q.tokens)};
 }
 
-// Sum over the lanes up to this one (row shifts, then the sums of rows and of halves of the wave handed on).
-__device__ __forceinline__ int wave_scan(int x) {
-  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);
-  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);
-  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);
-  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);
-  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);
-  x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);
-  return x;
-}
-
-// The largest of the lanes' numbers >= 0, in lane 63.
-__device__ __forceinline__ int wave_max_up(int x) {
-  x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false));
-  x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false));
-  x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false));
-  x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false));
-  x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false));
-  x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false));
-  return x;
-}
-
 // How long a head is only the device knows, so up to SCAN_HEADS heads every wave finds its workgroup's part by itself, without a
 // barrier: heads are cut into fragments of the same power of two of steps, numbered head after head, at most `target` of them beside
 // the last of each head.  A few rounds of workgroups keep the chip busy to the end whatever the lengths (16 requests of 68
@@ -306,7 +284,7 @@ __device__ __forceinline__ bool scan_part(const CacheView &C, const Queries &Q, 
     }
   }
   const int total = __builtin_amdgcn_readlane(wave_scan(mine), 63);          // the host has seen to it that this fits
-  longest = __builtin_amdgcn_readlane(wave_max_up(longest), 63);
+  longest = (int)__builtin_amdgcn_readlane(wave_max_up((unsigned)longest), 63);
   int log = ATT_LEAST_LOG, per = 0;        // steps of a fragment: 1 << log, or `per` where that is not 0
   while ((total - 1) >> log >= Q.target) ++log;
   // More than 16 query rows make a start dearer, and 64 leave room for one workgroup a unit: twice as much for each where there is enough
