@@ -663,7 +663,7 @@ class Cache:
                                       (t.stride(3) == 1 or page_size == 1) and t.stride() == mass.stride()):
                 _refuse("%s must be %s [page, layer, head, slot] = [%d, %d, %d, %d], slots contiguous, with the "
                         "strides of mass" % (name, dtype, pages, layers, heads, page_size))
-        for name, t in (("counts", counts), ("seen", seen), ("mass", mass), ("positions", positions)):
+        for name, t in (("k_pages", k_pages), ("counts", counts), ("seen", seen), ("mass", mass), ("positions", positions)):
             if t is not None and any(n > 1 and s == 0 for n, s in zip(t.shape, t.stride())):
                 _refuse("%s is written: its elements must not share memory" % name)
         self.device = k_pages.device

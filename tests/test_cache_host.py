@@ -206,7 +206,9 @@ def test_the_handle_checks_its_tensors(B):
                dict(mass=_g(20, 2, 16, 4)), dict(mass=_g(20, 2, 4, 16, dtype=torch.float16)),
                dict(positions=_g(20, 2, 4, 16)), dict(counts=_g(1, 2, 4, dtype=torch.int32).expand(3, 2, 4),
                                                       seen=_g(1, 2, 4, dtype=torch.int32).expand(3, 2, 4)),
-               dict(counts=torch.zeros(3, 2, 4, dtype=torch.int32))):
+               dict(counts=torch.zeros(3, 2, 4, dtype=torch.int32)),
+               dict(k_pages=_g(20, 1, 16, 4, 128, dtype=torch.bfloat16).expand(20, 2, 16, 4, 128),
+                    v_pages=_g(20, 1, 16, 4, 128, dtype=torch.bfloat16).expand(20, 2, 16, 4, 128))):
         with pytest.raises(ValueError):
             _handle(B, **kw)
     with pytest.raises(ValueError):

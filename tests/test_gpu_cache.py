@@ -332,6 +332,112 @@ def test_a_captured_step_is_replayed_as_the_cache_grows(C):
         U.same_pool(a, b.snapshot(), "replay %d" % i)
 
 
+@pytest.mark.parametrize("T,scope", [(1, 0), (5, 1)])
+def test_a_captured_step_over_long_heads(C, T, scope):
+    """The same with heads that several workgroups share, and evictions of several launches: two graphs of one workspace each,
+    replayed in turn with eager work between."""
+    def make():
+        P = U.Paged(C, DEV, _counts(2, 1, 4, 3000, 5000, 17, 4100, 2900), page=32, room=200, seed=6)
+        P.fill_positions()
+        return P
+
+    a, b = make(), make()
+    g = torch.Generator(device=DEV)
+    g.manual_seed(31)
+    k, v = (torch.empty(2, 1, T, 4, 128, dtype=torch.bfloat16, device=DEV) for _ in range(2))
+    q = torch.empty(2, 1, T, 16, 128, dtype=torch.bfloat16, device=DEV)
+    new = torch.tensor([T, 1], dtype=torch.int32, device=DEV)
+    n = max(C.compactor_cache_attention_workspace_size(a.cache, q, accumulate=True),
+            C.compactor_cache_evict_workspace_size(a.cache, scope=1))
+    shared = torch.empty(n, dtype=torch.uint8, device=DEV)
+    budgets = torch.tensor([2600, 2500], dtype=torch.int32, device=DEV)
+
+    def step(P, ws):
+        C.compactor_cache_append(P.cache, k, v, new_tokens=new)
+        return C.compactor_cache_attention(P.cache, q, new_tokens=new, accumulate=True, want_lse=True, workspace=ws)
+
+    def trim(P, ws):
+        C.compactor_cache_evict(P.cache, budgets=budgets, sink=2, recent=8, scope=scope, workspace=ws)
+
+    for t in (k, v, q):
+        t.normal_()
+    warm = make()
+    step(warm, shared), trim(warm, shared)
+    torch.cuda.synchronize()
+    side, first, second = torch.cuda.Stream(), torch.cuda.CUDAGraph(), torch.cuda.CUDAGraph()
+    with torch.cuda.graph(first, stream=side):
+        got = step(a, shared)
+    with torch.cuda.graph(second, stream=side):
+        trim(a, shared)
+    for i in range(6):
+        for t in (k, v, q):
+            t.copy_(torch.randn(t.shape, generator=g, device=DEV))
+        new.copy_(torch.tensor([T, i % 2], dtype=torch.int32))
+        first.replay()
+        want = step(b, None)
+        torch.cuda.synchronize()
+        assert torch.equal(U.bits(got[0]), U.bits(want[0])) and torch.equal(got[1], want[1]), i
+        if i % 2:
+            budgets.sub_(100)
+            second.replay()
+            trim(b, None)
+        U.same_pool(a, b.snapshot(), "replay %d" % i)
+
+
+@pytest.mark.parametrize("pages", [(1 << 17) - 5, 1 << 17, (1 << 17) + 1])
+def test_slots_far_apart(C, pages):
+    """Slot strides around the 2^24 elements up to which a lane's place in a page has 32 bits."""
+    pool = [torch.empty(16, pages, 128, dtype=torch.bfloat16, device=DEV) for _ in range(2)]
+    far = [p.view(16, pages, 1, 1, 128).permute(1, 2, 0, 3, 4) for p in pool]
+    at = torch.tensor([pages - 1, 3, pages // 2, 0], device=DEV)
+    g = torch.Generator(device=DEV)
+    g.manual_seed(2)
+    near = [torch.randn(4, 1, 16, 1, 128, generator=g, device=DEV).to(torch.bfloat16) for _ in range(2)]
+    for f, n in zip(far, near):
+        f[at] = n
+    q = torch.randn(1, 1, 3, 4, 128, generator=g, device=DEV).to(torch.bfloat16)
+    k = torch.randn(1, 1, 3, 1, 128, generator=g, device=DEV).to(torch.bfloat16)
+    made = []
+    for pages_of, table, n in ((far, at, pages), (near, torch.arange(4, device=DEV), 4)):
+        counts, seen = (torch.full((1, 1, 1), 58, dtype=torch.int32, device=DEV) for _ in range(2))
+        mass, pos = torch.zeros(n, 1, 1, 16, device=DEV), torch.zeros(n, 1, 1, 16, dtype=torch.int32, device=DEV)
+        cache = C.Cache(pages_of[0], pages_of[1], table.to(torch.int32).view(1, 4), counts, seen, mass, pos)
+        C.compactor_cache_append(cache, k, k)
+        out, lse = C.compactor_cache_attention(cache, q, want_lse=True)
+        keys, values = (U.f64(p[table].reshape(64, 128)) for p in pages_of)
+        for t, see in enumerate(O.sees(61, 3, 3)):
+            for h in range(4):
+                args = (U.f64(q[0, 0, t, h]), keys, values, see, np.ones(64, bool), 128 ** -0.5, 0.0)
+                want, want_lse, p = O.attend(*args)
+                b_out, b_lse, _ = U.attention_bounds(*args, want, p)
+                assert np.all(np.abs(U.f64(out[0, 0, t, h]) - want) <= b_out) and abs(float(lse[0, 0, t, h]) - want_lse) <= b_lse
+        mass[table] = torch.arange(64, device=DEV, dtype=torch.float32).mul(37).remainder(64).view(4, 1, 1, 16)
+        C.compactor_cache_evict(cache, budget=20)
+        made.append([counts, mass[table], pos[table]] + [U.bits(p[table]) for p in pages_of])
+    assert all(torch.equal(x, y) for x, y in zip(*made)) and int(made[0][0]) == 20
+
+
+def test_contexts_that_share_pages(C):
+    """A common prefix: pages that two contexts name, and one that names a page twice."""
+    P = U.Paged(C, DEV, _counts(3, 1, 2, 150, 130, 160), page=16)
+    P.tables[1, :4] = P.tables[0, :4]
+    P.tables[2, 5] = P.tables[2, 2]
+    _attend(C, P, _queries(P, 1, 8), accumulate=False)
+
+
+@pytest.mark.parametrize("shift", [128, 64])
+def test_keys_and_values_in_one_row(C, shift):
+    """V beside K in a slot, and V a part of K's row."""
+    P = U.Paged(C, DEV, _counts(2, 1, 2, 150, 90, 33), page=16, room=8)
+    row = torch.randn(P.pages, 1, 16, 2, 128 + shift, device=DEV).to(torch.bfloat16)
+    P.k, P.v = row[..., :128], row[..., shift:]
+    P.fill_positions()
+    P.cache = P.handle()
+    _attend(C, P, _queries(P, 1, 8))
+    _check_evict(C, P, [60, 50], 2, 5)
+    _attend(C, P, _queries(P, 1, 8))
+
+
 # ------------------------------------------------------------------------------------------ append
 def _check_append(C, P, T, new=None, what="", stride=1):
     g = torch.Generator(device=DEV)
@@ -554,6 +660,29 @@ def test_admit(C, scope, seeded, page, cut):
     C.compactor_cache_admit(params, reqs, idx, cnt, P.cache, scores=scores if seeded else None)
     torch.cuda.synchronize()
     U.same_pool(P, want, "scope %d" % scope)
+
+
+@pytest.mark.parametrize("scope", [0, 1])
+def test_admit_more_requests_than_a_launch_takes(C, scope):
+    lengths = tuple(40 + 7 * i for i in range(53))
+    ks, vs, params, reqs, so, ko, kk, scores, idx, cnt = _compressed(C, scope, lengths=lengths)
+    L, H, B = 2, 3, len(lengths)
+    most = max(min(n, H * k if scope else k) for n, k in zip(lengths, kk))
+    P = U.Paged(C, DEV, [[[most] * H] * L] * B, page=16)
+    C.compactor_cache_admit(params, reqs, idx, cnt, P.cache, scores=scores)
+    torch.cuda.synchronize()
+    assert torch.equal(P.counts.reshape(-1), cnt) and torch.equal(P.seen[:, 0, 0].cpu(), torch.tensor(lengths, dtype=torch.int32))
+    kept = idx.cpu().numpy()
+    for b in (0, 23, 24, 25, 47, 48, 52):
+        for l in range(L):
+            at = ko[b] + l * H * kk[b]
+            for h in range(H):
+                n = int(cnt[(b * L + l) * H + h])
+                _, _, mass, pos, _ = P.head(b, l, h)
+                assert np.array_equal(pos[:n], kept[at:at + n])
+                first = so[b] + (l * H + h) * lengths[b]
+                assert np.array_equal(mass[:n], scores[first:first + lengths[b]].cpu().numpy()[kept[at:at + n]])
+                at += n
 
 
 @pytest.mark.parametrize("scope", [0, 1])
