@@ -252,6 +252,7 @@ struct EvictPlan {
   int most;                    // tokens of a head that the launches reach
   // parts
   int parts;                   // of a head, at most
+  unsigned parts_mul, parts_shift;        // workgroup / parts
   long long pitch;             // ints from one head's keys to the next
   int list;                    // and its lists: `list / 2` destinations, then as many sources
   int *hist1, *hist2, *hist3;  // [pool][4096], [pool][256]: tallies of the first, the next 12 and the last 8 bits
@@ -570,9 +571,9 @@ struct EvictPart {
 };
 // -> false: nothing to do for this workgroup.  A head's first part is there even if it holds nothing, for its count.
 __device__ __forceinline__ bool evict_part(const CacheView &C, const EvictPlan &E, EvictPart &P) {
-  P.g = blockIdx.x / (unsigned)E.parts;
+  P.g = (unsigned)invariant_quotient(blockIdx.x, E.parts_mul, E.parts_shift);
   P.part = (int)(blockIdx.x - P.g * (unsigned)E.parts);
-  P.pool = E.pool_heads == 1 ? (int)P.g : (int)(P.g / (unsigned)E.pool_heads);
+  P.pool = E.pool_heads == 1 ? (int)P.g : invariant_quotient(P.g, C.layer_mul, C.layer_shift);
   P.g0 = (unsigned)P.pool * (unsigned)E.pool_heads;
   P.w = head_of(C, P.g);
   P.first = P.part * PART_SLOTS;
@@ -591,10 +592,8 @@ __device__ __forceinline__ bool evict_part(const CacheView &C, const EvictPlan &
     c += x;
     longest = max(longest, x);
   }
-  for (int d = 32; d > 0; d >>= 1) {
-    c += __shfl_xor(c, d);
-    longest = max(longest, __shfl_xor(longest, d));
-  }
+  c = __builtin_amdgcn_readlane(wave_scan(c), 63);
+  longest = (int)__builtin_amdgcn_readlane(wave_max_up((unsigned)longest), 63);
   return c > P.want && longest <= E.most;
 }
 
@@ -615,7 +614,7 @@ __global__ __launch_bounds__(PART_THREADS) void evict_keys_kernel(const CacheVie
   __shared__ int hist[4096];
   EvictPart P;
   if (!evict_part(C, E, P)) {
-    if (threadIdx.x == 0 && blockIdx.x % (unsigned)E.parts == 0) E.left[P.g] = -1;
+    if (threadIdx.x == 0 && P.part == 0) E.left[P.g] = -1;
     return;
   }
   for (int i = threadIdx.x; i < 4096; i += PART_THREADS) hist[i] = 0;
@@ -684,17 +683,23 @@ __global__ __launch_bounds__(PART_THREADS) void evict_last_kernel(const CacheVie
   if (threadIdx.x == 0) E.above[at] = all;
 }
 
-// Sums over the workgroup, to all.
+// Sums over the workgroup, to all: every wave adds up the eight waves' of all N at once, eight lanes each.
 template <int N>
 __device__ __forceinline__ void part_sums(int (&x)[N], int (*per_wave)[PART_WAVES]) {
+  static_assert(PART_WAVES == 8 && N <= 8, "eight lanes a sum");
+  const int lane = threadIdx.x & 63;
 #pragma unroll
   for (int i = 0; i < N; ++i) {
     const int upto = wave_scan(x[i]);
-    if ((threadIdx.x & 63) == 63) per_wave[i][threadIdx.x >> 6] = upto;
+    if (lane == 63) per_wave[i][threadIdx.x >> 6] = upto;
   }
   __syncthreads();
+  int all = lane < 8 * N ? per_wave[0][lane] : 0;
+  all += __builtin_amdgcn_update_dpp(0, all, 0xb1, 0xf, 0xf, false);         // the neighbour's, the other pair's, the other four's
+  all += __builtin_amdgcn_update_dpp(0, all, 0x4e, 0xf, 0xf, false);
+  all += __builtin_amdgcn_update_dpp(0, all, 0x141, 0xf, 0xf, false);
 #pragma unroll
-  for (int i = 0; i < N; ++i) waves_before<PART_WAVES>(per_wave[i], 0, x[i]);
+  for (int i = 0; i < N; ++i) x[i] = __builtin_amdgcn_readlane(all, 8 * i);
 }
 
 __global__ __launch_bounds__(PART_THREADS) void evict_list_kernel(const CacheView C, const EvictPlan E) {
@@ -786,6 +791,7 @@ static size_t evict_scratch(const CacheView &C, const compactor_cache_evict_para
   const size_t pools = e->scope == COMPACTOR_SCOPE_LAYER ? heads / C.kv_heads : heads;
   E->most = evict_most(C, e);
   E->parts = (int)(((long long)E->most + PART_SLOTS - 1) / PART_SLOTS);
+  invariant_divisor(E->parts, &E->parts_mul, &E->parts_shift);
   const size_t pitch = (size_t)E->parts * PART_SLOTS;
   E->list = 2 * (E->most / 2 + 1);               // a head moves at most half of its tokens (one into a slot that another left)
   size_t at = 0;
