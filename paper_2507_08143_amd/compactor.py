@@ -683,6 +683,7 @@ class Cache:
                          k_pages.shape[4], counts.data_ptr(), _ptr(seen), counts.stride(0), counts.stride(1),
                          _ptr(mass), _ptr(positions), st[0], st[1], st[2])
         self._ref = C.byref(self._c)
+        self._bytes = {}              # workspace sizes
 
     def layer(self, first: int, count: int = 1) -> "Cache":
         """The cache of `count` layers from `first` on, for calls layer by layer."""
@@ -701,28 +702,32 @@ class Cache:
             _refuse("new_tokens must live on the GPU of the cache")
         return t.data_ptr()
 
-    def _workspace(self, size, what, given, stream):
-        """-> (pointer, bytes), and the tensor that holds them"""
+    def _workspace(self, size, what, key, given, stream):
+        """-> (pointer, bytes), and the tensor that holds them.  key: what the size depends on beside the cache's own sizes."""
         if given is not None:
             _out(given, 0, torch.uint8, "workspace")
             if given.device != self.device:
                 _refuse("the workspace must live on the GPU of the cache")
             return given.data_ptr(), given.numel(), given
-        out = C.c_size_t(0)
-        _check(size(self._ref, what, C.byref(out)))
-        if out.value == 0:
+        need = self._bytes.get(key)
+        if need is None:
+            out = C.c_size_t(0)
+            _check(size(self._ref, what, C.byref(out)))
+            need = self._bytes[key] = out.value
+        if need == 0:
             return 0, 0, None
-        given = torch.empty(out.value, dtype=torch.uint8, device=self.device)
+        given = torch.empty(need, dtype=torch.uint8, device=self.device)
         if stream is not None:
             given.record_stream(stream)      # used on `stream`, see _workspace()
-        return given.data_ptr(), out.value, given
+        return given.data_ptr(), need, given
 
     def _on(self, stream, call):
         """call(stream handle) with the cache's GPU current."""
         if stream is not None and stream.device != self.device:
             _refuse("the stream belongs to another GPU than the cache")
-        if torch.cuda.current_device() == self.device.index:
-            _check(call(_stream(stream)))
+        here = torch.cuda.current_device()
+        if here == self.device.index:
+            _check(call(_stream(stream) if stream is not None or _raw_stream is None else _raw_stream(here)))
         else:
             with torch.cuda.device(self.device):
                 _check(call(_stream(stream)))
@@ -831,7 +836,8 @@ def compactor_cache_attention(cache: Cache, q: torch.Tensor, new_tokens: Optiona
             lse.record_stream(stream)
     query.lse = _ptr(lse)
     ref = C.byref(query)
-    ptr, nbytes, _keep = cache._workspace(_lib.compactor_cache_attention_workspace_size, ref, workspace, stream)
+    ptr, nbytes, _keep = cache._workspace(_lib.compactor_cache_attention_workspace_size, ref,
+                                        (shape[2], shape[3], accumulate, max_tokens), workspace, stream)
     cache._on(stream, lambda st: _lib.compactor_cache_attention(cache._ref, ref, ptr, nbytes, st))
     return out, lse
 
@@ -862,5 +868,5 @@ def compactor_cache_evict(cache: Cache, budget: Optional[int] = None, budgets: O
     """Brings every head (SCOPE_LAYER: the heads of every layer together) down to its budget: `budget`
     tokens, or budgets[request] of an int32 device tensor."""
     ref = C.byref(_cache_evict(cache, budget, budgets, sink, recent, scope, max_tokens))
-    ptr, nbytes, _keep = cache._workspace(_lib.compactor_cache_evict_workspace_size, ref, workspace, stream)
+    ptr, nbytes, _keep = cache._workspace(_lib.compactor_cache_evict_workspace_size, ref, (scope, max_tokens), workspace, stream)
     cache._on(stream, lambda st: _lib.compactor_cache_evict(cache._ref, ref, ptr, nbytes, st))
