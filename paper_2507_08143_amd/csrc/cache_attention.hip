@@ -224,7 +224,7 @@ __device__ __forceinline__ void mass_add(const Queries &Q, const float *lse2, co
 #pragma unroll
   for (int r = 0; r < MASS_ROWS; ++r)
     if (r < R) row(r, M.x[r]);
-#pragma unroll 4
+#pragma unroll 8
   for (int r = MASS_ROWS; r < R; ++r) row(r, *reinterpret_cast<const f32x4 *>(logits + (long long)r * Q.pitch + s));
 #pragma unroll
   for (int i = 0; i < 4; ++i)
@@ -661,15 +661,16 @@ __global__ __launch_bounds__(256, NT <= 2 ? 2 : 1) void attend_kernel(const Cach
 // Second launch: the fragments of a head meet.  The first heads * R workgroups take a query row each, 16 fragments side by side
 // and 8 channels a thread; the others add a fragment's weights to the mass.
 
+__device__ __forceinline__ void add_stats(float &m, float &l, const float2 &x) {
+  const float to = fmaxf(m, x.x);
+  l = to == -INFINITY ? 0.f : l * exp2_(m - to) + x.y * exp2_(x.x - to);
+  m = to;
+}
+
 // Maximum and sum of row r over the fragments, by the lanes of a wave.
 __device__ __forceinline__ float2 join_stats(const Queries &Q, int first, int parts, int R, int r) {
   float m = -INFINITY, l = 0.f;
-  for (int k = threadIdx.x & 63; k < parts; k += 64) {
-    const float2 x = Q.stats[(long long)(first + k) * R + r];
-    const float to = fmaxf(m, x.x);
-    l = to == -INFINITY ? 0.f : l * exp2_(m - to) + x.y * exp2_(x.x - to);
-    m = to;
-  }
+  for (int k = threadIdx.x & 63; k < parts; k += 64) add_stats(m, l, Q.stats[(long long)(first + k) * R + r]);
   float top = m;
   for (int d = 32; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
   float sum = top == -INFINITY ? 0.f : l * exp2_(m - top);
@@ -679,6 +680,7 @@ __device__ __forceinline__ float2 join_stats(const Queries &Q, int first, int pa
 
 __global__ __launch_bounds__(256) void attend_join_kernel(const CacheView C, const Queries Q) {
   __shared__ float part_o[16][D + 4], lse2[MOST_ROWS];
+  __shared__ float2 stats[256];                     // of the groups of more than 16 rows
   const int tid = threadIdx.x, R = Q.tokens * Q.group;
   const unsigned rows = (unsigned)C.nreq * (unsigned)C.layers * (unsigned)C.kv_heads * (unsigned)R;
   if (blockIdx.x < rows) {
@@ -718,9 +720,26 @@ __global__ __launch_bounds__(256) void attend_join_kernel(const CacheView C, con
   if (from >= to) return;
   MassQuad M;
   mass_fetch(C, Q, hp, logits, R, min(from + 4 * tid, (to - 1) & ~3), to, M);
-  for (int r = tid >> 6; r < R; r += 4) {          // every wave takes rows in turn
-    const float2 all = join_stats(Q, f.first, f.parts, R, r);
-    if ((tid & 63) == 0) lse2[r] = all.y == 0.f ? INFINITY : all.x + __builtin_amdgcn_logf(all.y);
+  // The rows' sums.  Up to 16 rows the waves take rows in turn, their lanes fragments (4 rows, 2.3 M slots: 248 us a call, in the other way 250);
+  // more of them all at once: thread (group, row) takes every groups-th fragment, the first R threads add up the groups' (28 rows,
+  // 72 heads of up to 3618: 56 us a call, in the first way 60).
+  if (R <= 16) {
+    for (int r = tid >> 6; r < R; r += 4) {
+      const float2 all = join_stats(Q, f.first, f.parts, R, r);
+      if ((tid & 63) == 0) lse2[r] = all.y == 0.f ? INFINITY : all.x + __builtin_amdgcn_logf(all.y);
+    }
+  } else {
+    const int groups = (int)(256u / (unsigned)R), group = (int)((unsigned)tid / (unsigned)R), r = tid - group * R;
+    float m = -INFINITY, l = 0.f;
+    if (group < groups)
+      for (int k = group; k < f.parts; k += groups) add_stats(m, l, Q.stats[(long long)(f.first + k) * R + r]);
+    stats[tid] = make_float2(m, l);
+    __syncthreads();
+    if (tid < R) {
+#pragma unroll 4
+      for (int i = 1; i < min(groups, f.parts); ++i) add_stats(m, l, stats[i * R + tid]);
+      lse2[tid] = l == 0.f ? INFINITY : m + __builtin_amdgcn_logf(l);
+    }
   }
   __syncthreads();
   for (int at = from + 4 * tid; at < to; at += 4 * 256) {
