@@ -741,20 +741,22 @@ def compactor_cache_admit(params: Params, reqs: Sequence[Request], kept_idx: tor
     n = len(reqs)
     _require(n >= 1, "at least one request is needed")
     arr = (_Request * n)()                     # n and ratio are all that is looked at
-    for i, r in enumerate(reqs):
-        L, H, arr[i].n, _d = r.k_score.shape
-        if L != params.layers or H != params.kv_heads:
+    layers, heads = params.layers, params.kv_heads
+    for r, a in zip(reqs, arr):
+        L, H, a.n, _d = r.k_score.shape
+        if L != layers or H != heads:
             _refuse("k_score has shape %s, the parameters say [%d, %d, n, %d]"
                     % (tuple(r.k_score.shape), params.layers, params.kv_heads, params.head_dim))
-        arr[i].ratio = r.ratio
+        a.ratio = r.ratio
     pp = C.byref(params.c(False))
-    so, ko, _ = _layout(pp, arr, n)
+    so, ko, kk = (C.c_int64 * (n + 1))(), (C.c_int64 * (n + 1))(), (C.c_int32 * n)()
+    _check(_lib.compactor_layout(pp, arr, n, so, ko, kk))
     if (n, params.layers, params.kv_heads) != (cache.nreq, cache.layers, cache.kv_heads):
         _refuse("the cache is of [%d, %d, %d] requests, layers and heads, the call of [%d, %d, %d]"
                 % (cache.nreq, cache.layers, cache.kv_heads, n, params.layers, params.kv_heads))
-    for t, numel, dtype, name in ((kept_idx, ko[-1], torch.int32, "kept_idx"),
+    for t, numel, dtype, name in ((kept_idx, ko[n], torch.int32, "kept_idx"),
                                   (kept_cnt, n * params.layers * params.kv_heads, torch.int32, "kept_cnt"),
-                                  (scores, so[-1], torch.float32, "scores")):
+                                  (scores, so[n], torch.float32, "scores")):
         _out(t, numel, dtype, name)
         if t is not None and t.device != cache.device:
             _refuse("%s must live on the GPU of the cache" % name)
