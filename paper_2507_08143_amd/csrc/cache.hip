@@ -236,13 +236,16 @@ hipError_t launch_cache_admit(const SegTable &T, const CacheView &C, const int32
 // tokens in front of a slot: slot s is hole number s - before, and the retained token in slot s >= left has left - 1 - before
 // others behind it.  Sources and destinations of a head are disjoint, so the moves need no order.
 //
-// One workgroup does everything where a pool is a head of up to ALONE_SLOTS tokens; its keys stay in registers.  Longer heads and
-// layers would keep one unit busy too long (some 70 instructions a slot: 32 layers of 79000 tokens 327 us), so there the pool is cut into parts of
-// PART_SLOTS slots and every part's workgroup does the same steps in a launch each: keys and the tally of their first 12 bits,
-// the next 12, the last 8, the lists, the moves.  What bounds both is not the 8 bytes of state a slot but the chain of steps, and the instructions
-// of each, which are fetched as they are run for the first time (lists of 10 units a wave: 5.1 us, run a second time 2.9).  Workgroups of 8
-// waves with 8 units each: 8 heads of 26215 tokens 36 us, 32 layers of 79000 tokens 57; 4 with 16 41 and 60, 16 with 4 35 and 71.
-constexpr uint32_t KEY_PROTECTED = 0xffffffffu;      // above the key of +inf (0xff800000); 0: NaN, or a page that is not there
+// One workgroup does everything where a pool has up to 256 units of 64 slots (a head of 16384 tokens, 8 heads of 2048); its keys stay in
+// registers.  More would keep one compute unit busy too long, so there the pool is cut into parts of PART_SLOTS slots and every part's
+// workgroup does the same steps in a launch each: keys and the tally of their first 12 bits, the next 12, the last 8, the lists,
+// the moves (us with the append in front, one workgroup / parts: one layer of 8 heads of 1700 tokens 26 / 33, 512 such layers 66 / 151).
+// What bounds both is not the 8 bytes of state a slot but the chain of steps and the instructions of each: a compute unit issues
+// one scalar instruction a cycle, and one vector instruction, for all its waves, and fetches what it runs for the first time (lists of 10 units a
+// wave: 5.1 us, run a second time 2.9).  Parts of 8 waves with 8 units each: 8 heads of 26215
+// tokens 36 us, 32 layers of 79000 tokens 57; 4 with 16 41 and 60, 16 with 4 35 and 71.
+constexpr uint32_t KEY_PROTECTED = 0xffffffffu;      // above the key of +inf (0xff800000)
+constexpr uint32_t KEY_NO_NUMBER = 1u;               // NaN, or a page that is not there; below the key of -inf (0x007fffff).  0: no token
 
 struct EvictPlan {
   int budget;
@@ -311,12 +314,10 @@ __device__ __forceinline__ void evict_keys(const CacheView &C, const HeadPlace &
 #pragma unroll
       for (int i = i0; i < i0 + 4; ++i) {
         const uint32_t rank = pos[i] < E.sink || pos[i] >= recent ? KEY_PROTECTED : score_key(mass[i]);
-        key[i] = page_there(C, page[i]) && first + 64 * i + lane < count ? rank : 0u;
+        key[i] = first + 64 * i + lane < count ? max(page_there(C, page[i]) ? rank : 0u, KEY_NO_NUMBER) : 0u;
       }
   }
 }
-
-__device__ __forceinline__ unsigned long long lanes_below(int n) { return n <= 0 ? 0ull : (n < 64 ? (1ull << n) - 1 : ~0ull); }
 
 // Sum of the waves before this one, and of all.
 template <int WAVES>
@@ -326,38 +327,57 @@ __device__ __forceinline__ int waves_before(const int *per_wave, int wave, int &
   return wave == 0 ? 0 : __builtin_amdgcn_readlane(upto, wave - 1);
 }
 
-// Equals of `last` and larger ones among a wave's keys.
+// Equals of `last` and larger ones among a wave's keys.  (last is some token's key, so never 0.)
 template <int N>
-__device__ __forceinline__ void count_keys(const uint32_t (&key)[N], int first, int units, int count, uint32_t last, int &equal, int &more) {
+__device__ __forceinline__ void count_keys(const uint32_t (&key)[N], int units, uint32_t last, int &equal, int &more) {
   equal = more = 0;
 #pragma unroll
   for (int i = 0; i < N; ++i)
     if (i < units) {
-      equal += __popcll(__ballot(key[i] == last) & lanes_below(count - first - 64 * i));
+      equal += __popcll(__ballot(key[i] == last));
       more += __popcll(__ballot(key[i] > last));
     }
 }
 
-// The places of a wave's tokens in the lists of their head: `equal` equals and `more` larger ones lie in front of the wave, `ties` equals
-// stay, `left` tokens in all.  -> retained tokens in slots from `left` on.
+__device__ __forceinline__ int lanes_before(unsigned long long mask, int start) {       // start + ones below the lane
+  return (int)__builtin_amdgcn_mbcnt_hi((unsigned)(mask >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)mask, (unsigned)start));
+}
+
+// Which lanes' tokens stay, where `room` more equals may.
+__device__ __forceinline__ unsigned long long who_stays(uint32_t key, uint32_t last, int room, int &equals) {
+  const unsigned long long eqs = __ballot(key == last);
+  unsigned long long stay = __ballot(key > last);
+  equals = __popcll(eqs);
+  if (equals <= room) stay |= eqs;
+  else if (room > 0) stay |= eqs & __ballot(lanes_before(eqs, 0) < room);
+  return stay;
+}
+
+// The places of a unit's tokens in the lists of their head: `before` of those that stay lie in front of it, `left` stay in all.  -> retained
+// tokens in slots from `left` on.  (Scalar instructions count: a compute unit issues one a cycle for all its waves.)
+__device__ __forceinline__ int list_unit(unsigned long long stay, int base, int before, int left, int *holes, int *late) {
+  const int slot = base + (int)(threadIdx.x & 63), in_front = lanes_before(stay, before);
+  if (base + 64 <= left) {
+    if (__builtin_amdgcn_inverse_ballot_w64(~stay)) holes[slot - in_front] = slot;
+    return 0;
+  }
+  const unsigned long long low = base < left ? (1ull << (left - base)) - 1 : 0ull;
+  if (__builtin_amdgcn_inverse_ballot_w64(low & ~stay)) holes[slot - in_front] = slot;
+  if (__builtin_amdgcn_inverse_ballot_w64(stay & ~low)) late[left - 1 - in_front] = slot;
+  return __popcll(stay & ~low);
+}
+
+// A wave's units: `equal` equals and `more` larger ones lie in front of the wave, `ties` equals stay.
 template <int N>
-__device__ __forceinline__ int list_keys(const uint32_t (&key)[N], int first, int units, int count, uint32_t last, int equal, int more, int ties, int left,
-                                         int *holes, int *late) {
-  const int lane = threadIdx.x & 63;
+__device__ __forceinline__ int list_keys(const uint32_t (&key)[N], int first, int units, uint32_t last, int equal, int more, int ties, int left, int *holes,
+                                         int *late) {
   int before = more + min(equal, ties), moves = 0;
 #pragma unroll
   for (int i = 0; i < N; ++i)
     if (i < units) {
-      const int base = first + 64 * i;
-      const unsigned long long in = lanes_below(count - base), low = lanes_below(left - base), eqs = __ballot(key[i] == last) & in;
-      unsigned long long stay = __ballot(key[i] > last);
-      const int n = __popcll(eqs), room = ties - equal;
-      if (n <= room) stay |= eqs;
-      else if (room > 0) stay |= eqs & __ballot((int)__builtin_amdgcn_mbcnt_hi((unsigned)(eqs >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)eqs, 0u)) < room);
-      const int in_front = (int)__builtin_amdgcn_mbcnt_hi((unsigned)(stay >> 32), __builtin_amdgcn_mbcnt_lo((unsigned)stay, (unsigned)before));
-      if (__builtin_amdgcn_inverse_ballot_w64(in & low & ~stay)) holes[base + lane - in_front] = base + lane;
-      if (__builtin_amdgcn_inverse_ballot_w64(stay & ~low)) late[left - 1 - in_front] = base + lane;
-      moves += __popcll(stay & ~low);
+      int n;
+      const unsigned long long stay = who_stays(key[i], last, ties - equal, n);
+      moves += list_unit(stay, first + 64 * i, before, left, holes, late);
       equal += n;
       before += __popcll(stay);
     }
@@ -441,28 +461,16 @@ static_assert(ALONE_BINS == 4 * ALONE_THREADS, "one store clears the tally");
 
 // Key of the last token that stays: its bin among 4096 of equal width between the least and the largest key that are neither
 // protected nor 0, so that bins are even whatever the weights' range; then among the few keys of the bin, or 4096 bins within it.
-__global__ __launch_bounds__(ALONE_THREADS) void evict_alone_kernel(const CacheView C, const EvictPlan E) {
-  __shared__ AloneLds L;
+// units of the wave hold keys, `left` tokens stay; L.hist is clear.  -> key of the last one that stays, and how many of its equals stay
+__device__ __forceinline__ void find_last(AloneLds &L, const uint32_t (&key)[ALONE_UNITS], int units, int left, uint32_t &last, int &ties) {
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
-  const HeadOf w = head_of(C, blockIdx.x);
-  const HeadPlace p = head_place(C, w);
-  const long long here = count_at(C, w.b, w.l, w.h);
-  const int seen = C.seen[here], c = clamp_to(C.counts[here], C.capacity);        // (leave together, with the budget)
-  const long long budget = evict_budget(E, w.b);
-  if (c <= budget || c > E.most) return;                   // uniform
-  const int left = (int)budget;
-  const int units = ((c + 63) / 64 + ALONE_WAVES - 1) / ALONE_WAVES, first = wave * units * 64;       // of every wave
-  uint32_t key[ALONE_UNITS];
-  clear_hist(L.hist);                                      // while the keys come
-  evict_keys(C, p, E, first, units, c, recent_from(E, seen), key);
-
   int both = 0;                                            // protected tokens, and 2^16 times plain ones
   uint32_t most = 0, least = 0;                            // least: as ~key
 #pragma unroll
   for (int i = 0; i < ALONE_UNITS; ++i)
     if (i < units) {
-      const bool plain = key[i] != 0u && key[i] != KEY_PROTECTED;
-      both += plain ? 1 << 16 : (key[i] != 0u ? 1 : 0);
+      const bool plain = key[i] > KEY_NO_NUMBER && key[i] != KEY_PROTECTED;
+      both += plain ? 1 << 16 : (key[i] == KEY_PROTECTED ? 1 : 0);
       most = max(most, plain ? key[i] : 0u);
       least = max(least, plain ? ~key[i] : 0u);
     }
@@ -480,13 +488,11 @@ __global__ __launch_bounds__(ALONE_THREADS) void evict_alone_kernel(const CacheV
   const int kept = both & 0xffff, plain = both >> 16;
   most = __builtin_amdgcn_readlane(wave_max_up(L.top[0][lane & (ALONE_WAVES - 1)]), 63);
   least = __builtin_amdgcn_readlane(wave_max_up(L.top[1][lane & (ALONE_WAVES - 1)]), 63);
-  uint32_t last;                                           // the key of the last one that stays
-  int ties;                                                // and how many of its equals stay
   if (left <= kept) {
     last = KEY_PROTECTED;
     ties = left;
   } else if (left - kept > plain) {
-    last = 0u;
+    last = KEY_NO_NUMBER;
     ties = left - kept - plain;
   } else {
     uint32_t lo = ~least, hi = most;
@@ -542,17 +548,171 @@ __global__ __launch_bounds__(ALONE_THREADS) void evict_alone_kernel(const CacheV
     }
   }
 
+}
+
+__global__ __launch_bounds__(ALONE_THREADS) void evict_alone_kernel(const CacheView C, const EvictPlan E) {
+  __shared__ AloneLds L;
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
+  const HeadOf w = head_of(C, blockIdx.x);
+  const HeadPlace p = head_place(C, w);
+  const long long here = count_at(C, w.b, w.l, w.h);
+  const int seen = C.seen[here], c = clamp_to(C.counts[here], C.capacity);        // (leave together, with the budget)
+  const long long budget = evict_budget(E, w.b);
+  if (c <= budget || c > E.most) return;                   // uniform
+  const int left = (int)budget;
+  const int units = ((c + 63) / 64 + ALONE_WAVES - 1) / ALONE_WAVES, first = wave * units * 64;       // of every wave
+  uint32_t key[ALONE_UNITS];
+  clear_hist(L.hist);                                      // while the keys come
+  evict_keys(C, p, E, first, units, c, recent_from(E, seen), key);
+
+  uint32_t last;
+  int ties;
+  find_last(L, key, units, left, last, ties);
   int equal, more, all;
-  count_keys(key, first, units, c, last, equal, more);
+  count_keys(key, units, last, equal, more);
   if (lane == 0) L.wave[1][wave] = equal | more << 16;     // (a wave may still read wave[0])
   __syncthreads();
   const int front = waves_before<ALONE_WAVES>(L.wave[1], wave, all);
-  const int late = list_keys(key, first, units, c, last, front & 0xffff, front >> 16, ties, left, L.holes, L.late);
+  const int late = list_keys(key, first, units, last, front & 0xffff, front >> 16, ties, left, L.holes, L.late);
   if (lane == 0 && late > 0) atomicAdd(&L.moves, late);
   __syncthreads();
   const int moves = L.moves;
   if (tid == 0) C.counts[here] = left;
   for (int i = tid >> 4; i < moves; i += ALONE_THREADS / 16) move_row(C, p, L.holes[i], L.late[moves - 1 - i], tid & 15);
+}
+
+// The same for the heads of a layer that share a budget: units of 64 slots, head after head, in equal numbers to the waves.
+constexpr int POOL_UNITS = ALONE_WAVES * ALONE_UNITS;
+struct PoolLds {
+  AloneLds a;
+  alignas(16) int before[POOL_UNITS + 4];                  // retained tokens of a unit; then, of all units before it
+  int start[POOL_UNITS + 1], count[POOL_UNITS], seen[POOL_UNITS];        // of a head: its first unit, tokens now and ever
+  int moves[POOL_UNITS], first_move[POOL_UNITS + 1];
+};
+
+__global__ __launch_bounds__(ALONE_THREADS) void evict_pool_kernel(const CacheView C, const EvictPlan E) {
+  __shared__ PoolLds L;
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, H = C.kv_heads;
+  const HeadOf w0 = head_of(C, blockIdx.x * (unsigned)H);
+  const long long budget = evict_budget(E, w0.b);
+  int total = 0, longest = 0, units_all = 0;               // (every wave for itself)
+  for (int h0 = 0; h0 < H; h0 += 64) {
+    const int h = min(h0 + lane, H - 1);
+    const long long at = count_at(C, w0.b, w0.l, h);
+    const int seen = C.seen[at], c = h0 + lane < H ? clamp_to(C.counts[at], C.capacity) : 0;
+    const int mine = (int)(((unsigned)c + 63) / 64), upto = units_all + wave_scan(min(mine, POOL_UNITS));
+    total += __builtin_amdgcn_readlane(wave_scan(c), 63);
+    longest = max(longest, (int)__builtin_amdgcn_readlane(wave_max_up((unsigned)c), 63));
+    if (wave == 0 && h0 + lane < H) {
+      L.start[h] = upto - mine;
+      L.count[h] = c;
+      L.seen[h] = seen;
+      L.moves[h] = 0;
+    }
+    units_all = __builtin_amdgcn_readlane(upto, 63);
+  }
+  if (total <= budget || longest > E.most) return;         // uniform; from here on the units fit (the host has seen to it)
+  if (tid == 0) L.start[H] = units_all;
+  clear_hist(L.a.hist);
+  __syncthreads();
+  const int units = (units_all + ALONE_WAVES - 1) / ALONE_WAVES, unit0 = wave * units;
+  // lane i: unit i of the wave
+  const int mine = unit0 + lane;
+  int head = 0;
+  for (int h = 1; h < H; ++h) head += L.start[h] <= mine;
+  const bool there = lane < units && mine < units_all;
+  const int unit_count = there ? L.count[head] : 0, unit_base = there ? 64 * (mine - L.start[head]) : 0, unit_recent = recent_from(E, L.seen[head]);
+  auto base = [&](int i) { return (int)__builtin_amdgcn_readlane(unit_base, i); };
+  auto count = [&](int i) { return (int)__builtin_amdgcn_readlane(unit_count, i); };
+  auto head_at = [&](int i) { return (int)__builtin_amdgcn_readlane(head, i); };
+
+  uint32_t key[ALONE_UNITS];
+  {
+    const HeadPlace p = head_place(C, w0);
+    int page[ALONE_UNITS], at[ALONE_UNITS], pos[ALONE_UNITS];
+    float mass[ALONE_UNITS];
+#pragma unroll
+    for (int i = 0; i < ALONE_UNITS; ++i)
+      if (i < units) {
+        const int slot = max(min(base(i) + lane, count(i) - 1), 0), q = invariant_quotient((unsigned)slot, C.div_mul, C.div_shift);
+        page[i] = p.table[(unsigned)q];
+        at[i] = slot - q * C.page_size;
+      }
+#pragma unroll
+    for (int i = 0; i < ALONE_UNITS; ++i)
+      if (i < units) {
+        const long long x = (page_there(C, page[i]) ? page[i] : 0) * C.state_page_stride + p.state + head_at(i) * C.state_head_stride + at[i];
+        mass[i] = C.mass[x];
+        pos[i] = C.positions[x];
+      }
+#pragma unroll
+    for (int i = 0; i < ALONE_UNITS; ++i) {
+      key[i] = 0u;
+      if (i < units) {
+        const uint32_t rank = pos[i] < E.sink || pos[i] >= (int)__builtin_amdgcn_readlane(unit_recent, i) ? KEY_PROTECTED : score_key(mass[i]);
+        key[i] = base(i) + lane < count(i) ? max(page_there(C, page[i]) ? rank : 0u, KEY_NO_NUMBER) : 0u;
+      }
+    }
+  }
+  uint32_t last;
+  int ties;
+  find_last(L.a, key, units, (int)budget, last, ties);
+
+  // equals in front, over all heads; then which slots of a unit stay
+  int equal, more, all;
+  count_keys(key, units, last, equal, more);
+  if (lane == 0) L.a.wave[1][wave] = equal;
+  __syncthreads();
+  equal = waves_before<ALONE_WAVES>(L.a.wave[1], wave, all);
+  unsigned long long unit_stay = 0ull;                     // lane i: of unit i
+#pragma unroll
+  for (int i = 0; i < ALONE_UNITS; ++i)
+    if (i < units) {
+      int n;
+      const unsigned long long stay = who_stays(key[i], last, ties - equal, n);
+      equal += n;
+      if (lane == i) unit_stay = stay;
+    }
+  if (lane < units) L.before[mine] = __popcll(unit_stay);
+  for (int u = units * ALONE_WAVES + tid; u < POOL_UNITS; u += ALONE_THREADS) L.before[u] = 0;
+  __syncthreads();
+  if (wave == 0) {                                         // sums over the units before each
+    int4 x = *reinterpret_cast<const int4 *>(&L.before[4 * lane]);
+    const int four = x.x + x.y + x.z + x.w, upto = wave_scan(four), b = upto - four;
+    *reinterpret_cast<int4 *>(&L.before[4 * lane]) = make_int4(b, b + x.x, b + x.x + x.y, b + x.x + x.y + x.z);
+    if (lane == 63) L.before[POOL_UNITS] = upto;
+  }
+  __syncthreads();
+  // A head's lists have half as many places as its units have slots: it moves at most half of its tokens.  Lane i again has unit i of the wave.
+  const int first_unit = L.start[head], front = L.before[first_unit], unit_left = L.before[L.start[head + 1]] - front;
+  const int unit_front = L.before[min(mine, POOL_UNITS - 1)] - front;
+#pragma unroll 1
+  for (int i = 0; i < units; ++i) {
+    const unsigned lo = __builtin_amdgcn_readlane((unsigned)unit_stay, i), hi = __builtin_amdgcn_readlane((unsigned)(unit_stay >> 32), i);
+    const int list = 32 * __builtin_amdgcn_readlane(first_unit, i);
+    if (unit0 + i >= units_all) break;
+    const int late = list_unit((unsigned long long)hi << 32 | lo, base(i), __builtin_amdgcn_readlane(unit_front, i), __builtin_amdgcn_readlane(unit_left, i),
+                               L.a.holes + list, L.a.late + list);
+    if (lane == 0 && late > 0) atomicAdd(&L.moves[head_at(i)], late);
+  }
+  __syncthreads();
+  int moves = 0;
+  for (int h0 = 0; h0 < H; h0 += 64) {
+    const int h = h0 + lane, n = h < H ? L.moves[h] : 0, upto = moves + wave_scan(n);
+    if (wave == 0 && h < H) {
+      L.first_move[h] = upto - n;
+      C.counts[count_at(C, w0.b, w0.l, h)] = L.before[L.start[h + 1]] - L.before[L.start[h]];
+    }
+    moves = __builtin_amdgcn_readlane(upto, 63);
+  }
+  if (tid == 0) L.first_move[H] = moves;
+  __syncthreads();
+  int h = 0;
+  for (int i = tid >> 4; i < moves; i += ALONE_THREADS / 16) {
+    while (L.first_move[h + 1] <= i) ++h;                  // (first_move[H] > i)
+    const int k = i - L.first_move[h], list = 32 * L.start[h];
+    move_row(C, head_place(C, HeadOf{w0.b, w0.l, h}), L.a.holes[list + k], L.a.late[list + L.moves[h] - 1 - k], tid & 15);
+  }
 }
 
 // ---- a workgroup a part
@@ -743,12 +903,12 @@ __global__ __launch_bounds__(PART_THREADS) void evict_list_kernel(const CacheVie
   if (tid == 0 && P.part == 0) E.left[P.g] = left;
 
   int equal, more, all;
-  count_keys(key, first, PART_UNITS, P.count, last, equal, more);
+  count_keys(key, PART_UNITS, last, equal, more);
   if (lane == 0) waves[wave] = equal | more << 16;
   __syncthreads();
   const int front = waves_before<PART_WAVES>(waves, wave, all);
   int *list = E.lists + (long long)P.g * E.list;
-  const int late = list_keys(key, first, PART_UNITS, P.count, last, sum[EQ_FRONT] + (front & 0xffff), sum[GT_FRONT] + (front >> 16), mine, left, list,
+  const int late = list_keys(key, first, PART_UNITS, last, sum[EQ_FRONT] + (front & 0xffff), sum[GT_FRONT] + (front >> 16), mine, left, list,
                              list + E.list / 2);
   if (lane == 0 && late > 0) atomicAdd(&E.moves[P.g], late);
 }
@@ -781,8 +941,11 @@ static int evict_check(const compactor_cache_evict_params_t *e, const CacheView 
   return COMPACTOR_OK;
 }
 
+// Whether one workgroup a pool does everything.
 static bool evict_alone(const CacheView &C, const compactor_cache_evict_params_t *e) {
-  return (e->scope == COMPACTOR_SCOPE_HEAD || C.kv_heads == 1) && evict_most(C, e) <= ALONE_SLOTS;
+  const int most = evict_most(C, e);
+  if (e->scope == COMPACTOR_SCOPE_HEAD || C.kv_heads == 1) return most <= ALONE_SLOTS;
+  return (long long)C.kv_heads * ((most + 63) / 64) <= POOL_UNITS;
 }
 
 // Sizes and places of the parts' scratch in a workspace at `ws` (null: sizes only); returns its bytes.
@@ -887,7 +1050,10 @@ int compactor_cache_evict(const compactor_cache_t *cache, const compactor_cache_
   if (evict_alone(C, evict)) {
     E.most = evict_most(C, evict);
     (void)hipGetLastError();
-    hipLaunchKernelGGL(evict_alone_kernel, dim3((unsigned)heads), dim3(ALONE_THREADS), 0, st, C, E);
+    if (E.pool_heads == 1)
+      hipLaunchKernelGGL(evict_alone_kernel, dim3((unsigned)heads), dim3(ALONE_THREADS), 0, st, C, E);
+    else
+      hipLaunchKernelGGL(evict_pool_kernel, dim3((unsigned)(heads / C.kv_heads)), dim3(ALONE_THREADS), 0, st, C, E);
     return hipGetLastError() == hipSuccess ? COMPACTOR_OK : COMPACTOR_EHIP;
   }
   if (!workspace || workspace_bytes < evict_bytes(C, evict)) return COMPACTOR_EWORKSPACE;

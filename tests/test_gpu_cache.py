@@ -574,6 +574,27 @@ def test_evict_pools_of_many_heads(C):
 
 
 @pytest.mark.parametrize("scope", [0, 1])
+def test_evict_protects_more_than_the_budget_of_long_heads(C, scope):
+    P = U.Paged(C, DEV, _counts(1, 2, 3, 9000, 7000, 1, 9500), page=16)
+    P.fill_positions()
+    _check_evict(C, P, [200], 10, 30000, scope)
+
+
+@pytest.mark.parametrize("H,lengths,page", [(4, (4096, 4000, 0, 2500), 64), (4, (4097, 4000, 0, 2500), 1), (256, (64, 3, 0, 40), 16),
+                                            (257, (64, 3, 0, 40), 16), (70, (200, 1, 0, 130, 64), 24), (2, (8192, 8100), 32), (3, (0, 0, 5000), 8)])
+def test_evict_layers_around_what_one_workgroup_takes(C, H, lengths, page):
+    P = U.Paged(C, DEV, _counts(1, 2, H, *lengths), page=page)
+    P.fill_positions()
+    full = int(P.counts.max())
+    g = torch.Generator(device=DEV)
+    g.manual_seed(3)
+    P.mass.copy_((torch.rand(P.mass.shape, generator=g, device=DEV) * 50).floor() / 50)        # many equal ones
+    P.mass[torch.rand(P.mass.shape, generator=g, device=DEV) < 0.1] = float("nan")
+    for budget in (full // 2, full // 3, full // 50, 0):
+        _check_evict(C, P, [budget], 2, 9, 1, what="budget %d" % budget)
+
+
+@pytest.mark.parametrize("scope", [0, 1])
 def test_evict_protects_more_than_the_budget(C, scope):
     P = U.Paged(C, DEV, _counts(1, 2, 3, 90, 70, 100), page=16)
     P.fill_positions()
