@@ -128,8 +128,8 @@ def test_the_workspace_follows_max_tokens(B):
         assert B._lib.compactor_cache_attention_workspace_size(C.byref(_cache(B)), C.byref(q), C.byref(n)) == 0
         sizes.append(n.value)
     assert sizes == sorted(sizes) and sizes[2] == sizes[3] == sizes[4]
-    # a head alone needs none up to 16384 tokens, a layer always does
-    for scope, tokens, some in ((0, (10, 16384), False), (0, (16385, 40000, 0), True), (1, (10, 9000, 0), True)):
+    # a head alone needs none up to 16384 tokens, nor a layer of 8 heads up to 2048 each
+    for scope, tokens, some in ((0, (10, 16384), False), (0, (16385, 40000, 0), True), (1, (10, 2048), False), (1, (2049, 9000, 0), True)):
         n = [C.c_size_t(7) for _ in tokens]
         for out, most in zip(n, tokens):
             e = _evict(B, max_tokens=most, scope=scope)
@@ -140,8 +140,8 @@ def test_the_workspace_follows_max_tokens(B):
 
 
 def test_bad_evictions(B):
-    cache, n = _cache(B), C.c_size_t(0)
-    assert B._lib.compactor_cache_evict_workspace_size(C.byref(cache), C.byref(_evict(B, scope=1)), C.byref(n)) == 0
+    cache, n = _cache(B, table_len=300, table_stride=300), C.c_size_t(0)
+    assert B._lib.compactor_cache_evict_workspace_size(C.byref(cache), C.byref(_evict(B, scope=1)), C.byref(n)) == 0 and n.value > 0
     assert _evicts(B, cache, None) == B.EINVAL
     for kw in (dict(budget=-1), dict(sink=-1), dict(recent=-1), dict(scope=2), dict(max_tokens=-5)):
         assert _evicts(B, cache, _evict(B, **kw), wsb=n.value) == B.EINVAL, kw
