@@ -14,7 +14,7 @@
 //
 // The length of a head is split over workgroups, and over the four waves of each; the waves meet in LDS, the workgroups
 // in a second launch (attend_join_kernel), which also adds the weights to the mass: they are only known once the sum is, so the logits
-// wait in the workspace, 4 bytes a slot and query row.
+// wait in the workspace, 4 bytes a slot and query row, or a third launch has K again (attend_mass_kernel).
 #include <math.h>
 
 #include <algorithm>
@@ -38,6 +38,10 @@ constexpr int SCAN_HEADS = 512, SCAN_ROUNDS = 6;        // heads that a wave loo
 constexpr int ATT_EVEN = 256, EVEN_PARTS = 4;          // units that have equal parts of heads of one length, and most parts of a head then
 constexpr int SPLIT_ALL = 4096, SPLIT_MOST = 8;        // more heads: parts of all of them, and of one, at most
 constexpr int ATT_ALONE = 8;                 // steps of a head up to which one workgroup takes all of it
+// Weights are found from K instead of from logits that are more than the last cache holds (us with K / logits: 96 heads of 18000, 64 rows 336 / 435, 40 rows
+// 305 / 341; 24 such heads, whose logits stay near, 101 / 110 and 85 / 82; 96 of 900 to 9831, 40 rows, 99 / 92).
+constexpr int AGAIN_ROWS = 32;
+constexpr size_t AGAIN_BYTES = 256u << 20;
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
 
 // A part of a head that one workgroup does.
@@ -65,6 +69,7 @@ struct Queries {
   float *partial;              // [fragment][row][D], relative to 2^m
   float2 *stats;               // [fragment][row]: m (base 2) and the sum of 2^(x - m)
   float *logits;               // accumulate: [head][row][pitch], base 2; else null
+  float *weights;              // or, summed over the rows, [head][pitch] (attend_mass_kernel)
   int most, pitch;             // slots that there is room for
 };
 
@@ -350,6 +355,52 @@ __device__ __forceinline__ bool split_part(const CacheView &C, const Queries &Q,
   return (int)part < F.parts;
 }
 
+// The tiles of a part that a wave has: every wave a run of them.
+struct Run { int begin, end, first, tiles; };
+__device__ __forceinline__ Run run_of(const Fragment &part, int wave) {
+  Run u;
+  u.end = part.n > 0 ? min(part.step1 * ATT_STEP, part.count) : 0;      // no queries: no tiles
+  u.begin = part.step0 * ATT_STEP;
+  const int each = (max(u.end - u.begin, 0) + ATT_STEP - 1) / ATT_STEP;
+  u.first = u.begin + wave * each * ATT_TILE;
+  u.tiles = u.first < u.end ? min(each, (u.end - u.first + ATT_TILE - 1) / ATT_TILE) : 0;
+  return u;
+}
+
+// Query rows as B operands: lane l has row l & 15, channels 32 kk + 8 (l >> 4) ..; see: the slots that it sees.
+template <int NT>
+__device__ __forceinline__ void load_queries(const Queries &Q, const HeadOf &w, int R, int count, int n, Piece (&q)[NT][4], int (&see)[NT]) {
+  const int n16 = threadIdx.x & 15, j = (threadIdx.x & 63) >> 4;
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt) {
+    const int r = 16 * nt + n16, t = r / Q.group;
+    see[nt] = r < R ? sees(count, n, t) : 0;
+    const uint16_t *qp = Q.q + w.b * Q.q_stride_b + w.l * Q.q_stride_l + t * Q.q_stride_t + (w.h * Q.group + r - t * Q.group) * Q.q_stride_h;
+#pragma unroll
+    for (int kk = 0; kk < 4; ++kk) {
+      q[nt][kk].u = make_uint4(0, 0, 0, 0);
+      if (see[nt] > 0) q[nt][kk].u = *reinterpret_cast<const uint4 *>(qp + 32 * kk + 8 * j);
+    }
+  }
+}
+
+// How products of K with query rows become logits in base 2.
+struct Scaling {
+  bool capped;
+  float to_base2, to_y, cap2;
+};
+__device__ __forceinline__ Scaling scaling_of(const Queries &Q) {
+  const bool capped = Q.softcap > 0.f;
+  return Scaling{capped, Q.scale * LOG2E, capped ? Q.scale / Q.softcap : 0.f, Q.softcap * LOG2E};
+}
+// tanh(y) = 1 - 2 / (e^2y + 1); near 0, where that cancels, y times a polynomial in y^2
+__device__ __forceinline__ float capped_logit(const Scaling &c, float dot) {
+  const float y = dot * c.to_y, z = y * y;
+  const float far = c.cap2 - 2.f * c.cap2 * __builtin_amdgcn_rcpf(exp2_(y * (2.f * LOG2E)) + 1.f);
+  const float slope = fmaf(z, fmaf(z, fmaf(z, fmaf(z, 62.f / 2835.f, -17.f / 315.f), 2.f / 15.f), -1.f / 3.f), 1.f);
+  return z < 1.f / 16.f ? dot * c.to_base2 * slope : far;
+}
+
 template <int NT, bool PAGE16>
 __global__ __launch_bounds__(256, NT <= 2 ? 2 : 1) void attend_kernel(const CacheView C, const Queries Q) {
   __shared__ AttendLds<NT> L;
@@ -370,10 +421,8 @@ __global__ __launch_bounds__(256, NT <= 2 ? 2 : 1) void attend_kernel(const Cach
   const HeadPlace hp = head_place(C, w);
   const int count = part.count, n = part.n;
   const bool complete = part.parts == 1;
-  const int end = n > 0 ? min(part.step1 * ATT_STEP, count) : 0;      // no queries: no tiles
-  // every wave has a run of the part's tiles
-  const int begin = part.step0 * ATT_STEP, each = (max(end - begin, 0) + ATT_STEP - 1) / ATT_STEP, first = begin + wave * each * ATT_TILE;
-  const int tiles = first < end ? min(each, (end - first + ATT_TILE - 1) / ATT_TILE) : 0;
+  const Run run = run_of(part, wave);
+  const int first = run.first, tiles = run.tiles;
   const int seen_by_all = count - (n - 1);
   const uint16_t *kp = C.k + hp.rows, *vp = C.v + hp.rows;
 
@@ -385,20 +434,9 @@ __global__ __launch_bounds__(256, NT <= 2 ? 2 : 1) void attend_kernel(const Cach
     places_take(C, P);
     places_fetch(C, hp, (long long)first + ATT_TILE, count, lane, P);
   }
-  // query rows as B operands: lane l has row l & 15, channels 32 kk + 8 (l >> 4) ..
   Piece q[NT][4];
   int see[NT];
-#pragma unroll
-  for (int nt = 0; nt < NT; ++nt) {
-    const int r = 16 * nt + n16, t = r / Q.group;
-    see[nt] = r < R ? sees(count, n, t) : 0;
-    const uint16_t *qp = Q.q + w.b * Q.q_stride_b + w.l * Q.q_stride_l + t * Q.q_stride_t + (w.h * Q.group + r - t * Q.group) * Q.q_stride_h;
-#pragma unroll
-    for (int kk = 0; kk < 4; ++kk) {
-      q[nt][kk].u = make_uint4(0, 0, 0, 0);
-      if (see[nt] > 0) q[nt][kk].u = *reinterpret_cast<const uint4 *>(qp + 32 * kk + 8 * j);
-    }
-  }
+  load_queries<NT>(Q, w, R, count, n, q, see);
   Piece k[8], v[8];
   const unsigned stride = PAGE16 ? 2u * (unsigned)C.slot_stride : 0u, k_at = n16 * stride + 16 * j, v_at = 4 * j * stride + 16 * n16;
   auto tile_there = [&](int tile) {
@@ -415,8 +453,7 @@ __global__ __launch_bounds__(256, NT <= 2 ? 2 : 1) void attend_kernel(const Cach
 #pragma unroll
     for (int c = 0; c < 8; ++c) acc[nt][c] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
-  const bool capped = Q.softcap > 0.f;
-  const float to_base2 = Q.scale * LOG2E, to_y = capped ? Q.scale / Q.softcap : 0.f, cap2 = Q.softcap * LOG2E;
+  const Scaling scaling = scaling_of(Q);
   const bool store = Q.logits != nullptr && count <= Q.most;
   float *logits = Q.logits + (long long)g * R * Q.pitch;
   float *kept = L.kept[wave];
@@ -490,17 +527,12 @@ __global__ __launch_bounds__(256, NT <= 2 ? 2 : 1) void attend_kernel(const Cach
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
       float x[8];
-      if (capped) {                // tanh(y) = 1 - 2 / (e^2y + 1); near 0, where that cancels, y times a polynomial in y^2
+      if (scaling.capped) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const float dot = s[nt][i >> 2][i & 3], y = dot * to_y, z = y * y;
-          const float far = cap2 - 2.f * cap2 * __builtin_amdgcn_rcpf(exp2_(y * (2.f * LOG2E)) + 1.f);
-          const float slope = fmaf(z, fmaf(z, fmaf(z, fmaf(z, 62.f / 2835.f, -17.f / 315.f), 2.f / 15.f), -1.f / 3.f), 1.f);
-          x[i] = z < 1.f / 16.f ? dot * to_base2 * slope : far;
-        }
+        for (int i = 0; i < 8; ++i) x[i] = capped_logit(scaling, s[nt][i >> 2][i & 3]);
       } else {
 #pragma unroll
-        for (int i = 0; i < 8; ++i) x[i] = s[nt][i >> 2][i & 3] * to_base2;
+        for (int i = 0; i < 8; ++i) x[i] = s[nt][i >> 2][i & 3] * scaling.to_base2;
       }
       if (__builtin_expect(!whole, 0)) {
         const int upto = see[nt] - s0 - 4 * j;
@@ -637,6 +669,7 @@ __global__ __launch_bounds__(256, NT <= 2 ? 2 : 1) void attend_kernel(const Cach
       if (complete) {
         finish_row(C, Q, w, row, ch, o, mm, sum);
         if (ch == 0) L.lse2[row] = sum == 0.f ? INFINITY : mm + __builtin_amdgcn_logf(sum);
+        if (ch == 0 && Q.weights != nullptr) Q.stats[(long long)fragment * R + row] = make_float2(mm, sum);
       } else {
         const long long at = (long long)fragment * R + row;
         f32x4 *to = reinterpret_cast<f32x4 *>(Q.partial + at * D + ch);
@@ -676,6 +709,32 @@ __device__ __forceinline__ float2 join_stats(const Queries &Q, int first, int pa
   float sum = top == -INFINITY ? 0.f : l * exp2_(m - top);
   for (int d = 32; d > 0; d >>= 1) sum += __shfl_xor(sum, d);
   return make_float2(top, sum);
+}
+
+// What every row's weights are relative to, by a workgroup; stats: 256 entries.
+__device__ __forceinline__ void row_sums(const Queries &Q, const Fragment &f, int R, float2 *stats, float *lse2) {
+  const int tid = threadIdx.x;
+  // Up to 16 rows the waves take rows in turn, their lanes fragments (4 rows, 2.3 M slots: 248 us a call, in the other way 250);
+  // more of them all at once: thread (group, row) takes every groups-th fragment, the first R threads add up the groups' (28 rows,
+  // 72 heads of up to 3618: 56 us a call, in the first way 60).
+  if (R <= 16) {
+    for (int r = tid >> 6; r < R; r += 4) {
+      const float2 all = join_stats(Q, f.first, f.parts, R, r);
+      if ((tid & 63) == 0) lse2[r] = all.y == 0.f ? INFINITY : all.x + __builtin_amdgcn_logf(all.y);
+    }
+  } else {
+    const int groups = (int)(256u / (unsigned)R), group = (int)((unsigned)tid / (unsigned)R), r = tid - group * R;
+    float m = -INFINITY, l = 0.f;
+    if (group < groups)
+      for (int k = group; k < f.parts; k += groups) add_stats(m, l, Q.stats[(long long)(f.first + k) * R + r]);
+    stats[tid] = make_float2(m, l);
+    __syncthreads();
+    if (tid < R) {
+#pragma unroll 4
+      for (int i = 1; i < min(groups, f.parts); ++i) add_stats(m, l, stats[i * R + tid]);
+      lse2[tid] = l == 0.f ? INFINITY : m + __builtin_amdgcn_logf(l);
+    }
+  }
 }
 
 __global__ __launch_bounds__(256) void attend_join_kernel(const CacheView C, const Queries Q) {
@@ -720,31 +779,144 @@ __global__ __launch_bounds__(256) void attend_join_kernel(const CacheView C, con
   if (from >= to) return;
   MassQuad M;
   mass_fetch(C, Q, hp, logits, R, min(from + 4 * tid, (to - 1) & ~3), to, M);
-  // The rows' sums.  Up to 16 rows the waves take rows in turn, their lanes fragments (4 rows, 2.3 M slots: 248 us a call, in the other way 250);
-  // more of them all at once: thread (group, row) takes every groups-th fragment, the first R threads add up the groups' (28 rows,
-  // 72 heads of up to 3618: 56 us a call, in the first way 60).
-  if (R <= 16) {
-    for (int r = tid >> 6; r < R; r += 4) {
-      const float2 all = join_stats(Q, f.first, f.parts, R, r);
-      if ((tid & 63) == 0) lse2[r] = all.y == 0.f ? INFINITY : all.x + __builtin_amdgcn_logf(all.y);
-    }
-  } else {
-    const int groups = (int)(256u / (unsigned)R), group = (int)((unsigned)tid / (unsigned)R), r = tid - group * R;
-    float m = -INFINITY, l = 0.f;
-    if (group < groups)
-      for (int k = group; k < f.parts; k += groups) add_stats(m, l, Q.stats[(long long)(f.first + k) * R + r]);
-    stats[tid] = make_float2(m, l);
-    __syncthreads();
-    if (tid < R) {
-#pragma unroll 4
-      for (int i = 1; i < min(groups, f.parts); ++i) add_stats(m, l, stats[i * R + tid]);
-      lse2[tid] = l == 0.f ? INFINITY : m + __builtin_amdgcn_logf(l);
-    }
-  }
+  row_sums(Q, f, R, stats, lse2);
   __syncthreads();
   for (int at = from + 4 * tid; at < to; at += 4 * 256) {
     if (at >= from + 4 * 256) mass_fetch(C, Q, hp, logits, R, at, to, M);
     mass_add(Q, lse2, logits, R, at, M);
+  }
+}
+
+// Weights of many rows from K, which is read again: 256 bytes a slot, where the logits' way through the workspace takes 8 for every row.
+// (Third launch.)  A fragment a workgroup; its rows' sums are known.  A lane has 8 slots of query l & 15 as in attend_kernel, and the sum over the
+// rows is one over its tiles of rows and 16 lanes.
+template <int NT>
+struct MassLds {
+  float2 stats[256];
+  float lse2[MOST_ROWS];
+};
+template <int NT, bool PAGE16>
+__global__ __launch_bounds__(256) void attend_mass_kernel(const CacheView C, const Queries Q) {
+  __shared__ MassLds<NT> L;
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, n16 = lane & 15, j = lane >> 4;
+  const int R = Q.tokens * Q.group;
+  const Fragment part = Q.frags[blockIdx.x];
+  if (part.head < 0 || part.n <= 0 || part.count > Q.most) return;
+  const HeadOf w = head_of(C, (unsigned)part.head);
+  const HeadPlace hp = head_place(C, w);
+  const int count = part.count, seen_by_all = count - (part.n - 1);
+  const Run run = run_of(part, wave);
+  const int first = run.first, tiles = run.tiles;
+  const uint16_t *kp = C.k + hp.rows;
+  Places<PAGE16> P;
+  if (PAGE16) {
+    places_run(C, hp, first, count, lane, P);
+  } else {
+    places_fetch(C, hp, first, count, lane, P);
+    places_take(C, P);
+    places_fetch(C, hp, (long long)first + ATT_TILE, count, lane, P);
+  }
+  Piece q[NT][4], k[8];
+  int see[NT];
+  load_queries<NT>(Q, w, R, count, part.n, q, see);
+  const unsigned stride = PAGE16 ? 2u * (unsigned)C.slot_stride : 0u, k_at = n16 * stride + 16 * j;
+  auto tile_there = [&](int tile) {
+    if (!PAGE16) return (unsigned)P.there;
+    const unsigned two = (unsigned)(P.there >> (2 * (tile & 31)));
+    return (two & 1u ? 0xffffu : 0u) | (two & 2u ? 0xffff0000u : 0u);
+  };
+  unsigned there = 0;
+  if (tiles > 0) {
+    load_rows<PAGE16, true>(kp, P, 0, lane, k_at, stride, k);
+    there = tile_there(0);
+  }
+  row_sums(Q, part, R, L.stats, L.lse2);
+  __syncthreads();
+  float z[NT];
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt) z[nt] = see[nt] > 0 ? L.lse2[16 * nt + n16] : INFINITY;
+  const Scaling scaling = scaling_of(Q);
+  float *weights = Q.weights + (long long)part.head * Q.pitch;
+
+  auto one_tile = [&](int tile, auto another) {
+    constexpr bool more = decltype(another)::value;
+    const int s0 = first + tile * ATT_TILE;
+    f32x4 s[NT][2];
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt)
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {
+        s[nt][half] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int kk = 0; kk < 4; ++kk)
+          s[nt][half] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(k[4 * half + kk].v, q[nt][kk].v, s[nt][half], 0, 0, 0);
+      }
+    unsigned there_next = 0;
+    if constexpr (more) {
+      if (PAGE16) {
+        if (((tile + 1) & 31) == 0) places_run(C, hp, s0 + ATT_TILE, count, lane, P);
+      } else {
+        places_take(C, P);
+        places_fetch(C, hp, (long long)s0 + 2 * ATT_TILE, count, lane, P);
+      }
+      load_rows<PAGE16, true>(kp, P, (tile + 1) & 31, lane, k_at, stride, k);
+      there_next = tile_there(tile + 1);
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    const int left = count - s0;
+    if (left < 32) there &= (1u << left) - 1u;
+    const bool whole = there == 0xffffffffu && s0 + ATT_TILE <= seen_by_all;
+    const unsigned there_at = there >> (4 * j);
+    float sum[8] = {};
+#pragma unroll
+    for (int nt = 0; nt < NT; ++nt) {
+      float x[8];
+      if (scaling.capped) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = capped_logit(scaling, s[nt][i >> 2][i & 3]);
+      } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = s[nt][i >> 2][i & 3] * scaling.to_base2;
+      }
+      if (__builtin_expect(!whole, 0)) {
+        const int upto = see[nt] - s0 - 4 * j;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const int at = 16 * (i >> 2) + (i & 3);
+          x[i] = (there_at >> at & 1u) && at < upto ? x[i] : -INFINITY;
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i) sum[i] += z[nt] == INFINITY ? 0.f : exp2_(x[i] - z[nt]);
+    }
+    // over the 16 lanes: neighbours, pairs, fours, eights
+    float mine = 0.f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      float y = sum[i];
+      y += __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(y), 0xb1, 0xf, 0xf, false));
+      y += __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(y), 0x4e, 0xf, 0xf, false));
+      y += __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(y), 0x141, 0xf, 0xf, false));
+      y += __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(y), 0x140, 0xf, 0xf, false));
+      mine = n16 == i ? y : mine;
+    }
+    if (n16 < 8) weights[s0 + 16 * (n16 >> 2) + 4 * j + (n16 & 3)] = mine;
+    there = there_next;
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  if (tiles > 0) {
+    for (int tile = 0; tile + 1 < tiles; ++tile) one_tile(tile, std::true_type());
+    one_tile(tiles - 1, std::false_type());
+  }
+  __threadfence_block();
+  __syncthreads();
+  const float inv = 1.f / (float)Q.group;
+  for (int at = run.begin + 4 * tid; at < run.end; at += 4 * 256) {
+    MassQuad M;
+    mass_fetch(C, Q, hp, weights, 1, at, run.end, M);
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (M.there[i]) *M.mass[i] = fmaf(M.x[0][i], inv, M.old[i]);
   }
 }
 
@@ -766,7 +938,8 @@ static int query_most(const CacheView &C, const compactor_cache_query_t *q) {
 
 struct AttendPlan {
   int rows, frags_most, target, split, pitch;
-  size_t frags, head_frags, partial, stats, logits;       // bytes, in this order in the workspace
+  bool again;                  // weights from K, read again
+  size_t frags, head_frags, partial, stats, logits;       // bytes, in this order in the workspace (logits: or weights)
   size_t bytes() const { return frags + head_frags + partial + stats + logits; }
 };
 
@@ -796,7 +969,9 @@ static AttendPlan attend_plan(const CacheView &C, const compactor_cache_query_t 
   A.head_frags = n > 0 ? up((size_t)heads * sizeof(int2)) : 0;
   A.partial = up(n * A.rows * D * sizeof(float));
   A.stats = up(n * A.rows * sizeof(float2));
-  A.logits = q->accumulate ? up((size_t)heads * A.rows * A.pitch * sizeof(float)) : 0;
+  const size_t a_row = (size_t)heads * A.pitch * sizeof(float);
+  A.again = q->accumulate && A.rows > AGAIN_ROWS && A.frags_most > 0 && a_row * A.rows > AGAIN_BYTES;
+  A.logits = q->accumulate ? up(A.again ? a_row : a_row * A.rows) : 0;
   return A;
 }
 
@@ -852,7 +1027,7 @@ int compactor_cache_attention(const compactor_cache_t *cache, const compactor_ca
   if (need > 0 && (reinterpret_cast<uintptr_t>(workspace) & 255u)) return COMPACTOR_EALIGN;
   const long long heads = (long long)C.nreq * C.layers * C.kv_heads;
   const long long blocks = A.frags_most > 0 ? A.frags_most : heads;
-  const long long join = A.frags_most > 0 ? heads * A.rows + (query->accumulate ? A.frags_most : 0) : 0;
+  const long long join = A.frags_most > 0 ? heads * A.rows + (query->accumulate && !A.again ? A.frags_most : 0) : 0;
   if (blocks > 0x7fffffffll || join > 0x7fffffffll) return COMPACTOR_EINVAL;
   Queries Q;
   Q.q = static_cast<const uint16_t *>(query->q);
@@ -875,19 +1050,28 @@ int compactor_cache_attention(const compactor_cache_t *cache, const compactor_ca
   Q.head_frags = reinterpret_cast<int2 *>(ws += A.frags);
   Q.partial = reinterpret_cast<float *>(ws += A.head_frags);
   Q.stats = reinterpret_cast<float2 *>(ws += A.partial);
-  Q.logits = query->accumulate ? reinterpret_cast<float *>(ws += A.stats) : nullptr;
+  ws += A.stats;
+  Q.logits = query->accumulate && !A.again ? reinterpret_cast<float *>(ws) : nullptr;
+  Q.weights = A.again ? reinterpret_cast<float *>(ws) : nullptr;
   Q.most = query_most(C, query);
   Q.pitch = A.pitch;
   hipStream_t st = static_cast<hipStream_t>(stream);
   (void)hipGetLastError();   // a leftover of earlier, unrelated HIP calls is not this call's error
   // halves of tiles with one origin, and offsets inside one that fit 32 bits
-  if (C.page_size % 16 == 0 && C.slot_stride <= (1 << 24))
+  const bool page16 = C.page_size % 16 == 0 && C.slot_stride <= (1 << 24);
+  if (page16)
     launch_attend<true>(C, Q, (unsigned)blocks, st);
   else
     launch_attend<false>(C, Q, (unsigned)blocks, st);
   if (A.frags_most > 0) {
     if (hipGetLastError() != hipSuccess) return COMPACTOR_EHIP;
     hipLaunchKernelGGL(attend_join_kernel, dim3((unsigned)join), dim3(256), 0, st, C, Q);
+  }
+  if (A.again) {
+    if (hipGetLastError() != hipSuccess) return COMPACTOR_EHIP;
+    const auto kernel = A.rows <= 48 ? (page16 ? attend_mass_kernel<3, true> : attend_mass_kernel<3, false>)
+                                     : (page16 ? attend_mass_kernel<4, true> : attend_mass_kernel<4, false>);
+    hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3(256), 0, st, C, Q);
   }
   return hipGetLastError() == hipSuccess ? COMPACTOR_OK : COMPACTOR_EHIP;
 }

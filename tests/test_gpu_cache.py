@@ -94,6 +94,24 @@ def test_attention_long(C, B, L, H, n, page, G, T):
     _attend(C, P, _queries(P, T, H * G), cap=20.0 if T > 1 else 0.0)
 
 
+@pytest.mark.parametrize("H,lengths,page", [(2, (9001, 300, 0, 1), 64), (1, (20011, 6000, 4500, 31), 24), (3, (5000, 3, 2500), 16), (1, (2100,) * 4, 7)])
+@pytest.mark.parametrize("G,T", [(8, 5), (8, 8), (64, 1), (1, 33), (7, 7)])
+@pytest.mark.parametrize("room", [0, 2 ** 28 + 1])
+def test_attention_weights_of_many_rows(C, H, lengths, page, G, T, room):
+    """More than 32 query rows over heads that several workgroups share, heads of one workgroup and empty ones beside them, padded
+    requests, a page that is not there, capped or not; tables with room for `room` bytes of logits too."""
+    P = U.Paged(C, DEV, _counts(4, 1, H, *lengths), page=page)
+    P.tables[1, 1] = -1
+    if room:             # (the oracle keeps to the pages that are there)
+        wide = torch.full((4, room // (4 * H * G * T * page * 4) + 1), -1, dtype=torch.int32, device=DEV)
+        wide[:, :P.per] = P.tables
+        P.cache = C.Cache(P.k, P.v, wide, P.counts, P.seen, P.mass, P.positions)
+        assert C.compactor_cache_attention_workspace_size(P.cache, _queries(P, T, H * G), accumulate=True) < 2 ** 28
+    cap = 15.0 if T == 5 else 0.0
+    _attend(C, P, _queries(P, T, H * G), cap=cap)
+    _attend(C, P, _queries(P, T, H * G), new=[T - 1, 0, T, 1], cap=cap, most=9000 if H == 2 else 0)
+
+
 @pytest.mark.parametrize("B,L,H,lengths", [(5, 2, 9, (2000, 1, 0, 1025, 700, 128, 129, 1999)), (16, 1, 8, (1300,)), (16, 1, 8, (1290, 1300, 1280)),
                                            (43, 1, 7, (1100, 30, 0, 1500)), (37, 2, 4, (1100, 1090)), (8, 8, 8, (1030, 1024, 513, 60)),
                                            (65, 1, 8, (1100, 5, 900, 0, 1400)), (9, 8, 9, (1200,)), (1, 513, 1, (1025,)), (200, 3, 7, (40, 1100, 0))])
