@@ -963,14 +963,15 @@ static AttendPlan attend_plan(const CacheView &C, const compactor_cache_query_t 
     if (A.split > 1) A.frags_most = A.split * (int)heads;
   }
   A.pitch = (int)((most + ATT_TILE - 1) / ATT_TILE * ATT_TILE);
+  const size_t a_row = (size_t)heads * A.pitch * sizeof(float);
+  A.again = q->accumulate && A.rows > AGAIN_ROWS && a_row * A.rows > AGAIN_BYTES;
+  if (A.again && A.frags_most == 0) A.frags_most = (int)heads;        // one each, for what is known of them
   auto up = [](size_t x) { return (x + 255) / 256 * 256; };
   const size_t n = A.frags_most;
   A.frags = up(n * sizeof(Fragment));
   A.head_frags = n > 0 ? up((size_t)heads * sizeof(int2)) : 0;
   A.partial = up(n * A.rows * D * sizeof(float));
   A.stats = up(n * A.rows * sizeof(float2));
-  const size_t a_row = (size_t)heads * A.pitch * sizeof(float);
-  A.again = q->accumulate && A.rows > AGAIN_ROWS && A.frags_most > 0 && a_row * A.rows > AGAIN_BYTES;
   A.logits = q->accumulate ? up(A.again ? a_row : a_row * A.rows) : 0;
   return A;
 }

@@ -112,6 +112,16 @@ def test_attention_weights_of_many_rows(C, H, lengths, page, G, T, room):
     _attend(C, P, _queries(P, T, H * G), new=[T - 1, 0, T, 1], cap=cap, most=9000 if H == 2 else 0)
 
 
+def test_attention_weights_of_many_rows_of_many_short_heads(C):
+    """The same where every head has a workgroup of its own."""
+    P = U.Paged(C, DEV, _counts(20, 1, 55, 0, 1, 33, 40), page=16)
+    wide = torch.full((20, 64), -1, dtype=torch.int32, device=DEV)
+    wide[:, :P.per] = P.tables
+    P.cache = C.Cache(P.k, P.v, wide, P.counts, P.seen, P.mass, P.positions)
+    assert C.compactor_cache_attention_workspace_size(P.cache, _queries(P, 1, 55 * 64), accumulate=True) < 2 ** 28
+    _attend(C, P, _queries(P, 1, 55 * 64), new=[1, 0] * 10)
+
+
 @pytest.mark.parametrize("B,L,H,lengths", [(5, 2, 9, (2000, 1, 0, 1025, 700, 128, 129, 1999)), (16, 1, 8, (1300,)), (16, 1, 8, (1290, 1300, 1280)),
                                            (43, 1, 7, (1100, 30, 0, 1500)), (37, 2, 4, (1100, 1090)), (8, 8, 8, (1030, 1024, 513, 60)),
                                            (65, 1, 8, (1100, 5, 900, 0, 1400)), (9, 8, 9, (1200,)), (1, 513, 1, (1025,)), (200, 3, 7, (40, 1100, 0))])
