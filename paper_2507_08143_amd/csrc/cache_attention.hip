@@ -790,14 +790,10 @@ __global__ __launch_bounds__(256) void attend_join_kernel(const CacheView C, con
 // Weights of many rows from K, which is read again: 256 bytes a slot, where the logits' way through the workspace takes 8 for every row.
 // (Third launch.)  A fragment a workgroup; its rows' sums are known.  A lane has 8 slots of query l & 15 as in attend_kernel, and the sum over the
 // rows is one over its tiles of rows and 16 lanes.
-template <int NT>
-struct MassLds {
-  float2 stats[256];
-  float lse2[MOST_ROWS];
-};
 template <int NT, bool PAGE16>
 __global__ __launch_bounds__(256) void attend_mass_kernel(const CacheView C, const Queries Q) {
-  __shared__ MassLds<NT> L;
+  __shared__ float2 stats[256];
+  __shared__ float lse2[MOST_ROWS];
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, n16 = lane & 15, j = lane >> 4;
   const int R = Q.tokens * Q.group;
   const Fragment part = Q.frags[blockIdx.x];
@@ -830,11 +826,11 @@ __global__ __launch_bounds__(256) void attend_mass_kernel(const CacheView C, con
     load_rows<PAGE16, true>(kp, P, 0, lane, k_at, stride, k);
     there = tile_there(0);
   }
-  row_sums(Q, part, R, L.stats, L.lse2);
+  row_sums(Q, part, R, stats, lse2);
   __syncthreads();
   float z[NT];
 #pragma unroll
-  for (int nt = 0; nt < NT; ++nt) z[nt] = see[nt] > 0 ? L.lse2[16 * nt + n16] : INFINITY;
+  for (int nt = 0; nt < NT; ++nt) z[nt] = see[nt] > 0 ? lse2[16 * nt + n16] : INFINITY;
   const Scaling scaling = scaling_of(Q);
   float *weights = Q.weights + (long long)part.head * Q.pitch;
 
