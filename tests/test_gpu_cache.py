@@ -122,6 +122,26 @@ def test_attention_weights_of_many_rows_of_many_short_heads(C):
     _attend(C, P, _queries(P, 1, 55 * 64), new=[1, 0] * 10)
 
 
+@pytest.mark.parametrize("page", [16, 24])
+@pytest.mark.parametrize("T", [1, 9])
+def test_attention_of_one_long_request_among_many(C, page, T):
+    """Few parts a head, because there are many heads: a wave has more tiles than it keeps places for."""
+    P = U.Paged(C, DEV, [[[34001, 40, 0, 20000, 33999, 1, 128, 16385]]], page=page)
+    B = 66
+    tables = torch.full((B, P.per), -1, dtype=torch.int32, device=DEV)
+    tables[0] = P.tables[0]
+    counts, seen = (torch.zeros(B, 1, 8, dtype=torch.int32, device=DEV) for _ in range(2))
+    counts[0] = P.counts[0]
+    cache = C.Cache(P.k, P.v, tables, counts, seen, P.mass, P.positions)
+    q = torch.zeros(B, 1, T, 32, 128, dtype=torch.bfloat16, device=DEV)
+    q[:1] = _queries(P, T, 32)
+    before = P.snapshot()
+    out, lse = C.compactor_cache_attention(cache, q, accumulate=True, want_lse=True)
+    torch.cuda.synchronize()
+    assert not out[1:].float().any() and torch.isneginf(lse[1:]).all()
+    U.check_attention(P, q[:1], None, 128 ** -0.5, 0.0, out[:1], lse[:1], before, True)
+
+
 @pytest.mark.parametrize("B,L,H,lengths", [(5, 2, 9, (2000, 1, 0, 1025, 700, 128, 129, 1999)), (16, 1, 8, (1300,)), (16, 1, 8, (1290, 1300, 1280)),
                                            (43, 1, 7, (1100, 30, 0, 1500)), (37, 2, 4, (1100, 1090)), (8, 8, 8, (1030, 1024, 513, 60)),
                                            (65, 1, 8, (1100, 5, 900, 0, 1400)), (9, 8, 9, (1200,)), (1, 513, 1, (1025,)), (200, 3, 7, (40, 1100, 0))])
