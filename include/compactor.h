@@ -401,7 +401,7 @@ typedef struct compactor_cache_query {
  *   out = sum_s p_s v_s,   mass[s] += 1/G sum over t and g of p_s   (accumulate).
  * A query that sees nothing, and a padding row (t >= n_b), gives zeros, lse -inf and no weight, whatever the
  * memory holds that it does not see.
- * softmax and sums in fp32, p v with p as two bf16 planes (16 mantissa bits), out rounded once. */
+ * softmax, weights and sums in fp32, out rounded once. */
 int compactor_cache_attention(const compactor_cache_t *cache, const compactor_cache_query_t *query,
                               void *workspace, size_t workspace_bytes, void *stream);
 

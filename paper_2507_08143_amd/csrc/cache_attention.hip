@@ -109,6 +109,21 @@ __device__ __forceinline__ void wave_lds_fence() {
   __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
 }
 
+// Two weights as sums of three bf16 numbers, 8 bits of their 24 each: truncated, so that no number is negative, and the two smaller ones no
+// less than 2^-126 unless the weight is 0.  A row of V with an infinity then adds infinities of one sign (with a difference of rounded numbers,
+// or 0 times it, their sum is NaN).  x: 0 or at least 2^-126.  (us with two rounded planes, 16 bits / with three: 2.3 M slots, 4 rows 248 / 249; 96 heads
+// of 18000, 32 rows 184 / 186, 40 rows with weights 302 / 313, 64 rows 230 / 260.)
+__device__ __forceinline__ void split(float x0, float x1, unsigned &hi, unsigned &mid, unsigned &lo) {
+  const auto rest = [](float x, float least) { return fmaxf(x - __uint_as_float(__float_as_uint(x) & 0xffff0000u), least); };
+  const auto upper = [](float a, float b) { return __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u); };
+  const float least0 = fminf(x0, 0x1p-126f), least1 = fminf(x1, 0x1p-126f);
+  hi = upper(x0, x1);
+  x0 = rest(x0, least0);
+  x1 = rest(x1, least1);
+  mid = upper(x0, x1);
+  lo = upper(rest(x0, least0), rest(x1, least1));
+}
+
 union Piece {
   uint4 u;
   unsigned w[4];
@@ -523,7 +538,7 @@ __global__ __launch_bounds__(256, NT <= 2 ? 2 : 1) void attend_kernel(const Cach
         }
       }
     }
-    Piece hi[NT], lo[NT];          // P as two bf16 planes, B operands: 16 mantissa bits
+    Piece hi[NT], mid[NT], lo[NT];          // P as three bf16 planes, B operands: split()
 #pragma unroll
     for (int nt = 0; nt < NT; ++nt) {
       float x[8];
@@ -568,10 +583,7 @@ __global__ __launch_bounds__(256, NT <= 2 ? 2 : 1) void attend_kernel(const Cach
       }
       l[nt] += sum;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        hi[nt].w[i] = pack_bf16(x[2 * i], x[2 * i + 1]);
-        lo[nt].w[i] = pack_bf16(x[2 * i] - __uint_as_float(hi[nt].w[i] << 16), x[2 * i + 1] - __uint_as_float(hi[nt].w[i] & 0xffff0000u));
-      }
+      for (int i = 0; i < 4; ++i) split(x[2 * i], x[2 * i + 1], hi[nt].w[i], mid[nt].w[i], lo[nt].w[i]);
       if (__builtin_expect(ahead, 0)) {
         float *mine = L.p[wave][n16];
         wave_lds_fence();
@@ -605,6 +617,7 @@ __global__ __launch_bounds__(256, NT <= 2 ? 2 : 1) void attend_kernel(const Cach
 #pragma unroll
       for (int nt = 0; nt < NT; ++nt) {
         acc[nt][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.v, hi[nt].v, acc[nt][c], 0, 0, 0);
+        acc[nt][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.v, mid[nt].v, acc[nt][c], 0, 0, 0);
         acc[nt][c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.v, lo[nt].v, acc[nt][c], 0, 0, 0);
       }
     }

@@ -206,6 +206,62 @@ def test_attention_values_that_are_seen_count(C):
     assert torch.isnan(o[4:6]).all() and torch.isnan(lse[0, 0, 0, 4:6]).all()
 
 
+@pytest.mark.parametrize("count,G,T", [(1, 1, 1), (1, 4, 1), (40, 4, 1), (129, 7, 1), (127, 4, 5), (100, 6, 6), (120, 8, 8), (2001, 4, 1)])
+@pytest.mark.parametrize("page,gain", [(16, 1.0), (24, 8.0)])
+def test_attention_infinite_values_that_are_seen(C, count, G, T, page, gain):
+    """An infinity in channel s of the value of slot s: the infinity, of its sign, whatever the weight, and numbers elsewhere."""
+    P = U.Paged(C, DEV, [[[count]]], page=page, gain=gain)
+    n = min(count, 128) - T + 1                   # seen by all queries
+    for s in range(n):
+        P.v[int(P.tables[0, s // page]), 0, s % page, 0, s] = float("inf") if s % 3 else -float("inf")
+    out, lse = C.compactor_cache_attention(P.cache, _queries(P, T, G), want_lse=True)
+    o = out.float()
+    want = torch.full((n,), float("inf"), device=DEV)
+    want[::3] = -float("inf")
+    assert torch.equal(o[..., :n], want.expand(1, 1, T, G, n)) and bool(torch.isfinite(o[..., n:]).all() & torch.isfinite(lse).all())
+
+
+def _weights_that_need_24_bits(n):
+    """n logits x in (-1, 0), exact in bf16, whose weights w = e^x are 2^-19 or more away from the sum of two bf16 numbers.
+    -> x, the two numbers, w"""
+    x = -torch.arange(1, 1024, dtype=torch.float64) / 1024
+    x = x[x.to(torch.bfloat16).double() == x]
+    w = x.exp()
+    one = w.to(torch.bfloat16).double()
+    two = (w - one).to(torch.bfloat16).double()
+    x, one, two, w = (t[(w - one - two).abs() >= 2.0 ** -19] for t in (x, one, two, w))
+    at = torch.arange(n) % len(x)
+    return x[at], one[at], two[at], w[at]
+
+
+@pytest.mark.parametrize("G,T", [(1, 1), (4, 1), (4, 5), (7, 6), (8, 8)])
+@pytest.mark.parametrize("page", [16, 24])
+@pytest.mark.parametrize("n,tile", [(100, 0), (100, 2), (9001, 137)])
+def test_attention_weights_have_all_bits(C, G, T, page, n, tile):
+    """Values that cancel all but the last 8 of the 24 bits of a weight.  Row r has logits 0, 0 and x_r at three slots of one tile and
+    less than -200 elsewhere, and its channel r the values -a, -b and 1 there: out = (w - a - b) / (2 + w), w = e^(x_r).
+    Of |x_r| < 1 the fp32 weight is off by at most w (2^-23 for its exponential, 2 |x| 2^-24 for the argument) <= 2^-22, and the
+    differences are exact in fp32; the division and the rounding to bf16 cost 2^-7 of the result at most.  A weight in 16 bits
+    would give 0 in place of 2^-19 / 3 or more."""
+    R = G * T
+    x, a, b, w = _weights_that_need_24_bits(R)
+    P = U.Paged(C, DEV, [[[n]]], page=page)
+    P.k.zero_(), P.v.zero_()
+    P.k[..., 127] = -200.0
+    s = 32 * tile + 5
+    rows = torch.arange(R)
+    for slot, key, value in ((s, torch.zeros(R), -a), (s + 3, x, torch.ones(R)), (s + 17, torch.zeros(R), -b)):
+        p, at = int(P.tables[0, slot // page]), slot % page
+        P.k[p, 0, at, 0] = 0.0
+        P.k[p, 0, at, 0, :R], P.v[p, 0, at, 0, :R] = key.to(DEV).to(torch.bfloat16), value.to(DEV).to(torch.bfloat16)
+    q = torch.zeros(R, 128, dtype=torch.bfloat16, device=DEV)
+    q[rows, rows], q[:, 127] = 1.0, 1.0
+    out, _ = C.compactor_cache_attention(P.cache, q.view(1, 1, T, G, 128), scale=1.0, accumulate=True)
+    got = out.view(R, 128).double().cpu()[rows, rows]
+    want = (w - a - b) / (2 + w)
+    assert bool(((got - want).abs() <= 2.0 ** -22 / (2 + w) + 2.0 ** -7 * want.abs()).all()), (got, want)
+
+
 def test_attention_strides_layers_and_buffers(C):
     """q and out inside larger tensors, token-major and head-major, one layer of several, given buffers."""
     P = U.Paged(C, DEV, _counts(2, 3, 4, 70, 200, 33, 1, 150), page=16, layout="token")
