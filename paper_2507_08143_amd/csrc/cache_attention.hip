@@ -670,7 +670,7 @@ __global__ __launch_bounds__(256, NT <= 2 ? 2 : 1) void attend_kernel(const Cach
 #pragma unroll
     for (int i = 1; i < ATT_WAVES; ++i) mm = fmaxf(mm, L.m[i][row]);
 #pragma unroll
-    for (int i = 0; i < ATT_WAVES; ++i) sum += mm == -INFINITY ? 0.f : L.l[i][row] * exp2_(L.m[i][row] - mm);
+    for (int i = 0; i < ATT_WAVES; ++i) sum += mm == -INFINITY ? L.l[i][row] : L.l[i][row] * exp2_(L.m[i][row] - mm);     // (-inf: 0, or NaN)
     f32x4 o[2];
 #pragma unroll
     for (int c = 0; c < 2; ++c) {
@@ -707,9 +707,10 @@ __global__ __launch_bounds__(256, NT <= 2 ? 2 : 1) void attend_kernel(const Cach
 // Second launch: the fragments of a head meet.  The first heads * R workgroups take a query row each, 16 fragments side by side
 // and 8 channels a thread; the others add a fragment's weights to the mass.
 
+// Where the maximum is -inf the sum is 0 (nothing was seen) or NaN (only logits that are none), which stays.
 __device__ __forceinline__ void add_stats(float &m, float &l, const float2 &x) {
   const float to = fmaxf(m, x.x);
-  l = to == -INFINITY ? 0.f : l * exp2_(m - to) + x.y * exp2_(x.x - to);
+  l = to == -INFINITY ? l + x.y : l * exp2_(m - to) + x.y * exp2_(x.x - to);
   m = to;
 }
 
@@ -719,7 +720,7 @@ __device__ __forceinline__ float2 join_stats(const Queries &Q, int first, int pa
   for (int k = threadIdx.x & 63; k < parts; k += 64) add_stats(m, l, Q.stats[(long long)(first + k) * R + r]);
   float top = m;
   for (int d = 32; d > 0; d >>= 1) top = fmaxf(top, __shfl_xor(top, d));
-  float sum = top == -INFINITY ? 0.f : l * exp2_(m - top);
+  float sum = top == -INFINITY ? l : l * exp2_(m - top);
   for (int d = 32; d > 0; d >>= 1) sum += __shfl_xor(sum, d);
   return make_float2(top, sum);
 }

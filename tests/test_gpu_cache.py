@@ -221,6 +221,48 @@ def test_attention_infinite_values_that_are_seen(C, count, G, T, page, gain):
     assert torch.equal(o[..., :n], want.expand(1, 1, T, G, n)) and bool(torch.isfinite(o[..., n:]).all() & torch.isfinite(lse).all())
 
 
+def _room_for_logits(C, P, G, T):
+    """Tables so long that the logits of more than 32 rows would take more than 256 MB."""
+    wide = torch.full((P.B, 2 ** 28 // (4 * P.B * P.L * P.H * G * T * P.page) + 2), -1, dtype=torch.int32, device=DEV)
+    wide[:, :P.per] = P.tables
+    P.cache = C.Cache(P.k, P.v, wide, P.counts, P.seen, P.mass, P.positions)
+
+
+def _bad_weights(P, before, h, upto):
+    """The mass of head h: NaN of the slots below `upto`, as before of the others."""
+    idx = P.tables[0].long()
+    mass, was = (t[idx, 0, h].reshape(-1) for t in (P.mass, before["mass"]))
+    return bool(torch.isnan(mass[:upto]).all()) and torch.equal(mass[upto:], was[upto:])
+
+
+@pytest.mark.parametrize("G", [1, 4, 16, 17, 40, 64])
+@pytest.mark.parametrize("n,page", [(1, 16), (40, 24), (300, 16), (9001, 64)])
+@pytest.mark.parametrize("room", [False, True])
+def test_attention_of_logits_that_are_none(C, G, n, page, room):
+    """A query that holds a NaN, and keys that all do: out, lse and the weights are NaN, not those of a query that sees nothing.
+    Heads: 0 has numbers only, 1 a query with a NaN, of 2 all keys have one, of 3 a stretch of keys of the length of any part of it."""
+    P = U.Paged(C, DEV, [[[n] * 4]], page=page)
+    if room:
+        _room_for_logits(C, P, G, 1)
+    q = _queries(P, 1, 4 * G)
+    q[0, 0, 0, G + G // 2, 77] = float("nan")
+    at = torch.arange(n)
+    at = at[(at >= n // 3) & (at < n // 3 + max(1, min(2600, n // 2)))]
+    p = P.tables[0].cpu().long()[at // page]
+    P.k[p.to(DEV), 0, (at % page).to(DEV), 3, 5] = float("nan")
+    P.k[:, :, :, 2, 9] = float("nan")
+    before = P.snapshot()
+    out, lse = C.compactor_cache_attention(P.cache, q, accumulate=True, want_lse=True)
+    torch.cuda.synchronize()
+    bad = torch.zeros(4 * G, dtype=torch.bool, device=DEV)
+    bad[G + G // 2], bad[2 * G:] = True, True
+    assert torch.equal(torch.isnan(lse[0, 0, 0]), bad) and bool(torch.isfinite(lse[0, 0, 0, ~bad]).all())
+    assert torch.equal(torch.isnan(out[0, 0, 0].float()), bad.view(-1, 1).expand(4 * G, 128))
+    for h in (1, 2, 3):
+        assert _bad_weights(P, before, h, n), h
+    assert bool(torch.isfinite(P.mass[:, 0, 0]).all())
+
+
 def _weights_that_need_24_bits(n):
     """n logits x in (-1, 0), exact in bf16, whose weights w = e^x are 2^-19 or more away from the sum of two bf16 numbers.
     -> x, the two numbers, w"""
