@@ -210,6 +210,13 @@ __device__ __forceinline__ void finish_row(const CacheView &C, const Queries &Q,
         sum == 0.f ? -INFINITY : LN2 * (m + __builtin_amdgcn_logf(sum));
 }
 
+// What a row's weights are relative to (base 2), inf for a row that has none.  The weights of a row whose sum is NaN are NaN at every slot that
+// it sees and at no other: it counts as a row without weights, and *none becomes the most slots that such a row sees.
+__device__ __forceinline__ float weights_from(const Queries &Q, int count, int n, int r, float m, float sum, int *none) {
+  if (sum != sum) atomicMax(none, sees(count, n, r / Q.group));
+  return sum > 0.f ? m + __builtin_amdgcn_logf(sum) : INFINITY;
+}
+
 // Weights of the head's slots s .. s + 3, s a multiple of 4, on the way to their mass: what does not depend on the rows' sums leaves
 // early (the mass, and the logits of the first MASS_ROWS rows).
 constexpr int MASS_ROWS = 4;
@@ -232,8 +239,8 @@ __device__ __forceinline__ void mass_fetch(const CacheView &C, const Queries &Q,
     M.old[i] = *M.mass[i];
   }
 }
-// 1/G sum over rows of 2^(x - lse2), lse2 = inf for a row without weights.
-__device__ __forceinline__ void mass_add(const Queries &Q, const float *lse2, const float *logits, int R, int s, const MassQuad &M) {
+// 1/G sum over rows of 2^(x - lse2), lse2 and none: weights_from().
+__device__ __forceinline__ void mass_add(const Queries &Q, const float *lse2, int none, const float *logits, int R, int s, const MassQuad &M) {
   const float inv = 1.f / (float)Q.group;
   f32x4 sum = f32x4{0.f, 0.f, 0.f, 0.f};
   auto row = [&](int r, const f32x4 &x) {
@@ -248,7 +255,7 @@ __device__ __forceinline__ void mass_add(const Queries &Q, const float *lse2, co
   for (int r = MASS_ROWS; r < R; ++r) row(r, *reinterpret_cast<const f32x4 *>(logits + (long long)r * Q.pitch + s));
 #pragma unroll
   for (int i = 0; i < 4; ++i)
-    if (M.there[i]) *M.mass[i] = fmaf(sum[i], inv, M.old[i]);
+    if (M.there[i]) *M.mass[i] = s + i < none ? NAN : fmaf(sum[i], inv, M.old[i]);
 }
 
 // Logits leave for the workspace 16 bytes a lane, or by way of LDS in whole lines, a run of tiles of a row at a time; up to 16 rows that pays
@@ -261,6 +268,7 @@ struct AttendLds {
   float kept[ATT_WAVES][kept_in_lds<NT> ? KEPT_FLOATS : 4], p[ATT_WAVES][16][ATT_TILE + 1];
   float m[ATT_WAVES][16 * NT], l[ATT_WAVES][16 * NT];
   float lse2[16 * NT];
+  int none;
 };
 
 // Steps of ATT_STEP slots of a head: one at least, so that every head has a workgroup that writes its rows.
@@ -436,6 +444,7 @@ __global__ __launch_bounds__(256, NT <= 2 ? 2 : 1) void attend_kernel(const Cach
   const HeadPlace hp = head_place(C, w);
   const int count = part.count, n = part.n;
   const bool complete = part.parts == 1;
+  if (tid == 0) L.none = 0;
   const Run run = run_of(part, wave);
   const int first = run.first, tiles = run.tiles;
   const int seen_by_all = count - (n - 1);
@@ -681,7 +690,7 @@ __global__ __launch_bounds__(256, NT <= 2 ? 2 : 1) void attend_kernel(const Cach
     if (row < R) {
       if (complete) {
         finish_row(C, Q, w, row, ch, o, mm, sum);
-        if (ch == 0) L.lse2[row] = sum == 0.f ? INFINITY : mm + __builtin_amdgcn_logf(sum);
+        if (ch == 0) L.lse2[row] = weights_from(Q, count, n, row, mm, sum, &L.none);
         if (ch == 0 && Q.weights != nullptr) Q.stats[(long long)fragment * R + row] = make_float2(mm, sum);
       } else {
         const long long at = (long long)fragment * R + row;
@@ -699,7 +708,7 @@ __global__ __launch_bounds__(256, NT <= 2 ? 2 : 1) void attend_kernel(const Cach
     for (int at = 4 * tid; at < count; at += 4 * 256) {
       MassQuad M;
       mass_fetch(C, Q, hp, logits, R, at, count, M);
-      mass_add(Q, L.lse2, logits, R, at, M);
+      mass_add(Q, L.lse2, L.none, logits, R, at, M);
     }
   }
 }
@@ -725,8 +734,8 @@ __device__ __forceinline__ float2 join_stats(const Queries &Q, int first, int pa
   return make_float2(top, sum);
 }
 
-// What every row's weights are relative to, by a workgroup; stats: 256 entries.
-__device__ __forceinline__ void row_sums(const Queries &Q, const Fragment &f, int R, float2 *stats, float *lse2) {
+// What every row's weights are relative to, by a workgroup; stats: 256 entries; *none is 0 to all of it.
+__device__ __forceinline__ void row_sums(const Queries &Q, const Fragment &f, int R, float2 *stats, float *lse2, int *none) {
   const int tid = threadIdx.x;
   // Up to 16 rows the waves take rows in turn, their lanes fragments (4 rows, 2.3 M slots: 248 us a call, in the other way 250);
   // more of them all at once: thread (group, row) takes every groups-th fragment, the first R threads add up the groups' (28 rows,
@@ -734,7 +743,7 @@ __device__ __forceinline__ void row_sums(const Queries &Q, const Fragment &f, in
   if (R <= 16) {
     for (int r = tid >> 6; r < R; r += 4) {
       const float2 all = join_stats(Q, f.first, f.parts, R, r);
-      if ((tid & 63) == 0) lse2[r] = all.y == 0.f ? INFINITY : all.x + __builtin_amdgcn_logf(all.y);
+      if ((tid & 63) == 0) lse2[r] = weights_from(Q, f.count, f.n, r, all.x, all.y, none);
     }
   } else {
     const int groups = (int)(256u / (unsigned)R), group = (int)((unsigned)tid / (unsigned)R), r = tid - group * R;
@@ -746,7 +755,7 @@ __device__ __forceinline__ void row_sums(const Queries &Q, const Fragment &f, in
     if (tid < R) {
 #pragma unroll 4
       for (int i = 1; i < min(groups, f.parts); ++i) add_stats(m, l, stats[i * R + tid]);
-      lse2[tid] = l == 0.f ? INFINITY : m + __builtin_amdgcn_logf(l);
+      lse2[tid] = weights_from(Q, f.count, f.n, tid, m, l, none);
     }
   }
 }
@@ -754,6 +763,7 @@ __device__ __forceinline__ void row_sums(const Queries &Q, const Fragment &f, in
 __global__ __launch_bounds__(256) void attend_join_kernel(const CacheView C, const Queries Q) {
   __shared__ float part_o[16][D + 4], lse2[MOST_ROWS];
   __shared__ float2 stats[256];                     // of the groups of more than 16 rows
+  __shared__ int none;
   const int tid = threadIdx.x, R = Q.tokens * Q.group;
   const unsigned rows = (unsigned)C.nreq * (unsigned)C.layers * (unsigned)C.kv_heads * (unsigned)R;
   if (blockIdx.x < rows) {
@@ -791,13 +801,15 @@ __global__ __launch_bounds__(256) void attend_join_kernel(const CacheView C, con
   const float *logits = Q.logits + (long long)f.head * R * Q.pitch;
   const int from = f.step0 * ATT_STEP, to = min(f.step1 * ATT_STEP, f.count);
   if (from >= to) return;
+  if (tid == 0) none = 0;
+  __syncthreads();
   MassQuad M;
   mass_fetch(C, Q, hp, logits, R, min(from + 4 * tid, (to - 1) & ~3), to, M);
-  row_sums(Q, f, R, stats, lse2);
+  row_sums(Q, f, R, stats, lse2, &none);
   __syncthreads();
   for (int at = from + 4 * tid; at < to; at += 4 * 256) {
     if (at >= from + 4 * 256) mass_fetch(C, Q, hp, logits, R, at, to, M);
-    mass_add(Q, lse2, logits, R, at, M);
+    mass_add(Q, lse2, none, logits, R, at, M);
   }
 }
 
@@ -808,10 +820,13 @@ template <int NT, bool PAGE16>
 __global__ __launch_bounds__(256) void attend_mass_kernel(const CacheView C, const Queries Q) {
   __shared__ float2 stats[256];
   __shared__ float lse2[MOST_ROWS];
+  __shared__ int none;
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, n16 = lane & 15, j = lane >> 4;
   const int R = Q.tokens * Q.group;
   const Fragment part = Q.frags[blockIdx.x];
   if (part.head < 0 || part.n <= 0 || part.count > Q.most) return;
+  if (tid == 0) none = 0;
+  __syncthreads();
   const HeadOf w = head_of(C, (unsigned)part.head);
   const HeadPlace hp = head_place(C, w);
   const int count = part.count, seen_by_all = count - (part.n - 1);
@@ -840,7 +855,7 @@ __global__ __launch_bounds__(256) void attend_mass_kernel(const CacheView C, con
     load_rows<PAGE16, true>(kp, P, 0, lane, k_at, stride, k);
     there = tile_there(0);
   }
-  row_sums(Q, part, R, stats, lse2);
+  row_sums(Q, part, R, stats, lse2, &none);
   __syncthreads();
   float z[NT];
 #pragma unroll
@@ -926,7 +941,7 @@ __global__ __launch_bounds__(256) void attend_mass_kernel(const CacheView C, con
     mass_fetch(C, Q, hp, weights, 1, at, run.end, M);
 #pragma unroll
     for (int i = 0; i < 4; ++i)
-      if (M.there[i]) *M.mass[i] = fmaf(M.x[0][i], inv, M.old[i]);
+      if (M.there[i]) *M.mass[i] = at + i < none ? NAN : fmaf(M.x[0][i], inv, M.old[i]);
   }
 }
 

@@ -263,6 +263,43 @@ def test_attention_of_logits_that_are_none(C, G, n, page, room):
     assert bool(torch.isfinite(P.mass[:, 0, 0]).all())
 
 
+@pytest.mark.parametrize("G,T,new", [(1, 2, 2), (4, 3, 3), (4, 5, 4), (7, 6, 6), (8, 8, 8), (2, 17, 9)])
+@pytest.mark.parametrize("n,page", [(20, 16), (300, 24), (9001, 64)])
+@pytest.mark.parametrize("room", [False, True])
+def test_attention_weights_of_none_end_where_their_query_looks(C, G, T, new, n, page, room):
+    """Of several new tokens the earlier ones' queries hold a NaN: the weights of the tokens behind the last of those are numbers, the sums
+    over the other queries."""
+    P = U.Paged(C, DEV, [[[n]]], page=page)
+    if room:
+        _room_for_logits(C, P, G, T)
+    q = _queries(P, T, G)
+    last = (new - 1) // 2
+    q[0, 0, 0, 0, 3], q[0, 0, last, G - 1, 90] = float("nan"), float("nan")
+    before = P.snapshot()
+    out, lse = C.compactor_cache_attention(P.cache, q, new_tokens=_new([new]), accumulate=True, want_lse=True)
+    torch.cuda.synchronize()
+    see = O.sees(n, new, T)
+    idx = P.tables[0].long()
+    mass, was = (t[idx, 0, 0].reshape(-1).double().cpu().numpy() for t in (P.mass, before["mass"]))
+    assert np.isnan(mass[:see[last]]).all() and np.array_equal(mass[n:], was[n:])
+    k, v, _, _, there = P.head(0, 0, 0)
+    qd, od = U.f64(q), U.f64(out)
+    weight, slack = np.zeros(P.capacity), np.zeros(P.capacity)
+    for t in range(T):
+        for g in range(G):
+            if (t, g) in ((0, 0), (last, G - 1)):
+                assert np.isnan(od[0, 0, t, g]).all() and bool(torch.isnan(lse[0, 0, t, g]))
+                continue
+            want, _, p = O.attend(qd[0, 0, t, g], k, v, see[t], there, 128 ** -0.5, 0.0)
+            b_out, _, rel = U.attention_bounds(qd[0, 0, t, g], k, v, see[t], there, 128 ** -0.5, 0.0, want, p)
+            assert np.all(np.abs(od[0, 0, t, g] - want) <= b_out)
+            weight += p / G
+            slack += p / G * (rel + 2 * U.STEP32)
+    at = slice(see[last], n)
+    bound = slack + (T * G + 2) * U.STEP32 * (weight + np.abs(was)) + 2.0 ** -120
+    assert n > see[last] and np.all(np.abs(mass - was - weight)[at] <= bound[at])
+
+
 def _weights_that_need_24_bits(n):
     """n logits x in (-1, 0), exact in bf16, whose weights w = e^x are 2^-19 or more away from the sum of two bf16 numbers.
     -> x, the two numbers, w"""
