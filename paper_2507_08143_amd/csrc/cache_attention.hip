@@ -21,6 +21,7 @@
 #include <type_traits>
 
 #include "cache.h"
+#include "fragments.h"
 
 namespace cmp {
 
@@ -32,10 +33,6 @@ constexpr int ATT_TILE = 32;                 // slots a wave takes at a time
 constexpr int ATT_WAVES = 4;
 constexpr int ATT_STEP = ATT_TILE * ATT_WAVES;
 constexpr int MOST_ROWS = 64;                // query rows of a head: G * T
-constexpr int ATT_LEAST_LOG = 2;             // fewest steps of a fragment where there are many, log 2
-constexpr int SCAN_HEADS = 512, SCAN_ROUNDS = 6;        // heads that a wave looks through, and fragments for every workgroup that
-                                             // there is room for on the chip
-constexpr int ATT_EVEN = 256, EVEN_PARTS = 4;          // units that have equal parts of heads of one length, and most parts of a head then
 constexpr int SPLIT_ALL = 4096, SPLIT_MOST = 8;        // more heads: parts of all of them, and of one, at most
 constexpr int ATT_ALONE = 8;                 // steps of a head up to which one workgroup takes all of it
 // Weights are found from K instead of from logits that are more than the last cache holds (us with K / logits: 96 heads of 18000, 64 rows 336 / 435, 40 rows
@@ -313,20 +310,7 @@ __device__ __forceinline__ bool scan_part(const CacheView &C, const Queries &Q, 
   }
   const int total = __builtin_amdgcn_readlane(wave_scan(mine), 63);          // the host has seen to it that this fits
   longest = (int)__builtin_amdgcn_readlane(wave_max_up((unsigned)longest), 63);
-  // More than 16 query rows make a step dearer and a start too, and more than 32 leave room for one workgroup a unit: fewer steps where all
-  // find room at once (16 heads of 500 to 1411, 40 rows: 34 us with 4 steps, 30 with 1; one of 20000, 64 rows, 27 and 23; up to 16 rows
-  // the join costs as much), and twice as many where there is enough for all (24 heads of 18000, 40 rows: 84 us with 4 steps, 64 with 8;
-  // 96 heads of 900 to 9800, 20 rows, 72 and 67).
-  const bool many_rows = Q.tokens * Q.group > 16;
-  int log = many_rows ? 0 : ATT_LEAST_LOG, per = 0;        // steps of a fragment: 1 << log, or `per` where that is not 0
-  while (log < ATT_LEAST_LOG && total >> log > ATT_EVEN) ++log;
-  while ((total - 1) >> log >= Q.target) ++log;
-  if (many_rows && log == ATT_LEAST_LOG && total >> (log + 1) >= ATT_EVEN) ++log;
-  if (10ll * total >= 9ll * longest * heads)
-    for (int parts = 1; parts <= EVEN_PARTS && per == 0; ++parts) {
-      const int wgs = heads * parts, over = wgs % ATT_EVEN;
-      if (wgs <= 2 * ATT_EVEN && (over == 0 || 10 * over >= 9 * ATT_EVEN)) per = max(1 << ATT_LEAST_LOG, (int)((unsigned)(longest + parts - 1) / (unsigned)parts));
-    }
+  const FragmentRule rule = fragment_rule(total, longest, heads, Q.tokens * Q.group, Q.target);
   int before = 0;
   for (int h0 = 0; h0 < heads; h0 += 64 * SCAN_GROUP) {
     if (h0 > 0) fetch(h0);
@@ -334,16 +318,11 @@ __device__ __forceinline__ bool scan_part(const CacheView &C, const Queries &Q, 
     for (int i = 0; i < SCAN_GROUP; ++i) {
       if (i > 0 && h0 + 64 * i >= heads) break;
       const int steps = steps_at(h0, i);
-      int parts = (steps + (1 << log) - 1) >> log;
-      if (per > 0) {
-        parts = 0;
-#pragma unroll
-        for (int k = 0; k < EVEN_PARTS; ++k) parts += steps > k * per;
-      }
+      const int parts = fragments_of(steps, rule);
       const int upto = before + wave_scan(parts);
       const unsigned long long beyond = __ballot(upto > fragment);
       if (beyond != 0) {
-        const int at = __builtin_ctzll(beyond), each = per > 0 ? per : 1 << log;
+        const int at = __builtin_ctzll(beyond), each = rule.per > 0 ? rule.per : 1 << rule.log;
         F.head = h0 + 64 * i + at;
         F.count = __builtin_amdgcn_readlane(size[i].count, at);
         F.n = __builtin_amdgcn_readlane(size[i].n, at);
@@ -981,8 +960,8 @@ static AttendPlan attend_plan(const CacheView &C, const compactor_cache_query_t 
   A.target = A.frags_most = 0;
   // a wave adds up the steps of heads that may hold more than `most`, and their fragments have to fit all the same
   if (steps > ATT_ALONE && heads <= SCAN_HEADS && heads * (((long long)C.capacity + ATT_STEP - 1) / ATT_STEP) <= 0x7fffffffll) {
-    A.target = (int)std::min((long long)SCAN_ROUNDS * (A.rows <= 32 ? 2 : 1) * cus, std::max(((heads * steps - 1) >> ATT_LEAST_LOG) + 1, 2ll * ATT_EVEN));
-    A.frags_most = A.target + (int)heads;
+    A.target = fragment_target(heads, steps, A.rows, cus);
+    A.frags_most = fragments_most((int)heads, A.target);
   } else if (steps > ATT_ALONE) {
     A.split = (int)std::max(std::min(std::min(SPLIT_ALL / heads, (long long)SPLIT_MOST), ((steps - 1) >> ATT_LEAST_LOG) + 1), 1ll);
     if (A.split > 1) A.frags_most = A.split * (int)heads;

@@ -1,5 +1,6 @@
 // The host side of the kernels' index and key arithmetic, for test_device_math.py.
 #include "common.h"
+#include "fragments.h"
 
 extern "C" {
 long long inplace_row(int run, int run_rows, int row_of_run) { return cmp::inplace_row(run, run_rows, row_of_run); }
@@ -19,5 +20,18 @@ int bin_bits(int bin, int fine, unsigned *lo) {
   const cmp::BinKeys k = cmp::bin_keys(bin, fine != 0);
   *lo = k.lo;
   return k.bits;
+}
+int fragments_launched(int heads, int steps, int rows, int units) {
+  return cmp::fragments_most(heads, cmp::fragment_target(heads, steps, rows, units));
+}
+int fragments_made(const int *steps, int heads, int promised, int rows, int units) {
+  int total = 0, longest = 0, made = 0;
+  for (int h = 0; h < heads; ++h) {
+    total += steps[h];
+    longest = steps[h] > longest ? steps[h] : longest;
+  }
+  const cmp::FragmentRule r = cmp::fragment_rule(total, longest, heads, rows, cmp::fragment_target(heads, promised, rows, units));
+  for (int h = 0; h < heads; ++h) made += cmp::fragments_of(steps[h], r);
+  return made;
 }
 }

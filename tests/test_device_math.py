@@ -100,3 +100,19 @@ def test_sampled_lines_lie_inside_the_pool(M, n):
         assert at[0] >= 0 and first + 16 * at[-1] + 16 <= n and np.all(np.diff(at) >= 0)
         stretch = lines / groups
         assert np.all(np.abs(at + 0.5 - (np.arange(groups) + 0.5) * stretch) <= 0.5 * stretch + 1)
+
+
+@pytest.mark.parametrize("units", [32, 38, 48, 64, 80, 128, 256, 304])
+@pytest.mark.parametrize("rows", [1, 16, 17, 32, 33, 64])
+def test_every_fragment_of_attention_has_a_workgroup(M, units, rows):
+    """The fragments that the rule makes of any heads, as the device finds them, are no more than the host has launched workgroups and made
+    room for: for heads of one length, nearly one length and any, and for heads longer than was promised."""
+    rng = np.random.default_rng(rows * 1000 + units)
+    for heads in range(1, 513):
+        for promised in (9, 16, 141, 1000):
+            launched = M.fragments_launched(heads, promised, rows, units)
+            for steps in (np.full(heads, promised), rng.integers(max(1, promised - promised // 12), promised + 1, heads),
+                          rng.integers(1, promised + 1, heads), np.full(heads, 7 * promised)):
+                steps = np.ascontiguousarray(steps, dtype=np.int32)
+                made = M.fragments_made(steps.ctypes.data_as(C.POINTER(C.c_int)), heads, promised, rows, units)
+                assert heads <= made <= launched, (heads, promised, steps)
