@@ -332,6 +332,23 @@ def _stream(stream):
     return C.c_void_p(stream.cuda_stream)
 
 
+def _empty(stream, *shape, returned=True, **kw):
+    """torch.empty for a call on `stream` (None: the current one).  The block comes from the pool of that stream: one of the current
+    stream's pool may still be in use there by work that was enqueued before and has given it back.  returned: the caller gets
+    the tensor, so the block waits for the caller's stream too when it is given back."""
+    return _made_on(stream, lambda: torch.empty(*shape, **kw), returned)
+
+
+def _made_on(stream, make, returned=True):
+    if stream is None:
+        return make()
+    with torch.cuda.stream(stream):
+        t = make()
+    if returned and t.is_cuda:
+        t.record_stream(torch.cuda.current_stream(t.device))
+    return t
+
+
 def _device(reqs):
     return reqs[0].k_score.device
 
@@ -366,7 +383,7 @@ def compactor_srht_phi(sketch_dim: int, signs, cols, device, stream=None) -> tor
     cl = (C.c_int32 * len(cols))(*[int(x) for x in cols])
     _require(len(signs) == 128 and len(cols) == sketch_dim,
              "signs must hold 128 values and cols sketch_dim values")
-    phi = torch.empty(128, sketch_dim, dtype=torch.float32, device=device)
+    phi = _empty(stream, 128, sketch_dim, dtype=torch.float32, device=device)
     with torch.cuda.device(phi.device):
         _check(_lib.compactor_srht_phi(sketch_dim, sg, cl, _ptr(phi), _stream(stream)))
     return phi
@@ -396,11 +413,7 @@ def compactor_workspace_size(params: Params, reqs: Sequence[Request]) -> int:
 def _workspace(call, reqs, workspace, stream=None):
     if workspace is None:
         nbytes = max(256, _workspace_bytes(*call))
-        workspace = torch.empty(nbytes, dtype=torch.uint8, device=_device(reqs))
-        if stream is not None:
-            # the block is used on `stream`, not on the stream torch allocated it for: tell the
-            # allocator, or it may hand the block out again while the kernels still run
-            workspace.record_stream(stream)
+        workspace = _empty(stream, nbytes, dtype=torch.uint8, device=_device(reqs))
     return workspace
 
 
@@ -412,9 +425,9 @@ def compactor_score(params: Params, reqs: Sequence[Request], scores=None, status
     dev, nh = _device(reqs), n * params.layers * params.kv_heads
     given = scores, status, workspace          # what is allocated here needs no check
     if scores is None:
-        scores = torch.empty(so[-1], dtype=torch.float32, device=dev)
+        scores = _empty(stream, so[-1], dtype=torch.float32, device=dev)
     if status is None:
-        status = torch.empty(nh, dtype=torch.int32, device=dev)
+        status = _empty(stream, nh, dtype=torch.int32, device=dev)
     workspace = _workspace(call, reqs, workspace, stream)
     _check_gpu(params, reqs)
     _out(given[0], so[-1], torch.float32, "scores")
@@ -432,9 +445,9 @@ def compactor_select(params: Params, reqs: Sequence[Request], scores: torch.Tens
     so, ko, _ = _layout(*call)
     dev, nh = scores.device, n * params.layers * params.kv_heads
     if kept_idx is None:
-        kept_idx = torch.empty(ko[-1], dtype=torch.int32, device=dev)
+        kept_idx = _empty(stream, ko[-1], dtype=torch.int32, device=dev)
     if kept_cnt is None:
-        kept_cnt = torch.empty(nh, dtype=torch.int32, device=dev)
+        kept_cnt = _empty(stream, nh, dtype=torch.int32, device=dev)
     _check_gpu(params, reqs)
     workspace = _workspace(call, reqs, workspace, stream)
     _out(scores, so[-1], torch.float32, "scores")       # the scores' device decides where the others live
@@ -453,9 +466,9 @@ def compactor_compact(params: Params, reqs: Sequence[Request], kept_idx: torch.T
     _, ko, _ = _layout(*call)
     dev = _device(reqs)
     if k_packed is None:
-        k_packed = torch.empty(ko[-1], params.head_dim, dtype=torch.bfloat16, device=dev)
+        k_packed = _empty(stream, ko[-1], params.head_dim, dtype=torch.bfloat16, device=dev)
     if v_packed is None:
-        v_packed = torch.empty(ko[-1], params.head_dim, dtype=torch.bfloat16, device=dev)
+        v_packed = _empty(stream, ko[-1], params.head_dim, dtype=torch.bfloat16, device=dev)
     _check_gpu(params, reqs)
     _out(kept_idx, ko[-1], torch.int32, "kept_idx")
     _out(kept_cnt, n * params.layers * params.kv_heads, torch.int32, "kept_cnt")
@@ -508,17 +521,17 @@ def compactor_compress(params: Params, reqs: Sequence[Request], want_scores: boo
     # what is allocated here needs no check
     given = scores, kept_idx, kept_cnt, k_packed, v_packed, status, workspace
     if scores is None and want_scores:
-        scores = torch.empty(so[-1], dtype=torch.float32, device=dev)
+        scores = _empty(stream, so[-1], dtype=torch.float32, device=dev)
     if kept_idx is None:
-        kept_idx = torch.empty(ko[-1], dtype=torch.int32, device=dev)
+        kept_idx = _empty(stream, ko[-1], dtype=torch.int32, device=dev)
     if kept_cnt is None:
-        kept_cnt = torch.empty(nh, dtype=torch.int32, device=dev)
+        kept_cnt = _empty(stream, nh, dtype=torch.int32, device=dev)
     if k_packed is None:
-        k_packed = torch.empty(ko[-1], params.head_dim, dtype=torch.bfloat16, device=dev)
+        k_packed = _empty(stream, ko[-1], params.head_dim, dtype=torch.bfloat16, device=dev)
     if v_packed is None:
-        v_packed = torch.empty(ko[-1], params.head_dim, dtype=torch.bfloat16, device=dev)
+        v_packed = _empty(stream, ko[-1], params.head_dim, dtype=torch.bfloat16, device=dev)
     if status is None:
-        status = torch.empty(nh, dtype=torch.int32, device=dev)
+        status = _empty(stream, nh, dtype=torch.int32, device=dev)
     workspace = _workspace(call, reqs, workspace, stream)
     _check_gpu(params, reqs)
     for t, numel, dtype, name in zip(
@@ -609,12 +622,10 @@ def compactor_attention_scores(params: AttnParams, reqs: Sequence[AttnRequest], 
     total = sum(params.layers * params.kv_heads * r.k.shape[2] for r in reqs)
     given = attn, workspace                    # what is allocated here needs no check
     if attn is None:
-        attn = torch.empty(total, dtype=torch.float32, device=dev)
+        attn = _empty(stream, total, dtype=torch.float32, device=dev)
     if workspace is None:
-        workspace = torch.empty(max(256, compactor_attention_workspace_size(params, reqs)),
-                                dtype=torch.uint8, device=dev)
-        if stream is not None:
-            workspace.record_stream(stream)
+        workspace = _empty(stream, max(256, compactor_attention_workspace_size(params, reqs)), returned=False,
+                           dtype=torch.uint8, device=dev)
     arr = (_AttnRequest * len(reqs))(*[r.c(params) for r in reqs])
     _out(given[0], total, torch.float32, "attn")
     _out(given[1], 0, torch.uint8, "workspace")
@@ -716,9 +727,7 @@ class Cache:
             need = self._bytes[key] = out.value
         if need == 0:
             return 0, 0, None
-        given = torch.empty(need, dtype=torch.uint8, device=self.device)
-        if stream is not None:
-            given.record_stream(stream)      # used on `stream`, see _workspace()
+        given = _empty(stream, need, returned=False, dtype=torch.uint8, device=self.device)
         return given.data_ptr(), need, given
 
     def _on(self, stream, call):
@@ -816,11 +825,9 @@ def compactor_cache_attention(cache: Cache, q: torch.Tensor, new_tokens: Optiona
     query = _cache_query(cache, q, new_tokens, scale, softcap, accumulate, max_tokens)
     shape = q.shape
     if out is None:
-        out = torch.empty_like(q)      # (half of what torch.empty with a device takes)
+        out = _made_on(stream, lambda: torch.empty_like(q))      # (half of what torch.empty with a device takes)
         if out.stride(4) != 1:
-            out = torch.empty(shape, dtype=torch.bfloat16, device=cache.device)
-        if stream is not None:
-            out.record_stream(stream)
+            out = _empty(stream, shape, dtype=torch.bfloat16, device=cache.device)
     else:
         if out.dtype != torch.bfloat16 or out.shape != shape or out.stride(4) != 1 or out.device != cache.device:
             _refuse("out must be bfloat16 of q's shape on the GPU of the cache, the channel contiguous")
@@ -833,9 +840,7 @@ def compactor_cache_attention(cache: Cache, q: torch.Tensor, new_tokens: Optiona
         if lse.device != cache.device:
             _refuse("lse must live on the GPU of the cache")
     elif want_lse:
-        lse = q.new_empty(shape[:4], dtype=torch.float32)
-        if stream is not None:
-            lse.record_stream(stream)
+        lse = _made_on(stream, lambda: q.new_empty(shape[:4], dtype=torch.float32))
     query.lse = _ptr(lse)
     ref = C.byref(query)
     ptr, nbytes, _keep = cache._workspace(_lib.compactor_cache_attention_workspace_size, ref,
