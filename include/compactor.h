@@ -423,8 +423,8 @@ typedef struct compactor_cache_evict_params {
 } compactor_cache_evict_params_t;
 
 /* Brings caches down to their budgets.  Of a head (layer) that holds more tokens than its budget, the
- * first ones in this order stay: protected tokens, then larger mass first, NaN last; equal ones by
- * lower (head, slot).  Retained tokens in slots from the new count on move, in ascending order, to the slots
+ * first ones in this order stay: protected tokens, then larger mass first, NaN last, and behind all of
+ * these the tokens whose page is not there; equal ones by lower (head, slot).  Retained tokens in slots from the new count on move, in ascending order, to the slots
  * below it that were given up, in ascending order: K and V rows, mass and position (into a page that is not there:
  * nowhere).  All others stay
  * where they are, and so do the contents of slots that no token is in any more. */

@@ -41,12 +41,12 @@ def append(count: int, seen: int, new: int, capacity: int):
 
 
 def rank_keys(mass, pos, there, seen: int, sink: int, recent: int):
-    """What the slots of a head are ranked by, largest first: (class, mass), class 3 protected, 2 a number, 1 NaN or a
+    """What the slots of a head are ranked by, largest first: (class, mass), class 3 protected, 2 a number, 1 NaN, 0 a
     page that is not there."""
     keys = []
     for m, p, t in zip(mass, pos, there):
         if not t:
-            keys.append((1, 0.0))
+            keys.append((0, 0.0))
         elif p < sink or p >= seen - recent:
             keys.append((3, 0.0))
         elif np.isnan(m):

@@ -245,7 +245,8 @@ hipError_t launch_cache_admit(const SegTable &T, const CacheView &C, const int32
 // wave: 5.1 us, run a second time 2.9).  Parts of 8 waves with 8 units each: 8 heads of 26215
 // tokens 36 us, 32 layers of 79000 tokens 57; 4 with 16 41 and 60, 16 with 4 35 and 71.
 constexpr uint32_t KEY_PROTECTED = 0xffffffffu;      // above the key of +inf (0xff800000)
-constexpr uint32_t KEY_NO_NUMBER = 1u;               // NaN, or a page that is not there; below the key of -inf (0x007fffff).  0: no token
+constexpr uint32_t KEY_NO_NUMBER = 2u;               // NaN; below the key of -inf (0x007fffff)
+constexpr uint32_t KEY_NOT_THERE = 1u;               // the token's page is not there.  0: no token
 
 struct EvictPlan {
   int budget;
@@ -314,7 +315,7 @@ __device__ __forceinline__ void evict_keys(const CacheView &C, const HeadPlace &
 #pragma unroll
       for (int i = i0; i < i0 + 4; ++i) {
         const uint32_t rank = pos[i] < E.sink || pos[i] >= recent ? KEY_PROTECTED : score_key(mass[i]);
-        key[i] = first + 64 * i + lane < count ? max(page_there(C, page[i]) ? rank : 0u, KEY_NO_NUMBER) : 0u;
+        key[i] = first + 64 * i + lane < count ? (page_there(C, page[i]) ? max(rank, KEY_NO_NUMBER) : KEY_NOT_THERE) : 0u;
       }
   }
 }
@@ -460,7 +461,7 @@ __device__ __forceinline__ void clear_hist(int (&hist)[ALONE_BINS]) {
 static_assert(ALONE_BINS == 4 * ALONE_THREADS, "one store clears the tally");
 
 // Key of the last token that stays: its bin among 4096 of equal width between the least and the largest key that are neither
-// protected nor 0, so that bins are even whatever the weights' range; then among the few keys of the bin, or 4096 bins within it.
+// protected nor such as are ranked behind all, so that bins are even whatever the weights' range; then among the few keys of the bin, or 4096 bins within it.
 // units of the wave hold keys, `left` tokens stay; L.hist is clear.  -> key of the last one that stays, and how many of its equals stay
 __device__ __forceinline__ void find_last(AloneLds &L, const uint32_t (&key)[ALONE_UNITS], int units, int left, uint32_t &last, int &ties) {
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
@@ -492,8 +493,16 @@ __device__ __forceinline__ void find_last(AloneLds &L, const uint32_t (&key)[ALO
     last = KEY_PROTECTED;
     ties = left;
   } else if (left - kept > plain) {
-    last = KEY_NO_NUMBER;
+    int numberless = 0;                                    // all of those stay before a token that is not there does
+#pragma unroll
+    for (int i = 0; i < ALONE_UNITS; ++i)
+      if (i < units) numberless += __popcll(__ballot(key[i] == KEY_NO_NUMBER));
+    if (lane == 0) L.wave[2][wave] = numberless;
+    __syncthreads();
+    waves_before<ALONE_WAVES>(L.wave[2], wave, numberless);
     ties = left - kept - plain;
+    last = ties <= numberless ? KEY_NO_NUMBER : KEY_NOT_THERE;
+    if (ties > numberless) ties -= numberless;
   } else {
     uint32_t lo = ~least, hi = most;
     int want = left - kept;
@@ -650,7 +659,7 @@ __global__ __launch_bounds__(ALONE_THREADS) void evict_pool_kernel(const CacheVi
       key[i] = 0u;
       if (i < units) {
         const uint32_t rank = pos[i] < E.sink || pos[i] >= (int)__builtin_amdgcn_readlane(unit_recent, i) ? KEY_PROTECTED : score_key(mass[i]);
-        key[i] = base(i) + lane < count(i) ? max(page_there(C, page[i]) ? rank : 0u, KEY_NO_NUMBER) : 0u;
+        key[i] = base(i) + lane < count(i) ? (page_there(C, page[i]) ? max(rank, KEY_NO_NUMBER) : KEY_NOT_THERE) : 0u;
       }
     }
   }

@@ -59,6 +59,15 @@ def test_what_stays():
     assert O.evict_keep([a, b], 1) == [[1], []]
 
 
+def test_a_page_that_is_not_there_goes_before_a_weight_that_is_no_number():
+    mass = [float("nan"), 2.0, float("nan"), 2.0, -math.inf, 0.1]
+    keys = O.rank_keys(mass, [5, 6, 7, 8, 9, 3], [True, False, True, False, True, True], 10, 0, 0)
+    assert O.evict_keep([keys], 5) == [[0, 1, 2, 4, 5]]
+    assert O.evict_keep([keys], 4) == [[0, 2, 4, 5]]
+    assert O.evict_keep([keys], 3) == [[0, 4, 5]]
+    assert O.evict_keep([keys], 1) == [[5]]
+
+
 def test_moves():
     assert O.evict_moves([0, 1, 2], 5) == []
     assert O.evict_moves([2, 3, 4], 5) == [(0, 3), (1, 4)]

@@ -795,6 +795,25 @@ def test_evict_pages_that_are_not_there(C, scope):
     _check_evict(C, P, [90, 40], 3, 10, scope)
 
 
+@pytest.mark.parametrize("scope", [0, 1])
+@pytest.mark.parametrize("counts,page", [([[[150, 100, 45]], [[64, 200, 0]]], 16), ([[[5000, 3000, 9000]], [[12000, 1, 700]]], 64),
+                                         ([[[20000, 300, 17000]], [[40, 9000, 16384]]], 64)])
+@pytest.mark.parametrize("number", [0.0, 0.3])
+def test_evict_pages_that_are_not_there_beside_weights_that_are_none(C, scope, counts, page, number):
+    """Tokens whose page is not there go first, then those whose weight is NaN: budgets that end among either, and behind all of both."""
+    P = U.Paged(C, DEV, counts, page=page)
+    P.seen.fill_(100000)
+    g = torch.Generator(device=DEV)
+    g.manual_seed(12)
+    P.mass[torch.rand(P.mass.shape, generator=g, device=DEV) >= number] = float("nan")
+    P.positions.copy_(torch.randint(0, 99000, P.positions.shape, device=DEV, dtype=torch.int32, generator=g))
+    P.tables[0, ::3] = -1
+    P.tables[1, 1::2] = P.pages + 3
+    mean = [sum(c[0]) // 3 for c in counts]
+    for part in (0.9, 0.7, 0.5, 0.3, 0.1):
+        _check_evict(C, P, [max(1, int(part * m)) for m in mean], 2, 900, scope, what=str(part))
+
+
 def test_evict_more_tokens_than_promised(C):
     for scope in (0, 1):
         P = U.Paged(C, DEV, _counts(2, 1, 3, 150, 100, 45, 30, 20, 10), page=16)
