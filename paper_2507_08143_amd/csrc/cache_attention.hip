@@ -60,9 +60,8 @@ struct Queries {
   float scale, softcap;
   int target;                  // > 0: whole fragments that there are to be (scan_part)
   int split;                   // else: workgroups a head (split_part)
-  bool fragments;              // false: every workgroup has a whole head
-  Fragment *frags;
-  int2 *head_frags;            // [head]: its first fragment, and how many
+  Fragment *frags;             // null where nobody asks for them: every workgroup has a whole head, and no third launch follows
+  int2 *head_frags;            // [head]: its first fragment, and how many; null: every workgroup has a whole head
   float *partial;              // [fragment][row][D], relative to 2^m
   float2 *stats;               // [fragment][row]: m (base 2) and the sum of 2^(x - m)
   float *logits;               // accumulate: [head][row][pitch], base 2; else null
@@ -414,9 +413,9 @@ __global__ __launch_bounds__(256, NT <= 2 ? 2 : 1) void attend_kernel(const Cach
     if (tid == 0) Q.frags[fragment].head = -1;
     return;
   }
-  if (Q.fragments && tid == 0) {
+  if (Q.frags != nullptr && tid == 0) {
     Q.frags[fragment] = part;
-    if (part.step0 == 0) Q.head_frags[part.head] = make_int2(part.first, part.parts);
+    if (Q.head_frags != nullptr && part.step0 == 0) Q.head_frags[part.head] = make_int2(part.first, part.parts);
   }
   const unsigned g = (unsigned)part.head;
   const HeadOf w = head_of(C, g);
@@ -942,6 +941,7 @@ static int query_most(const CacheView &C, const compactor_cache_query_t *q) {
 
 struct AttendPlan {
   int rows, frags_most, target, split, pitch;
+  bool joined;                 // heads may have several fragments
   bool again;                  // weights from K, read again
   size_t frags, head_frags, partial, stats, logits;       // bytes, in this order in the workspace (logits: or weights)
   size_t bytes() const { return frags + head_frags + partial + stats + logits; }
@@ -966,6 +966,7 @@ static AttendPlan attend_plan(const CacheView &C, const compactor_cache_query_t 
     A.split = (int)std::max(std::min(std::min(SPLIT_ALL / heads, (long long)SPLIT_MOST), ((steps - 1) >> ATT_LEAST_LOG) + 1), 1ll);
     if (A.split > 1) A.frags_most = A.split * (int)heads;
   }
+  A.joined = A.frags_most > 0;
   A.pitch = (int)((most + ATT_TILE - 1) / ATT_TILE * ATT_TILE);
   const size_t a_row = (size_t)heads * A.pitch * sizeof(float);
   A.again = q->accumulate && A.rows > AGAIN_ROWS && a_row * A.rows > AGAIN_BYTES;
@@ -973,8 +974,8 @@ static AttendPlan attend_plan(const CacheView &C, const compactor_cache_query_t 
   auto up = [](size_t x) { return (x + 255) / 256 * 256; };
   const size_t n = A.frags_most;
   A.frags = up(n * sizeof(Fragment));
-  A.head_frags = n > 0 ? up((size_t)heads * sizeof(int2)) : 0;
-  A.partial = up(n * A.rows * D * sizeof(float));
+  A.head_frags = A.joined ? up((size_t)heads * sizeof(int2)) : 0;
+  A.partial = A.joined ? up(n * A.rows * D * sizeof(float)) : 0;
   A.stats = up(n * A.rows * sizeof(float2));
   A.logits = q->accumulate ? up(A.again ? a_row : a_row * A.rows) : 0;
   return A;
@@ -1032,7 +1033,7 @@ int compactor_cache_attention(const compactor_cache_t *cache, const compactor_ca
   if (need > 0 && (reinterpret_cast<uintptr_t>(workspace) & 255u)) return COMPACTOR_EALIGN;
   const long long heads = (long long)C.nreq * C.layers * C.kv_heads;
   const long long blocks = A.frags_most > 0 ? A.frags_most : heads;
-  const long long join = A.frags_most > 0 ? heads * A.rows + (query->accumulate && !A.again ? A.frags_most : 0) : 0;
+  const long long join = A.joined ? heads * A.rows + (query->accumulate && !A.again ? A.frags_most : 0) : 0;
   if (blocks > 0x7fffffffll || join > 0x7fffffffll) return COMPACTOR_EINVAL;
   Queries Q;
   Q.q = static_cast<const uint16_t *>(query->q);
@@ -1049,10 +1050,10 @@ int compactor_cache_attention(const compactor_cache_t *cache, const compactor_ca
   Q.softcap = query->softcap;
   Q.target = A.target;
   Q.split = A.split;
-  Q.fragments = A.frags_most > 0;
   unsigned char *ws = static_cast<unsigned char *>(workspace);
-  Q.frags = reinterpret_cast<Fragment *>(ws);
-  Q.head_frags = reinterpret_cast<int2 *>(ws += A.frags);
+  Q.frags = A.frags_most > 0 ? reinterpret_cast<Fragment *>(ws) : nullptr;
+  ws += A.frags;
+  Q.head_frags = A.joined ? reinterpret_cast<int2 *>(ws) : nullptr;
   Q.partial = reinterpret_cast<float *>(ws += A.head_frags);
   Q.stats = reinterpret_cast<float2 *>(ws += A.partial);
   ws += A.stats;
@@ -1068,7 +1069,7 @@ int compactor_cache_attention(const compactor_cache_t *cache, const compactor_ca
     launch_attend<true>(C, Q, (unsigned)blocks, st);
   else
     launch_attend<false>(C, Q, (unsigned)blocks, st);
-  if (A.frags_most > 0) {
+  if (A.joined) {
     if (hipGetLastError() != hipSuccess) return COMPACTOR_EHIP;
     hipLaunchKernelGGL(attend_join_kernel, dim3((unsigned)join), dim3(256), 0, st, C, Q);
   }

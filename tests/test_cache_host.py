@@ -139,6 +139,17 @@ def test_the_workspace_follows_max_tokens(B):
         assert sizes == sorted(sizes) and (sizes[0] > 0 and len(set(sizes)) == len(sizes) if some else set(sizes) == {0})
 
 
+@pytest.mark.parametrize("G,room", [(40, 1024), (64, 256), (64, 1024)])
+def test_no_workspace_for_a_join_of_heads_of_one_workgroup(B, G, room):
+    """Weights of many rows of many short heads: room for a weight a slot, a sum a row and what is known of a head, and for no partial outputs."""
+    heads = 16384
+    cache = _cache(B, nreq=heads // 8, table_len=room // 16, table_stride=room // 16)
+    q, n = _query(B, accumulate=1, q_heads=8 * G), C.c_size_t(0)
+    assert B._lib.compactor_cache_attention_workspace_size(C.byref(cache), C.byref(q), C.byref(n)) == 0
+    least = heads * (4 * room + 8 * G)
+    assert least <= n.value <= least + 64 * heads
+
+
 def test_bad_evictions(B):
     cache, n = _cache(B, table_len=300, table_stride=300), C.c_size_t(0)
     assert B._lib.compactor_cache_evict_workspace_size(C.byref(cache), C.byref(_evict(B, scope=1)), C.byref(n)) == 0 and n.value > 0
