@@ -333,7 +333,8 @@ int compactor_attention_scores(const compactor_attn_params_t *p,
  * page that is not there: its slots are seen by no query, written by no call and evicted first.
  * Pages that are named more than once (a common prefix of several contexts) may be attended to, but not be
  * appended to, accumulated into or evicted from.  A cache of one layer for calls layer by layer: layers = 1 and
- * every pointer moved to that layer. */
+ * every pointer moved to that layer.  Calls over so many heads that a launch would take 2^32 threads are refused (COMPACTOR_EINVAL): with
+ * some millions of heads in an eviction, tens of millions in an attention, hundreds of millions in an append. */
 typedef struct compactor_cache {
   compactor_page_pool_t pool;
   const int32_t *tables;  /* device, int32 [nreq][table_stride] */

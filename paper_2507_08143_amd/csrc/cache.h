@@ -105,6 +105,9 @@ __device__ __forceinline__ unsigned wave_max_up(unsigned x) {
   return x;
 }
 
+// Whether a launch has fewer than 2^32 threads, the most that HIP takes.  Checked before a call's first launch.
+inline bool launchable(long long blocks, int threads) { return blocks <= 0xffffffffll / threads; }
+
 // Checks a caller's cache (COMPACTOR_OK or an error) and makes the view of it.
 enum CacheNeed { CACHE_SIZES, CACHE_ROWS, CACHE_STATE };      // sizes only; pages and counts; and seen, mass, positions
 int cache_view(const compactor_cache_t *c, CacheNeed need, CacheView *view);

@@ -1014,7 +1014,7 @@ int compactor_cache_append(const compactor_cache_t *cache, const compactor_cache
             rows->stride_l, rows->stride_t, rows->stride_h, rows->new_tokens, rows->tokens};
   const long long heads = (long long)C.nreq * C.layers * C.kv_heads;
   const int parts = (int)(((long long)R.tokens + APPEND_ROWS - 1) / APPEND_ROWS);
-  if (R.tokens > APPEND_FEW && heads * parts > 0x7fffffffll) return COMPACTOR_EINVAL;
+  if (!launchable(R.tokens <= APPEND_FEW ? (heads + 15) / 16 : heads * parts, 256)) return COMPACTOR_EINVAL;
   hipStream_t st = static_cast<hipStream_t>(stream);
   (void)hipGetLastError();   // a leftover of earlier, unrelated HIP calls is not this call's error
   if (R.tokens <= APPEND_FEW) {
@@ -1058,6 +1058,7 @@ int compactor_cache_evict(const compactor_cache_t *cache, const compactor_cache_
   hipStream_t st = static_cast<hipStream_t>(stream);
   if (evict_alone(C, evict)) {
     E.most = evict_most(C, evict);
+    if (!launchable(heads / E.pool_heads, ALONE_THREADS)) return COMPACTOR_EINVAL;
     (void)hipGetLastError();
     if (E.pool_heads == 1)
       hipLaunchKernelGGL(evict_alone_kernel, dim3((unsigned)heads), dim3(ALONE_THREADS), 0, st, C, E);
@@ -1070,7 +1071,7 @@ int compactor_cache_evict(const compactor_cache_t *cache, const compactor_cache_
   evict_scratch(C, evict, static_cast<unsigned char *>(workspace), &E);
   long long movers = 2048 / heads;
   movers = movers < 1 ? 1 : (movers > 128 ? 128 : movers);
-  if (heads * E.parts > 0x7fffffffll) return COMPACTOR_EINVAL;
+  if (!launchable(heads * E.parts, PART_THREADS) || !launchable(heads * movers, MOVE_THREADS)) return COMPACTOR_EINVAL;
   const dim3 grid((unsigned)(heads * E.parts)), block(PART_THREADS);
   const long long clear = (reinterpret_cast<unsigned char *>(E.left) - reinterpret_cast<unsigned char *>(E.hist1)) / (long long)sizeof(int);
   const unsigned clear_wgs = (unsigned)std::min((clear + 1023) / 1024, 1024ll);

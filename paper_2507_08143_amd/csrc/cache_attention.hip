@@ -1034,7 +1034,7 @@ int compactor_cache_attention(const compactor_cache_t *cache, const compactor_ca
   const long long heads = (long long)C.nreq * C.layers * C.kv_heads;
   const long long blocks = A.frags_most > 0 ? A.frags_most : heads;
   const long long join = A.joined ? heads * A.rows + (query->accumulate && !A.again ? A.frags_most : 0) : 0;
-  if (blocks > 0x7fffffffll || join > 0x7fffffffll) return COMPACTOR_EINVAL;
+  if (!launchable(blocks, 256) || !launchable(join, 256)) return COMPACTOR_EINVAL;
   Queries Q;
   Q.q = static_cast<const uint16_t *>(query->q);
   Q.out = static_cast<uint16_t *>(query->out);

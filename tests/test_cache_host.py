@@ -150,6 +150,22 @@ def test_no_workspace_for_a_join_of_heads_of_one_workgroup(B, G, room):
     assert least <= n.value <= least + 64 * heads
 
 
+def test_calls_that_no_launch_can_take(B):
+    """2^32 threads or more: refused before anything is enqueued, not by a launch that fails."""
+    def cache(heads, **kw):
+        return _cache(B, nreq=heads // 8, **kw)
+
+    assert _append(B, cache(1 << 28), _rows(B)) == B.EINVAL
+    assert _append(B, cache(1 << 28), _rows(B, tokens=8)) == B.EINVAL
+    assert _append(B, cache(1 << 24), _rows(B, tokens=64)) == B.EINVAL
+    assert _append(B, cache(1 << 20), _rows(B, tokens=1024)) == B.EINVAL
+    assert _attend(B, cache(1 << 24), _query(B)) == B.EINVAL
+    assert _attend(B, cache(1 << 24, table_len=1000, table_stride=1000), _query(B)) == B.EINVAL
+    assert _evicts(B, cache(1 << 22), _evict(B)) == B.EINVAL
+    assert _evicts(B, cache(1 << 25), _evict(B, scope=1)) == B.EINVAL
+    assert _evicts(B, cache(1 << 20, table_len=2048, table_stride=2048), _evict(B), wsb=1 << 60) == B.EINVAL
+
+
 def test_bad_evictions(B):
     cache, n = _cache(B, table_len=300, table_stride=300), C.c_size_t(0)
     assert B._lib.compactor_cache_evict_workspace_size(C.byref(cache), C.byref(_evict(B, scope=1)), C.byref(n)) == 0 and n.value > 0
