@@ -223,6 +223,13 @@ def _out(t: Optional[torch.Tensor], numel: int, dtype, name: str):
         _refuse("%s must live on the GPU" % name)
 
 
+def _int32(**values):
+    """A number that the C structures would cut to its last 32 bits."""
+    for name, x in values.items():
+        if not 0 <= x < 1 << 31:
+            _refuse("%s must be one of 0 .. 2^31 - 1, got %s" % (name, x))
+
+
 SCOPE_HEAD, SCOPE_LAYER = 0, 1
 
 
@@ -789,6 +796,7 @@ def compactor_cache_append(cache: Cache, k: torch.Tensor, v: torch.Tensor,
         _refuse("v must have the shape and strides of k, the channel contiguous")
     if k.device != cache.device or v.device != cache.device:
         _refuse("k and v must live on the GPU of the cache")
+    _int32(tokens=T)
     rows = _CacheRows(k.data_ptr(), v.data_ptr(), sb, sl, st_, sh, cache._new_tokens(new_tokens), T)
     cache._on(stream, lambda st: _lib.compactor_cache_append(cache._ref, C.byref(rows), st))
 
@@ -803,6 +811,7 @@ def _cache_query(cache: Cache, q, new_tokens, scale, softcap, accumulate, max_to
                 % (tuple(q.shape), q.stride(), cache.nreq, cache.layers, cache._c.head_dim))
     if q.device != cache.device:
         _refuse("q must live on the GPU of the cache")
+    _int32(max_tokens=max_tokens)
     return _CacheQuery(q.data_ptr(), 0, 0, sb, sl, st, sh, 0, 0, 0, 0, cache._new_tokens(new_tokens), T, Hq, scale,
                        softcap, 1 if accumulate else 0, max_tokens)
 
@@ -859,11 +868,14 @@ def _cache_evict(cache: Cache, budget, budgets, sink, recent, scope, max_tokens)
         if budgets.device != cache.device:
             _refuse("budgets must live on the GPU of the cache")
         ptr = budgets.data_ptr()
-    return _CacheEvict(0 if budget is None else budget, ptr, sink, recent, scope, max_tokens)
+    budget = 0 if budget is None else budget
+    _int32(budget=budget, sink=sink, recent=recent, max_tokens=max_tokens)
+    return _CacheEvict(budget, ptr, sink, recent, scope, max_tokens)
 
 
 def compactor_cache_evict_workspace_size(cache: Cache, scope: int = SCOPE_HEAD, max_tokens: int = 0) -> int:
     out = C.c_size_t(0)
+    _int32(max_tokens=max_tokens)
     evict = _CacheEvict(0, 0, 0, 0, scope, max_tokens)
     _check(_lib.compactor_cache_evict_workspace_size(cache._ref, C.byref(evict), C.byref(out)))
     return int(out.value)

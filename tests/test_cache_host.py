@@ -276,3 +276,21 @@ def test_the_calls_check_their_tensors(B):
             B.compactor_cache_admit(*a, c)
     with pytest.raises(ValueError):
         B.compactor_cache_admit(p, reqs, idx, cnt, c, scores=_g(239))
+
+
+def test_numbers_that_do_not_fit_the_structures(B):
+    """A budget of 2^32 is not one of 0, and tokens protected without end are not unprotected."""
+    c = _handle(B)
+    q, k = _g(3, 2, 1, 8, 128, dtype=torch.bfloat16), _g(3, 2, 1, 4, 128, dtype=torch.bfloat16)
+    for x in (1 << 31, 1 << 32, (1 << 32) + 5, 1 << 63, -1):
+        for kw in (dict(budget=x), dict(budget=3, sink=x), dict(budget=3, recent=x), dict(budget=3, max_tokens=x)):
+            with pytest.raises(ValueError):
+                B.compactor_cache_evict(c, **kw)
+        with pytest.raises(ValueError):
+            B.compactor_cache_attention(c, q, max_tokens=x)
+        with pytest.raises(ValueError):
+            B.compactor_cache_attention_workspace_size(c, q, max_tokens=x)
+        with pytest.raises(ValueError):
+            B.compactor_cache_evict_workspace_size(c, max_tokens=x)
+    with pytest.raises(ValueError):
+        B.compactor_cache_append(c, *[k.expand(3, 2, (1 << 32) + 1, 4, 128)] * 2)
