@@ -829,7 +829,7 @@ def compactor_cache_attention(cache: Cache, q: torch.Tensor, new_tokens: Optiona
                               max_tokens: int = 0, want_lse: bool = False, out=None, lse=None,
                               workspace=None, stream=None):
     """Attention of the tokens appended last to the cache.  q: bf16 [request, layer, token, query head,
-    channel], any strides with the channel contiguous.  -> (out, bf16 of q's shape; lse, fp32
+    channel], any strides with the channel contiguous; out must not be the memory of q.  -> (out, bf16 of q's shape; lse, fp32
     [request, layer, token, query head], or None unless asked for or given)"""
     query = _cache_query(cache, q, new_tokens, scale, softcap, accumulate, max_tokens)
     shape = q.shape

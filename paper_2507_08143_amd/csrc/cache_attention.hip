@@ -1018,7 +1018,7 @@ int compactor_cache_attention(const compactor_cache_t *cache, const compactor_ca
   if (rc) return rc;
   rc = query_check(query, C);
   if (rc) return rc;
-  if (!query->q || !query->out) return COMPACTOR_EINVAL;
+  if (!query->q || !query->out || query->out == query->q) return COMPACTOR_EINVAL;
   if (query->q_stride_b < 0 || query->q_stride_l < 0 || query->q_stride_t < 0 || query->q_stride_h < 0 ||
       query->out_stride_b < 0 || query->out_stride_l < 0 || query->out_stride_t < 0 || query->out_stride_h < 0)
     return COMPACTOR_EINVAL;

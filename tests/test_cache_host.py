@@ -121,6 +121,11 @@ def test_bad_queries(B):
     assert B._lib.compactor_cache_attention_workspace_size(C.byref(cache), None, C.byref(n)) == B.EINVAL
 
 
+def test_attention_does_not_write_over_its_queries(B):
+    """They are read again, for the weights of many rows."""
+    assert _attend(B, _cache(B), _query(B, out=0x100000)) == B.EINVAL
+
+
 def test_the_workspace_follows_max_tokens(B):
     sizes = []
     for most in (1, 50, 160, 1000, 0):
