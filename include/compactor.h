@@ -392,7 +392,9 @@ typedef struct compactor_cache_query {
   float   softcap;        /* c > 0: a logit x becomes c * tanh(x / c); 0 = none (scale/c, and both times log2 e, finite) */
   int32_t accumulate;     /* not 0: adds the weights to the cache's mass */
   int32_t max_tokens;     /* tokens that no head holds more of, 0 = what the tables hold.  Launches and
-                             workspace go by it.  A head that holds more all the same is attended to in
+                             workspace go by it (accumulate: 4 bytes a token, head and query row, or without the query
+                             rows where there are more than 32 and that is more than 256 MB), so it pays where
+                             tables have much more room than heads hold.  A head that holds more all the same is attended to in
                              full, but its weights are not accumulated. */
 } compactor_cache_query_t;
 
@@ -401,7 +403,10 @@ typedef struct compactor_cache_query {
  *   x_s = scale * q . k_s (capped by softcap),  lse = ln sum_s exp(x_s),  p_s = exp(x_s - lse),
  *   out = sum_s p_s v_s,   mass[s] += 1/G sum over t and g of p_s   (accumulate).
  * A query that sees nothing, and a padding row (t >= n_b), gives zeros, lse -inf and no weight, whatever the
- * memory holds that it does not see.
+ * memory holds that it does not see.  A query with a logit that is NaN has NaN for out, lse and the weights of all that it sees.
+ * Sums are relative to the largest logit and divided once at the end: values of more than some 2^90 may overflow in them.
+ * Weights are added for every query of the call: a program that drops drafted tokens again sets counts and seen back itself, and what
+ * their queries have added stays in the mass.  Verify without accumulate where that matters.
  * softmax, weights and sums in fp32, out rounded once. */
 int compactor_cache_attention(const compactor_cache_t *cache, const compactor_cache_query_t *query,
                               void *workspace, size_t workspace_bytes, void *stream);

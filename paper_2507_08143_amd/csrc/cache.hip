@@ -243,7 +243,7 @@ hipError_t launch_cache_admit(const SegTable &T, const CacheView &C, const int32
 // What bounds both is not the 8 bytes of state a slot but the chain of steps and the instructions of each: a compute unit issues
 // one scalar instruction a cycle, and one vector instruction, for all its waves, and fetches what it runs for the first time (lists of 10 units a
 // wave: 5.1 us, run a second time 2.9).  Parts of 8 waves with 8 units each: 8 heads of 26215
-// tokens 36 us, 32 layers of 79000 tokens 57; 4 with 16 41 and 60, 16 with 4 35 and 71.
+// tokens 35 us, 32 layers of 79000 tokens 52 (when the three were compared 36 and 57; 4 with 16 41 and 60, 16 with 4 35 and 71).
 constexpr uint32_t KEY_PROTECTED = 0xffffffffu;      // above the key of +inf (0xff800000)
 constexpr uint32_t KEY_NO_NUMBER = 2u;               // NaN; below the key of -inf (0x007fffff)
 constexpr uint32_t KEY_NOT_THERE = 1u;               // the token's page is not there.  0: no token

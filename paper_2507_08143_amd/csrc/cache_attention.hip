@@ -35,8 +35,10 @@ constexpr int ATT_STEP = ATT_TILE * ATT_WAVES;
 constexpr int MOST_ROWS = 64;                // query rows of a head: G * T
 constexpr int SPLIT_ALL = 4096, SPLIT_MOST = 8;        // more heads: parts of all of them, and of one, at most
 constexpr int ATT_ALONE = 8;                 // steps of a head up to which one workgroup takes all of it
-// Weights are found from K instead of from logits that are more than the last cache holds (us with K / logits: 96 heads of 18000, 64 rows 336 / 435, 40 rows
-// 305 / 341; 24 such heads, whose logits stay near, 101 / 110 and 85 / 82; 96 of 900 to 9831, 40 rows, 99 / 92).
+// Weights of more than 32 rows are found from K instead of from logits that are more than the last cache holds: 256 bytes a slot read again, against 4
+// written and 4 read for every row.  us with K / logits: 96 heads of 18000, 64 rows 352 / 434, 40 rows 311 / 339, 32 rows 293 / 294, 28 rows 290 / 277, 20 rows
+// 283 / 253; 192 such heads, 64 rows 643 / 837, 32 rows 550 / 577, 28 rows 546 / 550, 20 rows 534 / 503; 24 of them, whose logits (110 MB for 64 rows) stay near, 64 rows
+// 106 / 110, 40 rows 87 / 87, 32 rows 74 / 69.
 constexpr int AGAIN_ROWS = 32;
 constexpr size_t AGAIN_BYTES = 256u << 20;
 constexpr float LOG2E = 1.4426950408889634f, LN2 = 0.6931471805599453f;
@@ -255,7 +257,7 @@ __device__ __forceinline__ void mass_add(const Queries &Q, const float *lse2, in
 }
 
 // Logits leave for the workspace 16 bytes a lane, or by way of LDS in whole lines, a run of tiles of a row at a time; up to 16 rows that pays
-// (2.3 M slots with 4 rows: 249 us and 255, without logits 221; streamed, or behind the last barrier: the same), with 20 rows 66 us and 64, with 40 158 and 102.
+// (with weights in 16 bits: 2.3 M slots with 4 rows: 249 us and 255, without logits 221; streamed, or behind the last barrier: the same), with 20 rows 66 us and 64, with 40 158 and 102.
 constexpr int KEPT_FLOATS = 2048;            // that a wave keeps: 4 tiles of 16 rows
 template <int NT> constexpr bool kept_in_lds = NT == 1;
 template <int NT>
@@ -983,7 +985,7 @@ static AttendPlan attend_plan(const CacheView &C, const compactor_cache_query_t 
 
 template <bool PAGE16>
 static void launch_attend(const CacheView &C, const Queries &Q, unsigned blocks, hipStream_t st) {
-  // tiles of 16 query rows (40 rows, 96 heads of 18000: 192 us with three, 204 with four)
+  // tiles of 16 query rows (40 rows, 96 heads of 18000: 208 us with three, 240 with four; 24 of them 62 and 72)
   const int rows = Q.tokens * Q.group;
   const auto kernel = rows <= 16   ? attend_kernel<1, PAGE16>
                       : rows <= 32 ? attend_kernel<2, PAGE16>

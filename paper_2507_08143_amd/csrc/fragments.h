@@ -18,9 +18,9 @@ struct FragmentRule { int log, per; };
 // total: steps of all heads; rows: query rows of a head; target: fragments that there are to be, beside the last of each head
 __host__ __device__ __forceinline__ FragmentRule fragment_rule(int total, int longest, int heads, int rows, int target) {
   // More than 16 query rows make a step dearer and a start too, and more than 32 leave room for one workgroup a unit: fewer steps where all
-  // find room at once (16 heads of 500 to 1411, 40 rows: 34 us with 4 steps, 30 with 1; one of 20000, 64 rows, 27 and 23; up to 16 rows
-  // the join costs as much), and twice as many where there is enough for all (24 heads of 18000, 40 rows: 84 us with 4 steps, 64 with 8;
-  // 96 heads of 900 to 9800, 20 rows, 72 and 67).
+  // find room at once (16 heads of 500 to 1411, 40 rows: 24 us with 4 steps, 19 with 1; one of 20000, 64 rows, 30 and 28; up to 16 rows
+  // the join costs as much), and twice as many where there is enough for all (24 heads of 18000, 40 rows: 80 us with 4 steps, 62 with 8,
+  // with weights 100 and 87; 96 heads of 18000 or of 900 to 9800: the same within 1 %).
   const bool many_rows = rows > 16;
   FragmentRule r{many_rows ? 0 : ATT_LEAST_LOG, 0};
   while (r.log < ATT_LEAST_LOG && total >> r.log > ATT_EVEN) ++r.log;
