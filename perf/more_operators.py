@@ -527,12 +527,12 @@ def _plain_reserve(s):
     i = torch.arange(P, device=dev)
     there = (tables >= 0) & (tables < N)
     named = torch.where(there, tables, 0).long()
-    shared = (i >= first.unsqueeze(1)) & (i < holds.unsqueeze(1)) & there & (refs[named] > 1)
+    shared = (i >= first.unsqueeze(1)) & (i < need.unsqueeze(1)) & there & (refs[named] > 1)
     fresh = (i >= holds.unsqueeze(1)) & (i < need.unsqueeze(1)) & ~there
-    b = torch.arange(B, device=dev).unsqueeze(1).expand(B, P)
+    entry = torch.arange(B * P, device=dev).view(B, P)
     tally = torch.zeros(N, dtype=torch.int64, device=dev).scatter_add_(0, named.flatten(), shared.flatten().long())
-    last = torch.full((N,), -1, device=dev).scatter_reduce_(0, named.flatten(), torch.where(shared, b, -1).flatten(), "amax")
-    copied = shared & ~((tally[named] == refs[named]) & (last[named] == b))      # the last of all that name a page keeps it
+    last = torch.full((N,), -1, device=dev).scatter_reduce_(0, named.flatten(), torch.where(shared, entry, -1).flatten(), "amax")
+    copied = shared & ~((tally[named] == refs[named]) & (last[named] == entry))  # the last entry of all that name a page keeps it
     wants = (copied | fresh).flatten()
     rank = wants.cumsum(0) - 1
     free = (refs != 0).to(torch.int8).sort(stable=True).indices
