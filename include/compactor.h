@@ -17,7 +17,8 @@
  * and, beyond that path: the attention-based scores a themselves (Sec. 3.2), head-adaptive
  * selection across the heads of a layer (Sec. 3.3), a paged destination for the compaction,
  * the Hadamard right-sketch of App. D, and what serving from the paged result needs: attention of
- * new tokens to it, appending, and eviction by accumulated attention weight.
+ * new tokens to it, appending, and eviction by accumulated attention weight; the same with the cache
+ * in 4 bits; norms and rotation of queries and keys in front of it; and the pages of caches that share them.
  *
  * General conventions
  *   - Every pointer marked "device" is GPU memory owned by the caller; every
@@ -440,6 +441,50 @@ int compactor_cache_evict(const compactor_cache_t *cache, const compactor_cache_
 /* Bytes of 256-byte aligned device workspace for compactor_cache_evict; scratch, no state is kept.  0 where none is needed.  host. */
 int compactor_cache_evict_workspace_size(const compactor_cache_t *cache,
                                          const compactor_cache_evict_params_t *evict, size_t *bytes);
+
+/* ---- the cache in 4 bits ------------------------------------------------------------------ */
+/* The same cache with rows of 64 bytes: channels in groups of 32, a channel a 4-bit floating point number (E2M1: 0, 0.5, 1, 1.5, 2, 3, 4, 6 and
+ * a sign; channel 2i is the low half of byte i), a group a scale that is a power of two (E8M0: byte s stands for 2^(s - 127), 255 for
+ * NaN), the OCP microscaling format MXFP4.  136 bytes a token of a head instead of 512.  The value of a number is exact in bf16.
+ * What is written: of a group whose largest magnitude is m 2^k (1 <= m < 2) the scale is 2^(k - 2), or 2^(k - 1) where m >= 1.75, so that
+ * every number is off by half a step at most; between 2^-125 and 2^125; numbers are rounded to the nearest, ties to the even code, and to 6
+ * beyond it.  A group with an infinity or a NaN becomes NaN, all 32 of it. */
+typedef struct compactor_mx_cache {
+  compactor_cache_t cache;   /* pool.k_pages and v_pages: 4-bit rows; the pool's strides are in bytes, multiples of 16,
+                                slot_stride >= 64.  The rest as in a cache of 16 bits; the state strides are needed even without state. */
+  uint32_t *k_scales, *v_scales;   /* device: the four scale bytes of a row, that of channels 0 .. 31 first, at the place of mass */
+} compactor_mx_cache_t;
+
+/* compactor_cache_append into it: rows come in bf16. */
+int compactor_mx_append(const compactor_mx_cache_t *cache, const compactor_cache_rows_t *rows, void *stream);
+
+/* Makes a cache in 4 bits of one in 16: rows, counts (cut to what the tables of `cache` name) and, where `cache` has them, seen, mass and
+ * positions, by logical slot; `source` is of as many requests, layers and heads, has state if `cache` has, and shares no memory with it.
+ * A token whose page is not there, in either, leaves its slot as it was: give it a page, or evict it first. */
+int compactor_mx_store(const compactor_mx_cache_t *cache, const compactor_cache_t *source, void *stream);
+
+/* Rows of a cache in bf16: what the numbers stand for, exactly. */
+typedef struct compactor_cache_rows_out {
+  void *k, *v;            /* device, bf16, addressed as in compactor_cache_rows */
+  int64_t stride_b, stride_l, stride_t, stride_h;
+  const int32_t *new_tokens;   /* as in compactor_cache_rows */
+  int32_t tokens;         /* T >= 1 */
+  int32_t first;          /* row t of request b is slot first + t of its heads; -1: slot counts - n_b + t, n_b = T or
+                             new_tokens[b] (the tokens that were appended last) */
+} compactor_cache_rows_out_t;
+/* Writes all T rows of every request and head: zeros for a padding row (t >= n_b), where a head has no such slot, and where its page
+ * is not there. */
+int compactor_mx_read(const compactor_mx_cache_t *cache, const compactor_cache_rows_out_t *rows, void *stream);
+
+/* compactor_cache_attention, to it.  Weights go into the product with V in 16 bits, their sums in fp32. */
+int compactor_mx_attention(const compactor_mx_cache_t *cache, const compactor_cache_query_t *query, void *workspace,
+                            size_t workspace_bytes, void *stream);
+int compactor_mx_attention_workspace_size(const compactor_mx_cache_t *cache, const compactor_cache_query_t *query, size_t *bytes);
+
+/* compactor_cache_evict, from it. */
+int compactor_mx_evict(const compactor_mx_cache_t *cache, const compactor_cache_evict_params_t *evict, void *workspace,
+                        size_t workspace_bytes, void *stream);
+int compactor_mx_evict_workspace_size(const compactor_mx_cache_t *cache, const compactor_cache_evict_params_t *evict, size_t *bytes);
 
 /* Context-calibrated retention (Sec. 3.4): the smallest r in (0,1] with
  * f(r) = (exp(r b - b) - exp(-b)) / (1 - exp(-b)) >= tau, b = alpha*nll + beta, i.e.

@@ -96,6 +96,16 @@ class _CacheEvict(C.Structure):
                 ("recent", C.c_int32), ("scope", C.c_int32), ("max_tokens", C.c_int32)]
 
 
+class _MxCache(C.Structure):
+    _fields_ = [("cache", _Cache), ("k_scales", C.c_void_p), ("v_scales", C.c_void_p)]
+
+
+class _CacheRowsOut(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("stride_b", C.c_int64), ("stride_l", C.c_int64),
+                ("stride_t", C.c_int64), ("stride_h", C.c_int64), ("new_tokens", C.c_void_p),
+                ("tokens", C.c_int32), ("first", C.c_int32)]
+
+
 _PP, _RP = C.POINTER(_Params), C.POINTER(_Request)
 _CP, _CQP, _CEP = C.POINTER(_Cache), C.POINTER(_CacheQuery), C.POINTER(_CacheEvict)
 _lib.compactor_cache_admit.argtypes = [_PP, _RP, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p, _CP,
@@ -105,6 +115,14 @@ _lib.compactor_cache_attention.argtypes = [_CP, _CQP, C.c_void_p, C.c_size_t, C.
 _lib.compactor_cache_attention_workspace_size.argtypes = [_CP, _CQP, C.POINTER(C.c_size_t)]
 _lib.compactor_cache_evict.argtypes = [_CP, _CEP, C.c_void_p, C.c_size_t, C.c_void_p]
 _lib.compactor_cache_evict_workspace_size.argtypes = [_CP, _CEP, C.POINTER(C.c_size_t)]
+_MXP = C.POINTER(_MxCache)
+_lib.compactor_mx_append.argtypes = [_MXP, C.POINTER(_CacheRows), C.c_void_p]
+_lib.compactor_mx_store.argtypes = [_MXP, _CP, C.c_void_p]
+_lib.compactor_mx_read.argtypes = [_MXP, C.POINTER(_CacheRowsOut), C.c_void_p]
+_lib.compactor_mx_attention.argtypes = [_MXP, _CQP, C.c_void_p, C.c_size_t, C.c_void_p]
+_lib.compactor_mx_attention_workspace_size.argtypes = [_MXP, _CQP, C.POINTER(C.c_size_t)]
+_lib.compactor_mx_evict.argtypes = [_MXP, _CEP, C.c_void_p, C.c_size_t, C.c_void_p]
+_lib.compactor_mx_evict_workspace_size.argtypes = [_MXP, _CEP, C.POINTER(C.c_size_t)]
 _APP, _ARP = C.POINTER(_AttnParams), C.POINTER(_AttnRequest)
 _lib.compactor_attention_workspace_size.argtypes = [_APP, _ARP, C.c_int32, C.POINTER(C.c_size_t)]
 _lib.compactor_attention_scores.argtypes = [_APP, _ARP, C.c_int32, C.c_void_p, C.c_void_p,
@@ -145,7 +163,9 @@ EXPORTS = ["compactor_default_params", "compactor_keep_count", "compactor_layout
            "compactor_attention_workspace_size", "compactor_attention_scores",
            "compactor_cache_admit", "compactor_cache_append", "compactor_cache_attention",
            "compactor_cache_attention_workspace_size", "compactor_cache_evict",
-           "compactor_cache_evict_workspace_size"]
+           "compactor_cache_evict_workspace_size",
+           "compactor_mx_append", "compactor_mx_store", "compactor_mx_read", "compactor_mx_attention",
+           "compactor_mx_attention_workspace_size", "compactor_mx_evict", "compactor_mx_evict_workspace_size"]
 
 
 STAGES = ["gram", "reduce", "solve", "score", "blend", "select", "gather"]
@@ -657,8 +677,13 @@ class Cache:
     def __init__(self, k_pages: torch.Tensor, v_pages: torch.Tensor, tables: torch.Tensor,
                  counts: torch.Tensor, seen: Optional[torch.Tensor] = None,
                  mass: Optional[torch.Tensor] = None, positions: Optional[torch.Tensor] = None):
-        _require(k_pages.dtype == torch.bfloat16 and v_pages.dtype == torch.bfloat16,
-                 "k_pages and v_pages must be bfloat16")
+        self._c = self._take(k_pages, v_pages, torch.bfloat16, tables, counts, seen, mass, positions)
+        self._c.head_dim = k_pages.shape[4]
+        self._ref = C.byref(self._c)
+
+    def _take(self, k_pages, v_pages, dtype, tables, counts, seen, mass, positions) -> _Cache:
+        if k_pages.dtype != dtype or v_pages.dtype != dtype:
+            _refuse("k_pages and v_pages must be %s" % str(dtype).split(".")[1])
         _require(k_pages.dim() == 5 and k_pages.stride(4) == 1 and v_pages.shape == k_pages.shape and
                  v_pages.stride() == k_pages.stride(),
                  "k_pages and v_pages must be [page, layer, slot, head, channel] views of equal shape and "
@@ -694,22 +719,26 @@ class Cache:
         self.k_pages, self.v_pages, self.tables, self.counts = k_pages, v_pages, tables, counts
         self.seen, self.mass, self.positions = seen, mass, positions
         self.nreq, self.layers, self.kv_heads = nreq, layers, heads
+        self._bytes = {}              # workspace sizes
         pool = _PagePool(k_pages.data_ptr(), v_pages.data_ptr(), k_pages.stride(0), k_pages.stride(1),
                          k_pages.stride(3), k_pages.stride(2), page_size, pages)
         st = mass.stride() if mass is not None else (0, 0, 0)
-        self._c = _Cache(pool, tables.data_ptr(), max(tables.stride(0), table_len), table_len, nreq, layers, heads,
-                         k_pages.shape[4], counts.data_ptr(), _ptr(seen), counts.stride(0), counts.stride(1),
-                         _ptr(mass), _ptr(positions), st[0], st[1], st[2])
-        self._ref = C.byref(self._c)
-        self._bytes = {}              # workspace sizes
+        return _Cache(pool, tables.data_ptr(), max(tables.stride(0), table_len), table_len, nreq, layers, heads, 128,
+                      counts.data_ptr(), _ptr(seen), counts.stride(0), counts.stride(1), _ptr(mass), _ptr(positions),
+                      st[0], st[1], st[2])
 
     def layer(self, first: int, count: int = 1) -> "Cache":
         """The cache of `count` layers from `first` on, for calls layer by layer."""
         _require(0 <= first and count >= 1 and first + count <= self.layers, "no such layers")
         at = slice(first, first + count)
         some = lambda t: None if t is None else t[:, at]      # noqa: E731
-        return Cache(self.k_pages[:, at], self.v_pages[:, at], self.tables, self.counts[:, at], some(self.seen),
-                     some(self.mass), some(self.positions))
+        return self._of(self.k_pages[:, at], self.v_pages[:, at], *[some(t) for t in self._scales], self.tables, self.counts[:, at],
+                        some(self.seen), some(self.mass), some(self.positions))
+
+    _scales = ()
+
+    def _of(self, *tensors):
+        return type(self)(*tensors)
 
     def _new_tokens(self, t: Optional[torch.Tensor]) -> int:
         if t is None:
@@ -749,11 +778,52 @@ class Cache:
                 _check(call(_stream(stream)))
 
 
+class MxCache(Cache):
+    """A Cache in 4 bits (see compactor_mx_cache_t), for the compactor_mx_* calls and those that take either kind.
+
+    k_pages, v_pages    uint8 views indexed [page, layer, slot, head, byte], 64 bytes a row, contiguous
+    k_scales, v_scales  uint8 views indexed [page, layer, head, slot, group], 4 bytes a slot, slots contiguous, both with the same
+                        strides: four times those of mass
+    The others as in Cache."""
+
+    def __init__(self, k_pages: torch.Tensor, v_pages: torch.Tensor, k_scales: torch.Tensor, v_scales: torch.Tensor,
+                 tables: torch.Tensor, counts: torch.Tensor, seen: Optional[torch.Tensor] = None,
+                 mass: Optional[torch.Tensor] = None, positions: Optional[torch.Tensor] = None):
+        cache = self._take(k_pages, v_pages, torch.uint8, tables, counts, seen, mass, positions)
+        pages, layers, page_size, heads, width = k_pages.shape
+        if width != 64:
+            _refuse("a row of k_pages must have 64 bytes, got %d" % width)
+        st = k_scales.stride()
+        for name, t in (("k_scales", k_scales), ("v_scales", v_scales)):
+            if (t.dtype != torch.uint8 or tuple(t.shape) != (pages, layers, heads, page_size, 4) or t.stride() != st or
+                    st[4] != 1 or (st[3] != 4 and page_size > 1) or any(x % 4 for x in st[:3])):
+                _refuse("%s must be uint8 [page, layer, head, slot, group] = [%d, %d, %d, %d, 4], slots of 4 bytes one behind the other, "
+                        "with the strides of k_scales" % (name, pages, layers, heads, page_size))
+            if any(n > 1 and x == 0 for n, x in zip(t.shape, st)):
+                _refuse("%s is written: its elements must not share memory" % name)
+            if t.device != self.device or not t.is_cuda:
+                _refuse("%s must live on the GPU of the page pool" % name)
+        if mass is not None and any(n > 1 and x != 4 * y for n, x, y in zip(mass.shape, st, mass.stride())):
+            _refuse("the strides of k_scales must be four times those of mass")
+        cache.state_page_stride, cache.state_layer_stride, cache.state_head_stride = (x // 4 for x in st[:3])
+        self.k_scales, self.v_scales = self._scales = k_scales, v_scales
+        self._mx = _MxCache(cache, k_scales.data_ptr(), v_scales.data_ptr())
+        self._c = self._mx.cache
+        self._ref = C.byref(self._mx)
+
+
+def _either(cache, mx: bool):
+    """The calls of one kind of rows do not read the other."""
+    if isinstance(cache, MxCache) != mx:
+        _refuse("this call is for a cache of %s bits" % ("4" if mx else "16"))
+
+
 def compactor_cache_admit(params: Params, reqs: Sequence[Request], kept_idx: torch.Tensor,
                           kept_cnt: torch.Tensor, cache: Cache, scores: Optional[torch.Tensor] = None,
                           stream=None):
     """State of the rows that compactor_compact_paged has written into the cache's pages: counts, seen,
     positions and, from the scores, mass."""
+    _either(cache, False)
     n = len(reqs)
     _require(n >= 1, "at least one request is needed")
     arr = (_Request * n)()                     # n and ratio are all that is looked at
@@ -785,6 +855,12 @@ def compactor_cache_append(cache: Cache, k: torch.Tensor, v: torch.Tensor,
     """Rows of new tokens into the cache.  k, v: bf16 [request, layer, token, kv head, channel], any
     strides with the channel contiguous, the same for both; new_tokens: int32 [request], how many of
     its rows each request brings (None: all)."""
+    _either(cache, False)
+    rows = _rows(cache, k, v, new_tokens)
+    cache._on(stream, lambda st: _lib.compactor_cache_append(cache._ref, C.byref(rows), st))
+
+
+def _rows(cache: Cache, k, v, new_tokens) -> _CacheRows:
     if k.dtype != torch.bfloat16 or k.dim() != 5 or v.dtype != torch.bfloat16:
         _refuse("k and v must be bfloat16 [request, layer, token, head, channel]")
     B, L, T, H, d = k.shape
@@ -797,8 +873,7 @@ def compactor_cache_append(cache: Cache, k: torch.Tensor, v: torch.Tensor,
     if k.device != cache.device or v.device != cache.device:
         _refuse("k and v must live on the GPU of the cache")
     _int32(tokens=T)
-    rows = _CacheRows(k.data_ptr(), v.data_ptr(), sb, sl, st_, sh, cache._new_tokens(new_tokens), T)
-    cache._on(stream, lambda st: _lib.compactor_cache_append(cache._ref, C.byref(rows), st))
+    return _CacheRows(k.data_ptr(), v.data_ptr(), sb, sl, st_, sh, cache._new_tokens(new_tokens), T)
 
 
 def _cache_query(cache: Cache, q, new_tokens, scale, softcap, accumulate, max_tokens):
@@ -816,12 +891,17 @@ def _cache_query(cache: Cache, q, new_tokens, scale, softcap, accumulate, max_to
                        softcap, 1 if accumulate else 0, max_tokens)
 
 
-def compactor_cache_attention_workspace_size(cache: Cache, q: torch.Tensor, accumulate: bool = False,
-                                             max_tokens: int = 0) -> int:
+def _attention_bytes(call, cache, q, accumulate, max_tokens) -> int:
     out = C.c_size_t(0)
     query = _cache_query(cache, q, None, 0.0, 0.0, accumulate, max_tokens)
-    _check(_lib.compactor_cache_attention_workspace_size(cache._ref, C.byref(query), C.byref(out)))
+    _check(call(cache._ref, C.byref(query), C.byref(out)))
     return int(out.value)
+
+
+def compactor_cache_attention_workspace_size(cache: Cache, q: torch.Tensor, accumulate: bool = False,
+                                             max_tokens: int = 0) -> int:
+    _either(cache, False)
+    return _attention_bytes(_lib.compactor_cache_attention_workspace_size, cache, q, accumulate, max_tokens)
 
 
 def compactor_cache_attention(cache: Cache, q: torch.Tensor, new_tokens: Optional[torch.Tensor] = None,
@@ -831,6 +911,12 @@ def compactor_cache_attention(cache: Cache, q: torch.Tensor, new_tokens: Optiona
     """Attention of the tokens appended last to the cache.  q: bf16 [request, layer, token, query head,
     channel], any strides with the channel contiguous; out must not be the memory of q.  -> (out, bf16 of q's shape; lse, fp32
     [request, layer, token, query head], or None unless asked for or given)"""
+    _either(cache, False)
+    return _attention(_lib.compactor_cache_attention, _lib.compactor_cache_attention_workspace_size, cache, q, new_tokens, scale,
+                      softcap, accumulate, max_tokens, want_lse, out, lse, workspace, stream)
+
+
+def _attention(call, size, cache, q, new_tokens, scale, softcap, accumulate, max_tokens, want_lse, out, lse, workspace, stream):
     query = _cache_query(cache, q, new_tokens, scale, softcap, accumulate, max_tokens)
     shape = q.shape
     if out is None:
@@ -852,9 +938,8 @@ def compactor_cache_attention(cache: Cache, q: torch.Tensor, new_tokens: Optiona
         lse = _made_on(stream, lambda: q.new_empty(shape[:4], dtype=torch.float32))
     query.lse = _ptr(lse)
     ref = C.byref(query)
-    ptr, nbytes, _keep = cache._workspace(_lib.compactor_cache_attention_workspace_size, ref,
-                                        (shape[2], shape[3], accumulate, max_tokens), workspace, stream)
-    cache._on(stream, lambda st: _lib.compactor_cache_attention(cache._ref, ref, ptr, nbytes, st))
+    ptr, nbytes, _keep = cache._workspace(size, ref, (shape[2], shape[3], accumulate, max_tokens), workspace, stream)
+    cache._on(stream, lambda st: call(cache._ref, ref, ptr, nbytes, st))
     return out, lse
 
 
@@ -873,12 +958,17 @@ def _cache_evict(cache: Cache, budget, budgets, sink, recent, scope, max_tokens)
     return _CacheEvict(budget, ptr, sink, recent, scope, max_tokens)
 
 
-def compactor_cache_evict_workspace_size(cache: Cache, scope: int = SCOPE_HEAD, max_tokens: int = 0) -> int:
+def _evict_bytes(call, cache, scope, max_tokens) -> int:
     out = C.c_size_t(0)
     _int32(max_tokens=max_tokens)
     evict = _CacheEvict(0, 0, 0, 0, scope, max_tokens)
-    _check(_lib.compactor_cache_evict_workspace_size(cache._ref, C.byref(evict), C.byref(out)))
+    _check(call(cache._ref, C.byref(evict), C.byref(out)))
     return int(out.value)
+
+
+def compactor_cache_evict_workspace_size(cache: Cache, scope: int = SCOPE_HEAD, max_tokens: int = 0) -> int:
+    _either(cache, False)
+    return _evict_bytes(_lib.compactor_cache_evict_workspace_size, cache, scope, max_tokens)
 
 
 def compactor_cache_evict(cache: Cache, budget: Optional[int] = None, budgets: Optional[torch.Tensor] = None,
@@ -886,6 +976,88 @@ def compactor_cache_evict(cache: Cache, budget: Optional[int] = None, budgets: O
                           workspace=None, stream=None):
     """Brings every head (SCOPE_LAYER: the heads of every layer together) down to its budget: `budget`
     tokens, or budgets[request] of an int32 device tensor."""
+    _either(cache, False)
+    _evict(_lib.compactor_cache_evict, _lib.compactor_cache_evict_workspace_size, cache, budget, budgets, sink, recent, scope,
+           max_tokens, workspace, stream)
+
+
+def _evict(call, size, cache, budget, budgets, sink, recent, scope, max_tokens, workspace, stream):
     ref = C.byref(_cache_evict(cache, budget, budgets, sink, recent, scope, max_tokens))
-    ptr, nbytes, _keep = cache._workspace(_lib.compactor_cache_evict_workspace_size, ref, (scope, max_tokens), workspace, stream)
-    cache._on(stream, lambda st: _lib.compactor_cache_evict(cache._ref, ref, ptr, nbytes, st))
+    ptr, nbytes, _keep = cache._workspace(size, ref, (scope, max_tokens), workspace, stream)
+    cache._on(stream, lambda st: call(cache._ref, ref, ptr, nbytes, st))
+
+
+def compactor_mx_append(cache: MxCache, k: torch.Tensor, v: torch.Tensor,
+                         new_tokens: Optional[torch.Tensor] = None, stream=None):
+    """compactor_cache_append into a cache in 4 bits: k and v are bfloat16, as there."""
+    _either(cache, True)
+    rows = _rows(cache, k, v, new_tokens)
+    cache._on(stream, lambda st: _lib.compactor_mx_append(cache._ref, C.byref(rows), st))
+
+
+def compactor_mx_store(cache: MxCache, source: Cache, stream=None):
+    """Makes of `cache` what `source`, a cache of 16 bits of as many requests, layers and heads, holds."""
+    _either(cache, True)
+    _either(source, False)
+    if (source.nreq, source.layers, source.kv_heads) != (cache.nreq, cache.layers, cache.kv_heads):
+        _refuse("the source is of [%d, %d, %d] requests, layers and heads, the cache of [%d, %d, %d]"
+                % (source.nreq, source.layers, source.kv_heads, cache.nreq, cache.layers, cache.kv_heads))
+    _require(cache.mass is None or source.mass is not None, "a cache with state needs a source with state")
+    _require(source.device == cache.device, "the source must live on the GPU of the cache")
+    cache._on(stream, lambda st: _lib.compactor_mx_store(cache._ref, source._ref, st))
+
+
+def compactor_mx_read(cache: MxCache, tokens: int, first: Optional[int] = None, new_tokens: Optional[torch.Tensor] = None,
+                       k=None, v=None, stream=None):
+    """Rows of `tokens` slots from `first` on (None: those that were appended last, with new_tokens those of each request) as
+    bfloat16, zeros where there are none.  -> (k, v) [request, layer, token, kv head, channel]; given ones may have any
+    strides with the channel contiguous, the same for both."""
+    _either(cache, True)
+    _int32(tokens=tokens)
+    shape = (cache.nreq, cache.layers, tokens, cache.kv_heads, 128)
+    if (k is None) != (v is None):
+        _refuse("k and v: both, or none")
+    if k is None:
+        k, v = (_empty(stream, shape, dtype=torch.bfloat16, device=cache.device) for _ in range(2))
+    else:
+        for t in (k, v):
+            if t.dtype != torch.bfloat16 or tuple(t.shape) != shape or t.stride() != k.stride() or t.stride(4) != 1:
+                _refuse("k and v must be bfloat16 %s with the same strides, the channel contiguous" % (shape,))
+            if t.device != cache.device:
+                _refuse("k and v must live on the GPU of the cache")
+            if any(n > 1 and s == 0 for n, s in zip(shape, t.stride())):
+                _refuse("k and v are written: their elements must not share memory")
+    if first is not None:
+        _int32(first=first)
+    rows = _CacheRowsOut(k.data_ptr(), v.data_ptr(), *k.stride()[:4], cache._new_tokens(new_tokens), tokens, -1 if first is None else first)
+    cache._on(stream, lambda st: _lib.compactor_mx_read(cache._ref, C.byref(rows), st))
+    return k, v
+
+
+def compactor_mx_attention_workspace_size(cache: MxCache, q: torch.Tensor, accumulate: bool = False, max_tokens: int = 0) -> int:
+    _either(cache, True)
+    return _attention_bytes(_lib.compactor_mx_attention_workspace_size, cache, q, accumulate, max_tokens)
+
+
+def compactor_mx_attention(cache: MxCache, q: torch.Tensor, new_tokens: Optional[torch.Tensor] = None,
+                            scale: float = 0.0, softcap: float = 0.0, accumulate: bool = False,
+                            max_tokens: int = 0, want_lse: bool = False, out=None, lse=None,
+                            workspace=None, stream=None):
+    """compactor_cache_attention, to a cache in 4 bits."""
+    _either(cache, True)
+    return _attention(_lib.compactor_mx_attention, _lib.compactor_mx_attention_workspace_size, cache, q, new_tokens, scale,
+                      softcap, accumulate, max_tokens, want_lse, out, lse, workspace, stream)
+
+
+def compactor_mx_evict_workspace_size(cache: MxCache, scope: int = SCOPE_HEAD, max_tokens: int = 0) -> int:
+    _either(cache, True)
+    return _evict_bytes(_lib.compactor_mx_evict_workspace_size, cache, scope, max_tokens)
+
+
+def compactor_mx_evict(cache: MxCache, budget: Optional[int] = None, budgets: Optional[torch.Tensor] = None,
+                        sink: int = 0, recent: int = 0, scope: int = SCOPE_HEAD, max_tokens: int = 0,
+                        workspace=None, stream=None):
+    """compactor_cache_evict, from a cache in 4 bits."""
+    _either(cache, True)
+    _evict(_lib.compactor_mx_evict, _lib.compactor_mx_evict_workspace_size, cache, budget, budgets, sink, recent, scope,
+           max_tokens, workspace, stream)

@@ -348,6 +348,114 @@ __device__ __forceinline__ void row_sums(const Queries &Q, const Fragment &f, in
   }
 }
 
+// The four waves of a workgroup meet: rows of its only fragment are finished, else what the fragment has of them goes into the workspace.
+// A wave's lane has sums of query 16 nt + (l & 15) (m: what its exponents are relative to, l: the lane's part of the weights' sum), acc[nt][c][vv]
+// of channel 32 (l >> 4) + 8 vv + c.  Lds: o, m, l, lse2 and none, which is 0.
+template <int NT, class Lds>
+__device__ __forceinline__ void waves_meet(const CacheView &C, const Queries &Q, const HeadOf &w, const Fragment &part, int fragment, Lds &L,
+                                           f32x4 (&acc)[NT][8], float (&m)[NT], float (&l)[NT], const int (&see)[NT]) {
+  const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, n16 = lane & 15, j = lane >> 4;
+  const int R = Q.tokens * Q.group;
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt) {
+    l[nt] = quarters_sum(l[nt]);
+    if (see[nt] <= 0) {
+      m[nt] = -INFINITY;
+      l[nt] = 0.f;
+    }
+    if (j == 0) {
+      L.m[wave][16 * nt + n16] = m[nt];
+      L.l[wave][16 * nt + n16] = l[nt];
+    }
+  }
+  __syncthreads();
+#pragma unroll
+  for (int nt = 0; nt < NT; ++nt) {
+    const int r = 16 * nt + n16;
+    float top = L.m[0][r];
+#pragma unroll
+    for (int i = 1; i < ATT_WAVES; ++i) top = fmaxf(top, L.m[i][r]);
+    const float f = top == -INFINITY ? 0.f : exp2_(m[nt] - top);
+    if (nt > 0) __syncthreads();                    // the last tile of rows has been read
+#pragma unroll
+    for (int vv = 0; vv < 4; ++vv)
+#pragma unroll
+      for (int c = 0; c < 8; c += 4)
+        *reinterpret_cast<f32x4 *>(&L.o[wave][n16][32 * j + 8 * vv + c]) =
+            see[nt] > 0 ? f32x4{acc[nt][c][vv], acc[nt][c + 1][vv], acc[nt][c + 2][vv], acc[nt][c + 3][vv]} * f : f32x4{0.f, 0.f, 0.f, 0.f};
+    __syncthreads();
+    // 16 threads a row, 8 channels each
+    const int row = 16 * nt + (tid >> 4), ch = 8 * (tid & 15);
+    float mm = L.m[0][row], sum = 0.f;
+#pragma unroll
+    for (int i = 1; i < ATT_WAVES; ++i) mm = fmaxf(mm, L.m[i][row]);
+#pragma unroll
+    for (int i = 0; i < ATT_WAVES; ++i) sum += mm == -INFINITY ? L.l[i][row] : L.l[i][row] * exp2_(L.m[i][row] - mm);     // (-inf: 0, or NaN)
+    f32x4 o[2];
+#pragma unroll
+    for (int c = 0; c < 2; ++c) {
+      o[c] = *reinterpret_cast<const f32x4 *>(&L.o[0][tid >> 4][ch + 4 * c]);
+#pragma unroll
+      for (int i = 1; i < ATT_WAVES; ++i) o[c] += *reinterpret_cast<const f32x4 *>(&L.o[i][tid >> 4][ch + 4 * c]);
+    }
+    if (row < R) {
+      if (part.parts == 1) {
+        finish_row(C, Q, w, row, ch, o, mm, sum);
+        if (ch == 0) L.lse2[row] = weights_from(Q, part.count, part.n, row, mm, sum, &L.none);
+        if (ch == 0 && Q.weights != nullptr) Q.stats[(long long)fragment * R + row] = make_float2(mm, sum);
+      } else {
+        const long long at = (long long)fragment * R + row;
+        f32x4 *to = reinterpret_cast<f32x4 *>(Q.partial + at * D + ch);
+        to[0] = o[0];
+        to[1] = o[1];
+        if (ch == 0) Q.stats[at] = make_float2(mm, sum);
+      }
+    }
+  }
+}
+
+// A workgroup that has all of a head adds its weights to the mass.
+__device__ __forceinline__ void mass_here(const CacheView &C, const Queries &Q, const HeadPlace &hp, const float *logits, int R, int count,
+                                          const float *lse2, const int *none) {
+  __threadfence_block();
+  __syncthreads();                                // the workgroup's logits and sums
+  for (int at = 4 * (int)threadIdx.x; at < count; at += 4 * 256) {
+    MassQuad M;
+    mass_fetch(C, Q, hp, logits, R, at, count, M);
+    mass_add(Q, lse2, *none, logits, R, at, M);
+  }
+}
+
+// Lane n16 < 8 gets the n16-th of eight sums over 16 lanes: neighbours, pairs, fours, eights.
+__device__ __forceinline__ float lanes_sum(const float (&sum)[8], int n16) {
+  float mine = 0.f;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    float y = sum[i];
+    y += __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(y), 0xb1, 0xf, 0xf, false));
+    y += __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(y), 0x4e, 0xf, 0xf, false));
+    y += __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(y), 0x141, 0xf, 0xf, false));
+    y += __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(y), 0x140, 0xf, 0xf, false));
+    mine = n16 == i ? y : mine;
+  }
+  return mine;
+}
+
+// Weights of a fragment's slots, summed over the rows, to their mass.
+__device__ __forceinline__ void weights_to_mass(const CacheView &C, const Queries &Q, const HeadPlace &hp, const float *weights, const Run &run,
+                                                const int *none) {
+  __threadfence_block();
+  __syncthreads();
+  const float inv = 1.f / (float)Q.group;
+  for (int at = run.begin + 4 * (int)threadIdx.x; at < run.end; at += 4 * 256) {
+    MassQuad M;
+    mass_fetch(C, Q, hp, weights, 1, at, run.end, M);
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (M.there[i]) *M.mass[i] = at + i < *none ? NAN : fmaf(M.x[0][i], inv, M.old[i]);
+  }
+}
+
 // A call, checked and planned (cache_attention.hip), with the kernels of one kind of rows.  row16: pages hold whole halves of tiles, see there.
 struct AttendKernels {
   void (*attend)(const CacheView &C, const Queries &Q, bool row16, unsigned blocks, hipStream_t st);

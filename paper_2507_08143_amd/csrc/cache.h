@@ -20,7 +20,9 @@ struct CacheView {
   float *mass;
   int32_t *positions;
   long long state_page_stride, state_layer_stride, state_head_stride;
+  uint32_t *k_scales, *v_scales;             // rows of 4 bits: their scales, at the place of mass; else null
 };
+constexpr int ROW4 = D / 4;                  // a row of 4 bits in the units of the strides above
 
 // x / d for 0 <= x < 2^31, by the multiplicative inverse of an invariant divisor (Granlund and Montgomery 1994): with
 // 2^(shift-1) < d <= 2^shift and mul = floor(2^32 (2^shift - d) / d) + 1 the quotient is (mulhi(x, mul) + x) >> shift, and the
@@ -109,8 +111,10 @@ __device__ __forceinline__ unsigned wave_max_up(unsigned x) {
 inline bool launchable(long long blocks, int threads) { return blocks <= 0xffffffffll / threads; }
 
 // Checks a caller's cache (COMPACTOR_OK or an error) and makes the view of it.
-enum CacheNeed { CACHE_SIZES, CACHE_ROWS, CACHE_STATE };      // sizes only; pages and counts; and seen, mass, positions
+// sizes only; tables and counts; pages and counts; and seen, mass, positions
+enum CacheNeed { CACHE_SIZES, CACHE_TABLES, CACHE_ROWS, CACHE_STATE };
 int cache_view(const compactor_cache_t *c, CacheNeed need, CacheView *view);
+int cache_view(const compactor_mx_cache_t *c, CacheNeed need, CacheView *view);       // rows of 4 bits
 
 hipError_t launch_cache_admit(const SegTable &T, const CacheView &C, const int32_t *kept_idx, const int32_t *kept_cnt,
                               const float *scores, hipStream_t st);

@@ -5,10 +5,12 @@
 #include <algorithm>
 
 #include "cache.h"
+#include "fp4.h"
 
 namespace cmp {
 
-int cache_view(const compactor_cache_t *c, CacheNeed need, CacheView *view) {
+// row: of the pool, and unit: of its strides, both in 2 bytes
+static int view_of(const compactor_cache_t *c, CacheNeed need, int row, int unit, CacheView *view) {
   if (!c) return COMPACTOR_EINVAL;
   if (c->nreq < 1 || c->layers < 1 || c->kv_heads < 1) return COMPACTOR_EINVAL;
   if ((long long)c->layers * c->kv_heads > (1 << 20)) return COMPACTOR_EINVAL;
@@ -18,26 +20,30 @@ int cache_view(const compactor_cache_t *c, CacheNeed need, CacheView *view) {
   if (p.page_size < 1 || p.num_pages < 1 || c->table_len < 1 || c->table_stride < c->table_len) return COMPACTOR_EINVAL;
   // (half a TB of rows of one head; sums of a slot and a launch's steps, and a tile's end, then fit)
   if ((long long)c->table_len * p.page_size > 1ll << 30) return COMPACTOR_EINVAL;
-  if (need != CACHE_SIZES) {
-    if (!p.k_pages || !p.v_pages || !c->tables || !c->counts) return COMPACTOR_EINVAL;
-    if (p.page_stride < 0 || p.layer_stride < 0 || p.head_stride < 0 || p.slot_stride < D) return COMPACTOR_EINVAL;
+  if (need >= CACHE_TABLES) {
+    if (!c->tables || !c->counts) return COMPACTOR_EINVAL;
     if (c->count_stride_b < 0 || c->count_stride_l < 0) return COMPACTOR_EINVAL;
+  }
+  if (need >= CACHE_ROWS) {
+    if (!p.k_pages || !p.v_pages) return COMPACTOR_EINVAL;
+    if (p.page_stride < 0 || p.layer_stride < 0 || p.head_stride < 0 || p.slot_stride / unit < row) return COMPACTOR_EINVAL;
     if (c->state_page_stride < 0 || c->state_layer_stride < 0 || c->state_head_stride < 0) return COMPACTOR_EINVAL;
     const int state = (c->seen != nullptr) + (c->mass != nullptr) + (c->positions != nullptr);
     if (state != 3 && (state != 0 || need == CACHE_STATE)) return COMPACTOR_EINVAL;
     if (((reinterpret_cast<uintptr_t>(p.k_pages) | reinterpret_cast<uintptr_t>(p.v_pages)) & 15u) ||
-        ((p.page_stride | p.layer_stride | p.head_stride | p.slot_stride) & 7) ||
-        ((reinterpret_cast<uintptr_t>(c->tables) | reinterpret_cast<uintptr_t>(c->counts) |
-          reinterpret_cast<uintptr_t>(c->seen) | reinterpret_cast<uintptr_t>(c->mass) |
-          reinterpret_cast<uintptr_t>(c->positions)) & 3u))
+        ((p.page_stride | p.layer_stride | p.head_stride | p.slot_stride) & (8 * unit - 1)) ||
+        ((reinterpret_cast<uintptr_t>(c->mass) | reinterpret_cast<uintptr_t>(c->positions)) & 3u))
       return COMPACTOR_EALIGN;
   }
+  if (need >= CACHE_TABLES &&
+      ((reinterpret_cast<uintptr_t>(c->tables) | reinterpret_cast<uintptr_t>(c->counts) | reinterpret_cast<uintptr_t>(c->seen)) & 3u))
+    return COMPACTOR_EALIGN;
   CacheView &v = *view;
   memset(&v, 0, sizeof(v));
   v.k = static_cast<uint16_t *>(p.k_pages);
   v.v = static_cast<uint16_t *>(p.v_pages);
-  v.page_stride = p.page_stride; v.layer_stride = p.layer_stride;
-  v.head_stride = p.head_stride; v.slot_stride = p.slot_stride;
+  v.page_stride = p.page_stride / unit; v.layer_stride = p.layer_stride / unit;
+  v.head_stride = p.head_stride / unit; v.slot_stride = p.slot_stride / unit;
   v.tables = c->tables; v.table_stride = c->table_stride;
   v.page_size = p.page_size; v.num_pages = p.num_pages;
   v.capacity = c->table_len * p.page_size;
@@ -50,6 +56,19 @@ int cache_view(const compactor_cache_t *c, CacheNeed need, CacheView *view) {
   v.mass = c->mass; v.positions = c->positions;
   v.state_page_stride = c->state_page_stride; v.state_layer_stride = c->state_layer_stride;
   v.state_head_stride = c->state_head_stride;
+  return COMPACTOR_OK;
+}
+int cache_view(const compactor_cache_t *c, CacheNeed need, CacheView *view) { return view_of(c, need, D, 1, view); }
+int cache_view(const compactor_mx_cache_t *c, CacheNeed need, CacheView *view) {
+  if (!c) return COMPACTOR_EINVAL;
+  const int rc = view_of(&c->cache, need, ROW4, 2, view);
+  if (rc) return rc;
+  if (need >= CACHE_ROWS) {
+    if (!c->k_scales || !c->v_scales) return COMPACTOR_EINVAL;
+    if ((reinterpret_cast<uintptr_t>(c->k_scales) | reinterpret_cast<uintptr_t>(c->v_scales)) & 3u) return COMPACTOR_EALIGN;
+    view->k_scales = c->k_scales;
+    view->v_scales = c->v_scales;
+  }
   return COMPACTOR_OK;
 }
 
@@ -66,17 +85,35 @@ struct NewRows {
 constexpr int APPEND_FEW = 8;        // rows of a head that one group of 16 lanes takes alone
 constexpr int APPEND_ROWS = 64;      // else, rows of a head per workgroup
 
+// FP4: rows become rows of 4 bits on the way.
+template <bool FP4>
 __device__ __forceinline__ void append_row(const CacheView &C, const NewRows &R, const HeadOf &w, const HeadPlace &p,
                                            int count, int seen, int t, int lane) {
   const long long src = w.b * R.stride_b + w.l * R.stride_l + t * R.stride_t + w.h * R.stride_h + 8 * lane;
   const uint4 k = *reinterpret_cast<const uint4 *>(R.k + src);
   const uint4 v = *reinterpret_cast<const uint4 *>(R.v + src);
+  uint32_t k_scales = 0, v_scales = 0;
+  unsigned k4 = 0, v4 = 0;
+  if (FP4) {                     // by all 16 lanes
+    k4 = fp4_encode_row(k, lane, k_scales);
+    v4 = fp4_encode_row(v, lane, v_scales);
+  }
   if (t >= C.capacity - count) return;
   const SlotPlace s = slot_place(C, p, count + t);
   if (!page_there(C, s.page)) return;
-  const long long dst = row_at(C, p, s) + 8 * lane;
-  *reinterpret_cast<uint4 *>(C.k + dst) = k;
-  *reinterpret_cast<uint4 *>(C.v + dst) = v;
+  const long long dst = row_at(C, p, s) + (FP4 ? 2 : 8) * lane;
+  if (FP4) {
+    *reinterpret_cast<unsigned *>(C.k + dst) = k4;
+    *reinterpret_cast<unsigned *>(C.v + dst) = v4;
+    if (lane == 0) {
+      const long long at = state_at(C, p, s);
+      C.k_scales[at] = k_scales;
+      C.v_scales[at] = v_scales;
+    }
+  } else {
+    *reinterpret_cast<uint4 *>(C.k + dst) = k;
+    *reinterpret_cast<uint4 *>(C.v + dst) = v;
+  }
   if (C.mass != nullptr && lane == 0) {
     const long long at = state_at(C, p, s);
     C.mass[at] = 0.f;
@@ -90,6 +127,7 @@ __device__ __forceinline__ void append_count(const CacheView &C, const HeadOf &w
 }
 
 // A group of 16 lanes per head takes all its rows and then moves its counts on.
+template <bool FP4>
 __global__ __launch_bounds__(256) void append_few_kernel(const CacheView C, const NewRows R) {
   const unsigned g = blockIdx.x * 16u + (threadIdx.x >> 4);
   if (g >= (unsigned)C.nreq * (unsigned)C.layers * (unsigned)C.kv_heads) return;
@@ -98,11 +136,12 @@ __global__ __launch_bounds__(256) void append_few_kernel(const CacheView C, cons
   const HeadPlace p = head_place(C, w);
   const int n = tokens_new(R.new_tokens, w.b, R.tokens), count = held(C, w.b, w.l, w.h);
   const int seen = C.seen != nullptr ? C.seen[count_at(C, w.b, w.l, w.h)] : 0;
-  for (int t = 0; t < n; ++t) append_row(C, R, w, p, count, seen, t, lane);
+  for (int t = 0; t < n; ++t) append_row<FP4>(C, R, w, p, count, seen, t, lane);
   if (lane == 0 && n > 0) append_count(C, w, count, seen, n);
 }
 
 // A workgroup per APPEND_ROWS rows of a head; where a head has several, another launch moves the counts on.
+template <bool FP4>
 __global__ __launch_bounds__(256) void append_kernel(const CacheView C, const NewRows R, int parts) {
   const unsigned g = blockIdx.x / (unsigned)parts;
   const int part = (int)(blockIdx.x - g * (unsigned)parts), lane = threadIdx.x & 15;
@@ -114,7 +153,7 @@ __global__ __launch_bounds__(256) void append_kernel(const CacheView C, const Ne
 #pragma unroll
   for (int i = 0; i < APPEND_ROWS / 16; ++i) {
     const int t = t0 + 16 * i + (int)(threadIdx.x >> 4);
-    if (t < n) append_row(C, R, w, p, count, seen, t, lane);
+    if (t < n) append_row<FP4>(C, R, w, p, count, seen, t, lane);
   }
   if (parts == 1) {
     __syncthreads();                   // every wave has read the count
@@ -427,13 +466,25 @@ __device__ __forceinline__ void find_bin(const int *hist, int want, int *per_wav
 __device__ __forceinline__ void move_row(const CacheView &C, const HeadPlace &p, int to, int from, int lane) {
   const SlotPlace z = slot_place(C, p, to), a = slot_place(C, p, from);
   if (!page_there(C, z.page) || !page_there(C, a.page)) return;
-  const long long src = row_at(C, p, a) + 8 * lane, dst = row_at(C, p, z) + 8 * lane;
-  const uint4 k = *reinterpret_cast<const uint4 *>(C.k + src);
-  const uint4 v = *reinterpret_cast<const uint4 *>(C.v + src);
-  *reinterpret_cast<uint4 *>(C.k + dst) = k;
-  *reinterpret_cast<uint4 *>(C.v + dst) = v;
+  if (C.k_scales != nullptr) {               // 4 bytes a lane
+    const long long src = row_at(C, p, a) + 2 * lane, dst = row_at(C, p, z) + 2 * lane;
+    const unsigned k = *reinterpret_cast<const unsigned *>(C.k + src);
+    const unsigned v = *reinterpret_cast<const unsigned *>(C.v + src);
+    *reinterpret_cast<unsigned *>(C.k + dst) = k;
+    *reinterpret_cast<unsigned *>(C.v + dst) = v;
+  } else {
+    const long long src = row_at(C, p, a) + 8 * lane, dst = row_at(C, p, z) + 8 * lane;
+    const uint4 k = *reinterpret_cast<const uint4 *>(C.k + src);
+    const uint4 v = *reinterpret_cast<const uint4 *>(C.v + src);
+    *reinterpret_cast<uint4 *>(C.k + dst) = k;
+    *reinterpret_cast<uint4 *>(C.v + dst) = v;
+  }
   if (lane == 0) {
     const long long x = state_at(C, p, a), y = state_at(C, p, z);
+    if (C.k_scales != nullptr) {
+      C.k_scales[y] = C.k_scales[x];
+      C.v_scales[y] = C.v_scales[x];
+    }
     C.mass[y] = C.mass[x];
     C.positions[y] = C.positions[x];
   }
@@ -993,17 +1044,7 @@ static size_t evict_bytes(const CacheView &C, const compactor_cache_evict_params
   return evict_alone(C, e) ? 0 : evict_scratch(C, e, nullptr, &E);
 }
 
-}  // namespace cmp
-
-using namespace cmp;
-
-extern "C" {
-#pragma GCC visibility push(default)
-
-int compactor_cache_append(const compactor_cache_t *cache, const compactor_cache_rows_t *rows, void *stream) {
-  CacheView C;
-  const int rc = cache_view(cache, CACHE_ROWS, &C);
-  if (rc) return rc;
+static int append_call(const CacheView &C, const compactor_cache_rows_t *rows, void *stream) {
   if (!rows || !rows->k || !rows->v || rows->tokens < 1) return COMPACTOR_EINVAL;
   if (rows->stride_b < 0 || rows->stride_l < 0 || rows->stride_t < 0 || rows->stride_h < 0) return COMPACTOR_EINVAL;
   if (((reinterpret_cast<uintptr_t>(rows->k) | reinterpret_cast<uintptr_t>(rows->v)) & 15u) ||
@@ -1018,9 +1059,11 @@ int compactor_cache_append(const compactor_cache_t *cache, const compactor_cache
   hipStream_t st = static_cast<hipStream_t>(stream);
   (void)hipGetLastError();   // a leftover of earlier, unrelated HIP calls is not this call's error
   if (R.tokens <= APPEND_FEW) {
-    hipLaunchKernelGGL(append_few_kernel, dim3((unsigned)((heads + 15) / 16)), dim3(256), 0, st, C, R);
+    hipLaunchKernelGGL(C.k_scales != nullptr ? append_few_kernel<true> : append_few_kernel<false>,
+                       dim3((unsigned)((heads + 15) / 16)), dim3(256), 0, st, C, R);
   } else {
-    hipLaunchKernelGGL(append_kernel, dim3((unsigned)(heads * parts)), dim3(256), 0, st, C, R, parts);
+    hipLaunchKernelGGL(C.k_scales != nullptr ? append_kernel<true> : append_kernel<false>, dim3((unsigned)(heads * parts)),
+                       dim3(256), 0, st, C, R, parts);
     if (parts > 1) {
       if (hipGetLastError() != hipSuccess) return COMPACTOR_EHIP;
       hipLaunchKernelGGL(append_counts_kernel, dim3((unsigned)((heads + 255) / 256)), dim3(256), 0, st, C, R);
@@ -1029,24 +1072,16 @@ int compactor_cache_append(const compactor_cache_t *cache, const compactor_cache
   return hipGetLastError() == hipSuccess ? COMPACTOR_OK : COMPACTOR_EHIP;
 }
 
-int compactor_cache_evict_workspace_size(const compactor_cache_t *cache, const compactor_cache_evict_params_t *evict,
-                                         size_t *bytes) {
-  CacheView C;
-  int rc = cache_view(cache, CACHE_SIZES, &C);
-  if (rc) return rc;
-  rc = evict_check(evict, C);
+static int evict_workspace(const CacheView &C, const compactor_cache_evict_params_t *evict, size_t *bytes) {
+  const int rc = evict_check(evict, C);
   if (rc) return rc;
   if (!bytes) return COMPACTOR_EINVAL;
   *bytes = evict_bytes(C, evict);
   return COMPACTOR_OK;
 }
 
-int compactor_cache_evict(const compactor_cache_t *cache, const compactor_cache_evict_params_t *evict,
-                          void *workspace, size_t workspace_bytes, void *stream) {
-  CacheView C;
-  int rc = cache_view(cache, CACHE_STATE, &C);
-  if (rc) return rc;
-  rc = evict_check(evict, C);
+static int evict_call(const CacheView &C, const compactor_cache_evict_params_t *evict, void *workspace, size_t workspace_bytes, void *stream) {
+  const int rc = evict_check(evict, C);
   if (rc) return rc;
   if (!evict->budgets && evict->budget < 0) return COMPACTOR_EINVAL;
   if (reinterpret_cast<uintptr_t>(evict->budgets) & 3u) return COMPACTOR_EALIGN;
@@ -1088,6 +1123,52 @@ int compactor_cache_evict(const compactor_cache_t *cache, const compactor_cache_
   if (hipGetLastError() != hipSuccess) return COMPACTOR_EHIP;
   hipLaunchKernelGGL(evict_move_kernel, dim3((unsigned)(heads * movers)), dim3(MOVE_THREADS), 0, st, C, E, (int)movers);
   return hipGetLastError() == hipSuccess ? COMPACTOR_OK : COMPACTOR_EHIP;
+}
+
+}  // namespace cmp
+
+using namespace cmp;
+
+extern "C" {
+#pragma GCC visibility push(default)
+
+int compactor_cache_append(const compactor_cache_t *cache, const compactor_cache_rows_t *rows, void *stream) {
+  CacheView C;
+  const int rc = cache_view(cache, CACHE_ROWS, &C);
+  return rc ? rc : append_call(C, rows, stream);
+}
+
+int compactor_mx_append(const compactor_mx_cache_t *cache, const compactor_cache_rows_t *rows, void *stream) {
+  CacheView C;
+  const int rc = cache_view(cache, CACHE_ROWS, &C);
+  return rc ? rc : append_call(C, rows, stream);
+}
+
+int compactor_cache_evict_workspace_size(const compactor_cache_t *cache, const compactor_cache_evict_params_t *evict,
+                                         size_t *bytes) {
+  CacheView C;
+  const int rc = cache_view(cache, CACHE_SIZES, &C);
+  return rc ? rc : evict_workspace(C, evict, bytes);
+}
+
+int compactor_cache_evict(const compactor_cache_t *cache, const compactor_cache_evict_params_t *evict,
+                          void *workspace, size_t workspace_bytes, void *stream) {
+  CacheView C;
+  const int rc = cache_view(cache, CACHE_STATE, &C);
+  return rc ? rc : evict_call(C, evict, workspace, workspace_bytes, stream);
+}
+
+int compactor_mx_evict_workspace_size(const compactor_mx_cache_t *cache, const compactor_cache_evict_params_t *evict, size_t *bytes) {
+  CacheView C;
+  const int rc = cache_view(cache, CACHE_SIZES, &C);
+  return rc ? rc : evict_workspace(C, evict, bytes);
+}
+
+int compactor_mx_evict(const compactor_mx_cache_t *cache, const compactor_cache_evict_params_t *evict, void *workspace,
+                        size_t workspace_bytes, void *stream) {
+  CacheView C;
+  const int rc = cache_view(cache, CACHE_STATE, &C);
+  return rc ? rc : evict_call(C, evict, workspace, workspace_bytes, stream);
 }
 
 #pragma GCC visibility pop

@@ -328,73 +328,9 @@ __global__ __launch_bounds__(256, NT <= 2 ? 2 : 1) void attend_kernel(const Cach
     one_tile(tiles - 1, std::false_type());
   }
 
-  // the four waves meet
-#pragma unroll
-  for (int nt = 0; nt < NT; ++nt) {
-    l[nt] = quarters_sum(l[nt]);
-    if (see[nt] <= 0) {
-      m[nt] = -INFINITY;
-      l[nt] = 0.f;
-    }
-    if (j == 0) {
-      L.m[wave][16 * nt + n16] = m[nt];
-      L.l[wave][16 * nt + n16] = l[nt];
-    }
-  }
-  __syncthreads();
-#pragma unroll
-  for (int nt = 0; nt < NT; ++nt) {
-    const int r = 16 * nt + n16;
-    float top = L.m[0][r];
-#pragma unroll
-    for (int i = 1; i < ATT_WAVES; ++i) top = fmaxf(top, L.m[i][r]);
-    const float f = top == -INFINITY ? 0.f : exp2_(m[nt] - top);
-    if (nt > 0) __syncthreads();                    // the last tile of rows has been read
-#pragma unroll
-    for (int vv = 0; vv < 4; ++vv)
-#pragma unroll
-      for (int c = 0; c < 8; c += 4)
-        *reinterpret_cast<f32x4 *>(&L.o[wave][n16][32 * j + 8 * vv + c]) =
-            see[nt] > 0 ? f32x4{acc[nt][c][vv], acc[nt][c + 1][vv], acc[nt][c + 2][vv], acc[nt][c + 3][vv]} * f : f32x4{0.f, 0.f, 0.f, 0.f};
-    __syncthreads();
-    // 16 threads a row, 8 channels each
-    const int row = 16 * nt + (tid >> 4), ch = 8 * (tid & 15);
-    float mm = L.m[0][row], sum = 0.f;
-#pragma unroll
-    for (int i = 1; i < ATT_WAVES; ++i) mm = fmaxf(mm, L.m[i][row]);
-#pragma unroll
-    for (int i = 0; i < ATT_WAVES; ++i) sum += mm == -INFINITY ? L.l[i][row] : L.l[i][row] * exp2_(L.m[i][row] - mm);     // (-inf: 0, or NaN)
-    f32x4 o[2];
-#pragma unroll
-    for (int c = 0; c < 2; ++c) {
-      o[c] = *reinterpret_cast<const f32x4 *>(&L.o[0][tid >> 4][ch + 4 * c]);
-#pragma unroll
-      for (int i = 1; i < ATT_WAVES; ++i) o[c] += *reinterpret_cast<const f32x4 *>(&L.o[i][tid >> 4][ch + 4 * c]);
-    }
-    if (row < R) {
-      if (complete) {
-        finish_row(C, Q, w, row, ch, o, mm, sum);
-        if (ch == 0) L.lse2[row] = weights_from(Q, count, n, row, mm, sum, &L.none);
-        if (ch == 0 && Q.weights != nullptr) Q.stats[(long long)fragment * R + row] = make_float2(mm, sum);
-      } else {
-        const long long at = (long long)fragment * R + row;
-        f32x4 *to = reinterpret_cast<f32x4 *>(Q.partial + at * D + ch);
-        to[0] = o[0];
-        to[1] = o[1];
-        if (ch == 0) Q.stats[at] = make_float2(mm, sum);
-      }
-    }
-  }
+  waves_meet<NT>(C, Q, w, part, fragment, L, acc, m, l, see);
   if (kept_in_lds<NT> && store && tiles > 0) leave(tiles);
-  if (complete && store && n > 0) {
-    __threadfence_block();
-    __syncthreads();                                // the workgroup's logits and sums
-    for (int at = 4 * tid; at < count; at += 4 * 256) {
-      MassQuad M;
-      mass_fetch(C, Q, hp, logits, R, at, count, M);
-      mass_add(Q, L.lse2, L.none, logits, R, at, M);
-    }
-  }
+  if (complete && store && n > 0) mass_here(C, Q, hp, logits, R, count, L.lse2, &L.none);
 }
 
 // Second launch: the fragments of a head meet.  The first heads * R workgroups take a query row each, 16 fragments side by side
@@ -554,17 +490,7 @@ __global__ __launch_bounds__(256) void attend_mass_kernel(const CacheView C, con
 #pragma unroll
       for (int i = 0; i < 8; ++i) sum[i] += z[nt] == INFINITY ? 0.f : exp2_(x[i] - z[nt]);
     }
-    // over the 16 lanes: neighbours, pairs, fours, eights
-    float mine = 0.f;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      float y = sum[i];
-      y += __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(y), 0xb1, 0xf, 0xf, false));
-      y += __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(y), 0x4e, 0xf, 0xf, false));
-      y += __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(y), 0x141, 0xf, 0xf, false));
-      y += __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(y), 0x140, 0xf, 0xf, false));
-      mine = n16 == i ? y : mine;
-    }
+    const float mine = lanes_sum(sum, n16);
     if (n16 < 8) weights[s0 + 16 * (n16 >> 2) + 4 * j + (n16 & 3)] = mine;
     there = there_next;
     __builtin_amdgcn_sched_barrier(0);
@@ -573,16 +499,7 @@ __global__ __launch_bounds__(256) void attend_mass_kernel(const CacheView C, con
     for (int tile = 0; tile + 1 < tiles; ++tile) one_tile(tile, std::true_type());
     one_tile(tiles - 1, std::false_type());
   }
-  __threadfence_block();
-  __syncthreads();
-  const float inv = 1.f / (float)Q.group;
-  for (int at = run.begin + 4 * tid; at < run.end; at += 4 * 256) {
-    MassQuad M;
-    mass_fetch(C, Q, hp, weights, 1, at, run.end, M);
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-      if (M.there[i]) *M.mass[i] = at + i < none ? NAN : fmaf(M.x[0][i], inv, M.old[i]);
-  }
+  weights_to_mass(C, Q, hp, weights, run, &none);
 }
 
 static float scale_of(const compactor_cache_query_t *q) { return q->scale > 0.f ? q->scale : 1.0f / sqrtf((float)D); }
