@@ -486,6 +486,55 @@ int compactor_mx_evict(const compactor_mx_cache_t *cache, const compactor_cache_
                         size_t workspace_bytes, void *stream);
 int compactor_mx_evict_workspace_size(const compactor_mx_cache_t *cache, const compactor_cache_evict_params_t *evict, size_t *bytes);
 
+/* ---- norms and rotation of queries and keys --------------------------------------------------- */
+/* What a layer does between its projections and its cache: RMS norms of every query and key head, and rotary positions.  Keys are
+ * scored before the rotation and cached after it. */
+typedef struct compactor_rotation {
+  const double *freqs;    /* device, double [rotary_dim / 2]: angle of pair i per position, in radians */
+  int32_t rotary_dim;     /* channels 0 .. rotary_dim-1 are rotated, a multiple of 8 from 8 to 128; the others stay */
+  int32_t interleaved;    /* 0: pair i is channels i and i + rotary_dim/2; else 2 i and 2 i + 1 */
+  const float *q_norm, *k_norm;   /* device, fp32 [layers][128], 16-byte aligned: weights of the norms, each NULL where there is none */
+  float   eps;            /* of the norms, >= 2^-100 where there is one */
+} compactor_rotation_t;
+
+/* For row x of a head at position p, with weight w:
+ *   y_c = x_c w_c / sqrt(sum_c x_c^2 / 128 + eps)   (without a norm: x_c),
+ *   (y_i, y_j) of pair i becomes (y_i cos a - y_j sin a, y_j cos a + y_i sin a), a = p * freqs[i] in 64 bits, taken modulo 2 pi without loss;
+ * all else in fp32, rounded once.  (Rows with numbers of more than 2^60 overflow in the sum of a norm.) */
+typedef struct compactor_rotate_rows {
+  const void *q, *k;      /* device, bf16, as in compactor_cache_rows; q NULL with q_heads 0, or k with kv_heads 0 */
+  void *q_out, *k_out;    /* device, bf16, rotated */
+  void *k_plain;          /* device, bf16: y, not rotated; or NULL */
+  int64_t q_stride_b, q_stride_l, q_stride_t, q_stride_h;
+  int64_t k_stride_b, k_stride_l, k_stride_t, k_stride_h;
+  int64_t q_out_stride_b, q_out_stride_l, q_out_stride_t, q_out_stride_h;
+  int64_t k_out_stride_b, k_out_stride_l, k_out_stride_t, k_out_stride_h;
+  int64_t k_plain_stride_b, k_plain_stride_l, k_plain_stride_t, k_plain_stride_h;
+                          /* strides are multiples of 8; an output is its input in place, with the same strides, or shares no memory with anything */
+  const int32_t *positions;    /* device, int32: of token t of request b at b*position_stride_b + t */
+  int64_t position_stride_b;   /* 0: the same for all requests */
+  const int32_t *new_tokens;   /* as in compactor_cache_rows; the outputs' padding rows stay as they are */
+  int32_t nreq, layers, tokens, q_heads, kv_heads;
+} compactor_rotate_rows_t;
+int compactor_rotate(const compactor_rotation_t *rotation, const compactor_rotate_rows_t *rows, void *stream);
+
+/* The queries of the tokens that are appended. */
+typedef struct compactor_rotate_queries {
+  const void *q;          /* device, bf16, as in compactor_cache_query */
+  void *q_out;            /* q in place, with the same strides, or other memory */
+  int64_t q_stride_b, q_stride_l, q_stride_t, q_stride_h;
+  int64_t q_out_stride_b, q_out_stride_l, q_out_stride_t, q_out_stride_h;
+  int32_t q_heads;        /* a multiple of kv_heads */
+} compactor_rotate_queries_t;
+/* compactor_cache_append of keys that are normed and rotated on the way, and of values as they are; the queries of the same tokens
+ * likewise (queries NULL: none).  Token t of head h has position seen + t, that which it is appended with, and so have the query
+ * heads that share h.  Queries of rows that the table has no room for are rotated too; those of padding rows stay as they are. */
+int compactor_cache_append_rotated(const compactor_cache_t *cache, const compactor_rotation_t *rotation, const compactor_cache_rows_t *rows,
+                                   const compactor_rotate_queries_t *queries, void *stream);
+/* The same into a cache in 4 bits, of the keys that are rounded to bf16. */
+int compactor_mx_append_rotated(const compactor_mx_cache_t *cache, const compactor_rotation_t *rotation, const compactor_cache_rows_t *rows,
+                                const compactor_rotate_queries_t *queries, void *stream);
+
 /* Context-calibrated retention (Sec. 3.4): the smallest r in (0,1] with
  * f(r) = (exp(r b - b) - exp(-b)) / (1 - exp(-b)) >= tau, b = alpha*nll + beta, i.e.
  * r* = 1 + ln(tau (1 - e^-b) + e^-b) / b (r* = tau in the limit b -> 0). host. */

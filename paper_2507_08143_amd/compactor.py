@@ -106,6 +106,23 @@ class _CacheRowsOut(C.Structure):
                 ("tokens", C.c_int32), ("first", C.c_int32)]
 
 
+class _Rotation(C.Structure):
+    _fields_ = [("freqs", C.c_void_p), ("rotary_dim", C.c_int32), ("interleaved", C.c_int32),
+                ("q_norm", C.c_void_p), ("k_norm", C.c_void_p), ("eps", C.c_float)]
+
+
+class _RotateRows(C.Structure):
+    _fields_ = ([(n, C.c_void_p) for n in ("q", "k", "q_out", "k_out", "k_plain")] +
+                [("%s_stride_%s" % (n, d), C.c_int64) for n in ("q", "k", "q_out", "k_out", "k_plain") for d in "blth"] +
+                [("positions", C.c_void_p), ("position_stride_b", C.c_int64), ("new_tokens", C.c_void_p)] +
+                [(n, C.c_int32) for n in ("nreq", "layers", "tokens", "q_heads", "kv_heads")])
+
+
+class _RotateQueries(C.Structure):
+    _fields_ = ([("q", C.c_void_p), ("q_out", C.c_void_p)] +
+                [("%s_stride_%s" % (n, d), C.c_int64) for n in ("q", "q_out") for d in "blth"] + [("q_heads", C.c_int32)])
+
+
 _PP, _RP = C.POINTER(_Params), C.POINTER(_Request)
 _CP, _CQP, _CEP = C.POINTER(_Cache), C.POINTER(_CacheQuery), C.POINTER(_CacheEvict)
 _lib.compactor_cache_admit.argtypes = [_PP, _RP, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p, _CP,
@@ -123,6 +140,10 @@ _lib.compactor_mx_attention.argtypes = [_MXP, _CQP, C.c_void_p, C.c_size_t, C.c_
 _lib.compactor_mx_attention_workspace_size.argtypes = [_MXP, _CQP, C.POINTER(C.c_size_t)]
 _lib.compactor_mx_evict.argtypes = [_MXP, _CEP, C.c_void_p, C.c_size_t, C.c_void_p]
 _lib.compactor_mx_evict_workspace_size.argtypes = [_MXP, _CEP, C.POINTER(C.c_size_t)]
+_ROP = C.POINTER(_Rotation)
+_lib.compactor_rotate.argtypes = [_ROP, C.POINTER(_RotateRows), C.c_void_p]
+_lib.compactor_cache_append_rotated.argtypes = [_CP, _ROP, C.POINTER(_CacheRows), C.POINTER(_RotateQueries), C.c_void_p]
+_lib.compactor_mx_append_rotated.argtypes = [_MXP, _ROP, C.POINTER(_CacheRows), C.POINTER(_RotateQueries), C.c_void_p]
 _APP, _ARP = C.POINTER(_AttnParams), C.POINTER(_AttnRequest)
 _lib.compactor_attention_workspace_size.argtypes = [_APP, _ARP, C.c_int32, C.POINTER(C.c_size_t)]
 _lib.compactor_attention_scores.argtypes = [_APP, _ARP, C.c_int32, C.c_void_p, C.c_void_p,
@@ -165,7 +186,8 @@ EXPORTS = ["compactor_default_params", "compactor_keep_count", "compactor_layout
            "compactor_cache_attention_workspace_size", "compactor_cache_evict",
            "compactor_cache_evict_workspace_size",
            "compactor_mx_append", "compactor_mx_store", "compactor_mx_read", "compactor_mx_attention",
-           "compactor_mx_attention_workspace_size", "compactor_mx_evict", "compactor_mx_evict_workspace_size"]
+           "compactor_mx_attention_workspace_size", "compactor_mx_evict", "compactor_mx_evict_workspace_size",
+           "compactor_rotate", "compactor_cache_append_rotated", "compactor_mx_append_rotated"]
 
 
 STAGES = ["gram", "reduce", "solve", "score", "blend", "select", "gather"]
@@ -1061,3 +1083,148 @@ def compactor_mx_evict(cache: MxCache, budget: Optional[int] = None, budgets: Op
     _either(cache, True)
     _evict(_lib.compactor_mx_evict, _lib.compactor_mx_evict_workspace_size, cache, budget, budgets, sink, recent, scope,
            max_tokens, workspace, stream)
+
+
+class Rotation:
+    """Norms and rotary positions of the heads of some layers (see compactor_rotation_t).  Checked once, here; the tensors stay the caller's.
+
+    freqs           float64 [rotary_dim / 2]: radians per position of each pair of channels
+    rotary_dim      channels that are rotated (None: twice as many as freqs); interleaved: pairs of neighbours, else of halves
+    q_norm, k_norm  float32 [layer, 128]: weights of the norms, None where there is none; eps: theirs"""
+
+    def __init__(self, freqs: torch.Tensor, rotary_dim: Optional[int] = None, interleaved: bool = False,
+                 q_norm: Optional[torch.Tensor] = None, k_norm: Optional[torch.Tensor] = None, eps: float = 1e-6):
+        rotary_dim = 2 * freqs.numel() if rotary_dim is None else rotary_dim
+        if freqs.dtype != torch.float64 or freqs.dim() != 1 or not freqs.is_contiguous() or 2 * freqs.numel() != rotary_dim:
+            _refuse("freqs must be a contiguous float64 tensor of rotary_dim / 2 = %s / 2 numbers" % rotary_dim)
+        if not 8 <= rotary_dim <= 128 or rotary_dim % 8:
+            _refuse("rotary_dim must be a multiple of 8 from 8 to 128, got %s" % rotary_dim)
+        self.device, self.layers = freqs.device, None
+        for name, t in (("q_norm", q_norm), ("k_norm", k_norm)):
+            if t is None:
+                continue
+            if t.dtype != torch.float32 or t.dim() != 2 or t.shape[1] != 128 or not t.is_contiguous():
+                _refuse("%s must be a contiguous float32 tensor [layers, 128]" % name)
+            if self.layers not in (None, t.shape[0]):
+                _refuse("q_norm and k_norm must be of as many layers")
+            if t.device != self.device:
+                _refuse("%s must live on the GPU of freqs" % name)
+            self.layers = t.shape[0]
+        _require(freqs.is_cuda, "freqs must live on the GPU")
+        self.freqs, self.rotary_dim, self.interleaved = freqs, rotary_dim, interleaved
+        self.q_norm, self.k_norm, self.eps = q_norm, k_norm, eps
+        self._c = _Rotation(freqs.data_ptr(), rotary_dim, 1 if interleaved else 0, _ptr(q_norm), _ptr(k_norm), eps)
+        self._ref = C.byref(self._c)
+
+    def layer(self, first: int, count: int = 1) -> "Rotation":
+        """That of `count` layers from `first` on, for calls layer by layer."""
+        _require(self.layers is None or (0 <= first and count >= 1 and first + count <= self.layers), "no such layers")
+        some = lambda t: None if t is None else t[first:first + count]      # noqa: E731
+        return Rotation(self.freqs, self.rotary_dim, self.interleaved, some(self.q_norm), some(self.k_norm), self.eps)
+
+    def _fits(self, layers: int, device):
+        if self.layers not in (None, layers):
+            _refuse("the norms are of %s layers, the rows of %s" % (self.layers, layers))
+        if self.device != device:
+            _refuse("the rotation and the rows must live on the same GPU")
+
+
+def _head_rows(t, what, shape=None, device=None):
+    if t.dtype != torch.bfloat16 or t.dim() != 5 or t.stride(4) != 1 or t.shape[4] != 128:
+        _refuse("%s must be bfloat16 [request, layer, token, head, 128], the channel contiguous" % what)
+    if shape is not None and t.shape != shape:
+        _refuse("%s has shape %s, %s is needed" % (what, tuple(t.shape), tuple(shape)))
+    if device is not None and t.device != device:
+        _refuse("%s must live on the GPU of the others" % what)
+
+
+def _head_rows_out(t, like, what, stream):
+    """A given output, or a new one."""
+    if t is None:
+        t = _made_on(stream, lambda: torch.empty_like(like))
+        return t if t.stride(4) == 1 else _empty(stream, like.shape, dtype=torch.bfloat16, device=like.device)
+    _head_rows(t, what, like.shape, like.device)
+    if any(n > 1 and s == 0 for n, s in zip(t.shape, t.stride())):
+        _refuse("%s is written: its elements must not share memory" % what)
+    return t
+
+
+def _on_gpu(device, stream, call):
+    """call(stream handle) with the tensors' GPU current."""
+    if stream is not None and stream.device != device:
+        _refuse("the stream belongs to another GPU than the rows")
+    if device.index in (None, torch.cuda.current_device()):
+        _check(call(_stream(stream)))
+    else:
+        with torch.cuda.device(device):
+            _check(call(_stream(stream)))
+
+
+def compactor_rotate(rotation: Rotation, q: Optional[torch.Tensor], k: Optional[torch.Tensor], positions: torch.Tensor,
+                     new_tokens: Optional[torch.Tensor] = None, want_plain: bool = False, q_out=None, k_out=None, k_plain=None,
+                     stream=None):
+    """Queries and keys normed and rotated by position.  q, k: bf16 [request, layer, token, head, 128], any strides with the channel
+    contiguous, one of them may be None; positions: int32 [request, token], or [token] for all requests; q_out, k_out: other
+    memory, or q and k themselves.  -> (q, k, keys before the rotation, or None unless asked for or given)"""
+    rows = q if q is not None else k
+    _require(rows is not None, "q or k is needed")
+    for name, t in (("q", q), ("k", k)):
+        if t is not None:
+            _head_rows(t, name, None, rows.device)
+            _require(t.is_cuda, "q and k must live on the GPU")
+            if t.shape[:3] != rows.shape[:3]:
+                _refuse("q and k must be of the same requests, layers and tokens")
+    B, L, T = rows.shape[:3]
+    rotation._fits(L, rows.device)
+    if positions.dtype != torch.int32 or tuple(positions.shape) not in ((B, T), (T,)) or (positions.stride(-1) != 1 and T > 1):
+        _refuse("positions must be int32 [%d, %d] or [%d], tokens contiguous" % (B, T, T))
+    if new_tokens is not None and (new_tokens.dtype != torch.int32 or tuple(new_tokens.shape) != (B,) or not new_tokens.is_contiguous()):
+        _refuse("new_tokens must be a contiguous int32 tensor of %d requests" % B)
+    for name, t in (("positions", positions), ("new_tokens", new_tokens)):
+        if t is not None and t.device != rows.device:
+            _refuse("%s must live on the GPU of the rows" % name)
+    if k is None and (want_plain or k_plain is not None or k_out is not None) or q is None and q_out is not None:
+        _refuse("an output without its rows")
+    if q is not None:
+        q_out = _head_rows_out(q_out, q, "q_out", stream)
+    if k is not None:
+        k_out = _head_rows_out(k_out, k, "k_out", stream)
+        if want_plain or k_plain is not None:
+            k_plain = _head_rows_out(k_plain, k, "k_plain", stream)
+    tensors = q, k, q_out, k_out, k_plain
+    strides = [s for t in tensors for s in (t.stride()[:4] if t is not None else (0, 0, 0, 0))]
+    c = _RotateRows(*[_ptr(t) for t in tensors], *strides, positions.data_ptr(), positions.stride(0) if positions.dim() == 2 and B > 1 else 0,
+                    _ptr(new_tokens), B, L, T, q.shape[3] if q is not None else 0, k.shape[3] if k is not None else 0)
+    _on_gpu(rows.device, stream, lambda st: _lib.compactor_rotate(rotation._ref, C.byref(c), st))
+    return q_out, k_out, k_plain
+
+
+def compactor_cache_append_rotated(cache: Cache, rotation: Rotation, k: torch.Tensor, v: torch.Tensor, q: Optional[torch.Tensor] = None,
+                                   new_tokens: Optional[torch.Tensor] = None, q_out=None, stream=None):
+    """compactor_cache_append of keys that are normed and rotated on the way, to the positions that they get, and the queries of the
+    same tokens likewise.  -> q rotated (None without q); rows of padding tokens are left as they are, in new memory they hold anything"""
+    _either(cache, False)
+    return _append_rotated(_lib.compactor_cache_append_rotated, cache, rotation, k, v, q, new_tokens, q_out, stream)
+
+
+def compactor_mx_append_rotated(cache: MxCache, rotation: Rotation, k: torch.Tensor, v: torch.Tensor, q: Optional[torch.Tensor] = None,
+                                new_tokens: Optional[torch.Tensor] = None, q_out=None, stream=None):
+    """compactor_cache_append_rotated, into a cache in 4 bits."""
+    _either(cache, True)
+    return _append_rotated(_lib.compactor_mx_append_rotated, cache, rotation, k, v, q, new_tokens, q_out, stream)
+
+
+def _append_rotated(call, cache, rotation, k, v, q, new_tokens, q_out, stream):
+    rows = _rows(cache, k, v, new_tokens)
+    rotation._fits(cache.layers, cache.device)
+    queries = None
+    if q is not None:
+        _head_rows(q, "q", None, cache.device)
+        if q.shape[:3] != k.shape[:3]:
+            _refuse("q and k must be of the same requests, layers and tokens")
+        q_out = _head_rows_out(q_out, q, "q_out", stream)
+        queries = C.byref(_RotateQueries(q.data_ptr(), q_out.data_ptr(), *q.stride()[:4], *q_out.stride()[:4], q.shape[3]))
+    elif q_out is not None:
+        _refuse("an output without its rows")
+    cache._on(stream, lambda st: call(cache._ref, rotation._ref, C.byref(rows), queries, st))
+    return q_out

@@ -85,6 +85,13 @@ __device__ __forceinline__ long long state_at(const CacheView &C, const HeadPlac
   return s.page * C.state_page_stride + p.state + s.at;
 }
 
+// The counts of a head that n tokens have been appended to.
+__device__ __forceinline__ void append_count(const CacheView &C, const HeadOf &w, int count, int seen, int n) {
+  const long long at = count_at(C, w.b, w.l, w.h);
+  C.counts[at] = n < C.capacity - count ? count + n : C.capacity;
+  if (C.seen != nullptr) C.seen[at] = (int)((unsigned)seen + (unsigned)n);
+}
+
 // Sum over the lanes up to this one (row shifts, then the sums of rows and of halves of the wave handed on).
 __device__ __forceinline__ int wave_scan(int x) {
   x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);

@@ -120,11 +120,6 @@ __device__ __forceinline__ void append_row(const CacheView &C, const NewRows &R,
     C.positions[at] = (int)((unsigned)seen + (unsigned)t);
   }
 }
-__device__ __forceinline__ void append_count(const CacheView &C, const HeadOf &w, int count, int seen, int n) {
-  const long long at = count_at(C, w.b, w.l, w.h);
-  C.counts[at] = n < C.capacity - count ? count + n : C.capacity;
-  if (C.seen != nullptr) C.seen[at] = (int)((unsigned)seen + (unsigned)n);
-}
 
 // A group of 16 lanes per head takes all its rows and then moves its counts on.
 template <bool FP4>
