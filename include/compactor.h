@@ -535,6 +535,51 @@ int compactor_cache_append_rotated(const compactor_cache_t *cache, const compact
 int compactor_mx_append_rotated(const compactor_mx_cache_t *cache, const compactor_rotation_t *rotation, const compactor_cache_rows_t *rows,
                                 const compactor_rotate_queries_t *queries, void *stream);
 
+/* ---- pages -------------------------------------------------------------------------------- */
+/* Pages that caches share and give back.  refs, device, int32 [num_pages], is the program's: how many times the tables of its caches name a page (and
+ * whatever else holds it); 0: the page is free, and none is below 0.  The calls keep it up as they change the tables of `cache`, which they write to although
+ * compactor_cache_t has them const.  Its tables are those of all layers, so these calls take the cache of all of them; of the pool only the sizes are looked at,
+ * but by compactor_pages_copy, and a cache in 4 bits is passed as its member `cache`.  No two of them (on any caches) that share refs run at a time.
+ * nreq <= 16384.  Entries outside [0, num_pages) name no page. */
+
+/* Room for new tokens.  With n_b new tokens of request b, `top` the most and `low` the fewest tokens that one of its heads holds, its entries from
+ * ceil(top / page_size) up to ceil((top + n_b) / page_size) (or the table's end) that name no page get one, and a page from low / page_size on up to there that is
+ * named more than once is exchanged for a page of its own, a copy of it: an append can then write to all of them.  Where all that
+ * name a page are exchanged in this call, the last of them (by request, then entry) keeps it.  Free pages are given in ascending order, to entries by
+ * request, then place.  Where there are too few, nothing changes but `done`. */
+typedef struct compactor_pages_reserve_params {
+  int32_t *refs;
+  const int32_t *new_tokens;   /* as in compactor_cache_rows */
+  int32_t tokens;         /* T >= 0 */
+  int32_t own_all;        /* not 0: pages are exchanged from the first on, not from low / page_size (what accumulates into or evicts from all) */
+  int32_t *pairs;         /* device, int32 [min(nreq * table_len, num_pages)][2]: out, pages to copy: from, to */
+  int32_t *done;          /* device, int32 [2]: out, how many pairs; how many pages were too few (then no pairs) */
+} compactor_pages_reserve_params_t;
+int compactor_pages_reserve(const compactor_cache_t *cache, const compactor_pages_reserve_params_t *reserve, void *workspace, size_t workspace_bytes,
+                            void *stream);
+/* Bytes of 256-byte aligned device workspace, for reserve and for compact; scratch, no state is kept.  host. */
+int compactor_pages_reserve_workspace_size(const compactor_cache_t *cache, size_t *bytes);
+int compactor_pages_compact_workspace_size(const compactor_cache_t *cache, size_t *bytes);
+
+/* Copies pages, all layers and heads and, where the cache has them, mass and positions (and scales): of the first done[0] of at most max_pairs pairs.  No
+ * page is in two of them.  Pairs with a page that is not there are passed over. */
+int compactor_pages_copy(const compactor_cache_t *cache, const int32_t *pairs, int32_t max_pairs, const int32_t *done, void *stream);
+int compactor_mx_pages_copy(const compactor_mx_cache_t *cache, const int32_t *pairs, int32_t max_pairs, const int32_t *done, void *stream);
+
+/* Request b goes on as request parents[b] was (device, int32 [nreq]): its tables, counts and seen; all at once, so that parents may be any.  One outside [0, nreq): as it is.
+ * A page's rows and state are then shared until compactor_pages_reserve exchanges it. */
+int compactor_pages_fork(const compactor_cache_t *cache, int32_t *refs, const int32_t *parents, void *stream);
+
+/* Requests b with finished[b] != 0 (device, int32 [nreq], or NULL: none) hold and have seen nothing any more.  Of all, entries behind the last page that holds a token
+ * give their page back and become -1. */
+int compactor_pages_release(const compactor_cache_t *cache, int32_t *refs, const int32_t *finished, void *stream);
+
+/* Pushes the pages that are not free together to 0 .. n-1, n of them: those from n on go to the free ones below, the i-th highest to the i-th lowest; refs and the
+ * tables follow, pairs (as in reserve: int32 [num_pages / 2 + 1][2]) say what is to be copied and, to a program whose other tables name pages, what has moved;
+ * done: how many pairs, and n. */
+int compactor_pages_compact(const compactor_cache_t *cache, int32_t *refs, int32_t *pairs, int32_t *done, void *workspace, size_t workspace_bytes,
+                            void *stream);
+
 /* Context-calibrated retention (Sec. 3.4): the smallest r in (0,1] with
  * f(r) = (exp(r b - b) - exp(-b)) / (1 - exp(-b)) >= tau, b = alpha*nll + beta, i.e.
  * r* = 1 + ln(tau (1 - e^-b) + e^-b) / b (r* = tau in the limit b -> 0). host. */

@@ -20,7 +20,7 @@ INCLUDE = os.path.join(ROOT, "include")
 BUILD = os.path.join(ROOT, "_build")
 LIB = os.path.join(HERE, "libcompactor.so")
 SOURCES = ["api.hip", "gram.hip", "solve.hip", "score.hip", "select.hip", "gather.hip", "attention.hip",
-           "cache.hip", "cache_attention.hip", "fp4.hip", "fp4_attention.hip", "rotate.hip"]
+           "cache.hip", "cache_attention.hip", "fp4.hip", "fp4_attention.hip", "rotate.hip", "pages.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [

@@ -123,6 +123,11 @@ class _RotateQueries(C.Structure):
                 [("%s_stride_%s" % (n, d), C.c_int64) for n in ("q", "q_out") for d in "blth"] + [("q_heads", C.c_int32)])
 
 
+class _PagesReserve(C.Structure):
+    _fields_ = [("refs", C.c_void_p), ("new_tokens", C.c_void_p), ("tokens", C.c_int32), ("own_all", C.c_int32),
+                ("pairs", C.c_void_p), ("done", C.c_void_p)]
+
+
 _PP, _RP = C.POINTER(_Params), C.POINTER(_Request)
 _CP, _CQP, _CEP = C.POINTER(_Cache), C.POINTER(_CacheQuery), C.POINTER(_CacheEvict)
 _lib.compactor_cache_admit.argtypes = [_PP, _RP, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p, _CP,
@@ -144,6 +149,14 @@ _ROP = C.POINTER(_Rotation)
 _lib.compactor_rotate.argtypes = [_ROP, C.POINTER(_RotateRows), C.c_void_p]
 _lib.compactor_cache_append_rotated.argtypes = [_CP, _ROP, C.POINTER(_CacheRows), C.POINTER(_RotateQueries), C.c_void_p]
 _lib.compactor_mx_append_rotated.argtypes = [_MXP, _ROP, C.POINTER(_CacheRows), C.POINTER(_RotateQueries), C.c_void_p]
+_lib.compactor_pages_reserve.argtypes = [_CP, C.POINTER(_PagesReserve), C.c_void_p, C.c_size_t, C.c_void_p]
+_lib.compactor_pages_reserve_workspace_size.argtypes = [_CP, C.POINTER(C.c_size_t)]
+_lib.compactor_pages_compact_workspace_size.argtypes = [_CP, C.POINTER(C.c_size_t)]
+_lib.compactor_pages_copy.argtypes = [_CP, C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p]
+_lib.compactor_mx_pages_copy.argtypes = [_MXP, C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p]
+_lib.compactor_pages_fork.argtypes = [_CP, C.c_void_p, C.c_void_p, C.c_void_p]
+_lib.compactor_pages_release.argtypes = [_CP, C.c_void_p, C.c_void_p, C.c_void_p]
+_lib.compactor_pages_compact.argtypes = [_CP, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]
 _APP, _ARP = C.POINTER(_AttnParams), C.POINTER(_AttnRequest)
 _lib.compactor_attention_workspace_size.argtypes = [_APP, _ARP, C.c_int32, C.POINTER(C.c_size_t)]
 _lib.compactor_attention_scores.argtypes = [_APP, _ARP, C.c_int32, C.c_void_p, C.c_void_p,
@@ -187,7 +200,10 @@ EXPORTS = ["compactor_default_params", "compactor_keep_count", "compactor_layout
            "compactor_cache_evict_workspace_size",
            "compactor_mx_append", "compactor_mx_store", "compactor_mx_read", "compactor_mx_attention",
            "compactor_mx_attention_workspace_size", "compactor_mx_evict", "compactor_mx_evict_workspace_size",
-           "compactor_rotate", "compactor_cache_append_rotated", "compactor_mx_append_rotated"]
+           "compactor_rotate", "compactor_cache_append_rotated", "compactor_mx_append_rotated",
+           "compactor_pages_reserve", "compactor_pages_reserve_workspace_size", "compactor_pages_compact",
+           "compactor_pages_compact_workspace_size", "compactor_pages_copy", "compactor_mx_pages_copy",
+           "compactor_pages_fork", "compactor_pages_release"]
 
 
 STAGES = ["gram", "reduce", "solve", "score", "blend", "select", "gather"]
@@ -754,13 +770,13 @@ class Cache:
         _require(0 <= first and count >= 1 and first + count <= self.layers, "no such layers")
         at = slice(first, first + count)
         some = lambda t: None if t is None else t[:, at]      # noqa: E731
-        return self._of(self.k_pages[:, at], self.v_pages[:, at], *[some(t) for t in self._scales], self.tables, self.counts[:, at],
-                        some(self.seen), some(self.mass), some(self.positions))
+        part = type(self)(self.k_pages[:, at], self.v_pages[:, at], *[some(t) for t in self._scales], self.tables, self.counts[:, at],
+                          some(self.seen), some(self.mass), some(self.positions))
+        part._whole = self._whole and count == self.layers
+        return part
 
     _scales = ()
-
-    def _of(self, *tensors):
-        return type(self)(*tensors)
+    _whole = True                 # of all the layers that share the tables
 
     def _new_tokens(self, t: Optional[torch.Tensor]) -> int:
         if t is None:
@@ -1228,3 +1244,112 @@ def _append_rotated(call, cache, rotation, k, v, q, new_tokens, q_out, stream):
         _refuse("an output without its rows")
     cache._on(stream, lambda st: call(cache._ref, rotation._ref, C.byref(rows), queries, st))
     return q_out
+
+
+def _pages(cache: Cache, **tensors):
+    """Checks of the calls that change tables -> the cache, as they take it.  tensors: (tensor, shape), int32 and contiguous, or None"""
+    if not cache._whole:
+        _refuse("the pages are those of all layers: this call takes the cache that layer() was called on")
+    for name, (t, shape) in tensors.items():
+        if t is None:
+            continue
+        if t.dtype != torch.int32 or tuple(t.shape) != shape or not t.is_contiguous():
+            _refuse("%s must be a contiguous int32 tensor %s" % (name, list(shape)))
+        if t.device != cache.device:
+            _refuse("%s must live on the GPU of the cache" % name)
+    return C.byref(cache._c)
+
+
+def _pages_bytes(call, cache: Cache) -> int:
+    need = cache._bytes.get(call.__name__)
+    if need is None:
+        out = C.c_size_t(0)
+        _check(call(C.byref(cache._c), C.byref(out)))
+        need = cache._bytes[call.__name__] = int(out.value)
+    return need
+
+
+def _pages_workspace(call, cache, given, stream):
+    if given is None:
+        given = _empty(stream, _pages_bytes(call, cache), returned=False, dtype=torch.uint8, device=cache.device)
+    else:
+        _out(given, 0, torch.uint8, "workspace")
+        if given.device != cache.device:
+            _refuse("the workspace must live on the GPU of the cache")
+    return given
+
+
+def _pages_out(cache, pairs, most, done, stream):
+    got = []
+    for t, shape in ((pairs, (most, 2)), (done, (2,))):
+        got.append(_empty(stream, shape, dtype=torch.int32, device=cache.device) if t is None else t)
+    return got
+
+
+def compactor_pages_reserve_workspace_size(cache: Cache) -> int:
+    return _pages_bytes(_lib.compactor_pages_reserve_workspace_size, cache)
+
+
+def compactor_pages_compact_workspace_size(cache: Cache) -> int:
+    return _pages_bytes(_lib.compactor_pages_compact_workspace_size, cache)
+
+
+def compactor_pages_reserve(cache: Cache, refs: torch.Tensor, tokens: int, new_tokens: Optional[torch.Tensor] = None, own_all: bool = False,
+                            pairs=None, done=None, workspace=None, stream=None):
+    """Room for new tokens: entries of the tables that they need get free pages, pages that others name too are exchanged.  refs:
+    int32 [page], how many times each is named, 0 a free one.  -> (pairs int32 [most, 2], done int32 [2]: how many pairs, how many pages were
+    too few), for compactor_pages_copy.  cache: of 16 or 4 bits, here and in the calls below."""
+    N = cache._c.pool.num_pages
+    most = min(cache.nreq * cache._c.table_len, N)
+    _int32(tokens=tokens)
+    ref = _pages(cache, refs=(refs, (N,)), pairs=(pairs, (most, 2)), done=(done, (2,)))
+    pairs, done = _pages_out(cache, pairs, most, done, stream)
+    ws = _pages_workspace(_lib.compactor_pages_reserve_workspace_size, cache, workspace, stream)
+    c = _PagesReserve(refs.data_ptr(), cache._new_tokens(new_tokens), tokens, 1 if own_all else 0, pairs.data_ptr(), done.data_ptr())
+    cache._on(stream, lambda st: _lib.compactor_pages_reserve(ref, C.byref(c), ws.data_ptr(), ws.numel(), st))
+    return pairs, done
+
+
+def _copy(call, cache, pairs, done, stream):
+    _pages(cache, done=(done, (2,)))
+    if pairs.dtype != torch.int32 or pairs.dim() != 2 or pairs.shape[1] != 2 or pairs.shape[0] < 1 or not pairs.is_contiguous():
+        _refuse("pairs must be a contiguous int32 tensor [most, 2]")
+    if pairs.device != cache.device:
+        _refuse("pairs must live on the GPU of the cache")
+    cache._on(stream, lambda st: call(cache._ref, pairs.data_ptr(), pairs.shape[0], done.data_ptr(), st))
+
+
+def compactor_pages_copy(cache: Cache, pairs: torch.Tensor, done: torch.Tensor, stream=None):
+    """Copies the pages of the first done[0] pairs (from, to): rows of all layers and heads and their state."""
+    _either(cache, False)
+    _copy(_lib.compactor_pages_copy, cache, pairs, done, stream)
+
+
+def compactor_mx_pages_copy(cache: MxCache, pairs: torch.Tensor, done: torch.Tensor, stream=None):
+    """compactor_pages_copy, of a cache in 4 bits."""
+    _either(cache, True)
+    _copy(_lib.compactor_mx_pages_copy, cache, pairs, done, stream)
+
+
+def compactor_pages_fork(cache: Cache, refs: torch.Tensor, parents: torch.Tensor, stream=None):
+    """Request b goes on as request parents[b] was, on its pages.  parents: int32 [request]"""
+    ref = _pages(cache, refs=(refs, (cache._c.pool.num_pages,)), parents=(parents, (cache.nreq,)))
+    cache._on(stream, lambda st: _lib.compactor_pages_fork(ref, refs.data_ptr(), parents.data_ptr(), st))
+
+
+def compactor_pages_release(cache: Cache, refs: torch.Tensor, finished: Optional[torch.Tensor] = None, stream=None):
+    """Gives back the pages behind the last token of every request, and all of those that are finished (int32 [request], not 0)."""
+    ref = _pages(cache, refs=(refs, (cache._c.pool.num_pages,)), finished=(finished, (cache.nreq,)))
+    cache._on(stream, lambda st: _lib.compactor_pages_release(ref, refs.data_ptr(), _ptr(finished), st))
+
+
+def compactor_pages_compact(cache: Cache, refs: torch.Tensor, pairs=None, done=None, workspace=None, stream=None):
+    """Pushes the pages that are not free together to the lowest numbers.  -> (pairs int32 [most, 2], done int32 [2]: how many pairs, how many pages
+    are not free), for compactor_pages_copy"""
+    N = cache._c.pool.num_pages
+    most = N // 2 + 1
+    ref = _pages(cache, refs=(refs, (N,)), pairs=(pairs, (most, 2)), done=(done, (2,)))
+    pairs, done = _pages_out(cache, pairs, most, done, stream)
+    ws = _pages_workspace(_lib.compactor_pages_compact_workspace_size, cache, workspace, stream)
+    cache._on(stream, lambda st: _lib.compactor_pages_compact(ref, refs.data_ptr(), pairs.data_ptr(), done.data_ptr(), ws.data_ptr(), ws.numel(), st))
+    return pairs, done
