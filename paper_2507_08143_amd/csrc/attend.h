@@ -188,6 +188,9 @@ __device__ __forceinline__ HeadSize head_size(const CacheView &C, const Queries 
 // heads on each is cut into the same few parts (split_part): 1024 heads of 4000, us with a scan / a plan / parts 407 / 384 / 360, of 250 to 8000
 // 249 / 237 / 232, 4096 of 2000 1045 / 786 / 692.  -> false: there is no such fragment.
 constexpr int SCAN_GROUP = 4;                // of 64 heads whose sizes are fetched together; the first stays
+// PAIRS: rows of two heads share the lines of memory; the parts of both with the same slots go to one XCD, which reads a line once (workgroups go round the
+// eight).
+template <bool PAIRS = false>
 __device__ __forceinline__ bool scan_part(const CacheView &C, const Queries &Q, int fragment, Fragment &F) {
   const int heads = C.nreq * C.layers * C.kv_heads, lane = threadIdx.x & 63;
   HeadSize size[SCAN_GROUP];
@@ -228,7 +231,13 @@ __device__ __forceinline__ bool scan_part(const CacheView &C, const Queries &Q, 
         F.n = __builtin_amdgcn_readlane(size[i].n, at);
         F.parts = __builtin_amdgcn_readlane(parts, at);
         F.first = __builtin_amdgcn_readlane(upto, at) - F.parts;
-        F.step0 = (fragment - F.first) * each;
+        int k = fragment - F.first;
+        if (PAIRS && (at & 1)) {             // the parts of the head before take as many workgroups more or less than whole rounds of the XCDs
+          const int turn = __builtin_amdgcn_readlane(parts, at - 1) & 7;
+          k += turn < F.parts ? turn : 0;
+          k -= k >= F.parts ? F.parts : 0;
+        }
+        F.step0 = k * each;
         F.step1 = min(F.step0 + each, __builtin_amdgcn_readlane(steps, at));
         return true;
       }
@@ -240,10 +249,14 @@ __device__ __forceinline__ bool scan_part(const CacheView &C, const Queries &Q, 
 
 // Part blockIdx.x / heads of a head.  Workgroups go round the eight XCDs, and heads often come in eights: neighbours in a group of eight
 // change places from group to group, or an XCD would have the same kv head of every request, long or short.
+template <bool PAIRS = false>
 __device__ __forceinline__ bool split_part(const CacheView &C, const Queries &Q, Fragment &F, int &fragment) {
   const unsigned heads = (unsigned)C.nreq * (unsigned)C.layers * (unsigned)C.kv_heads;
   const unsigned part = Q.split == 1 ? 0u : blockIdx.x / heads, i = blockIdx.x - part * heads;
-  F.head = (int)((i | 7u) < heads ? (i & ~7u) | ((i + (i >> 3) + part) & 7u) : i);
+  if (PAIRS)
+    F.head = (int)((i | 15u) < heads ? (i & ~15u) | (((i + (i >> 4) + part) & 7u) << 1) | (i >> 3 & 1u) : i);
+  else
+    F.head = (int)((i | 7u) < heads ? (i & ~7u) | ((i + (i >> 3) + part) & 7u) : i);
   const HeadSize size = head_size(C, Q, (unsigned)F.head);
   F.count = size.count;
   F.n = size.n;
@@ -297,11 +310,15 @@ __device__ __forceinline__ Scaling scaling_of(const Queries &Q) {
   return Scaling{capped, Q.scale * LOG2E, capped ? Q.scale / Q.softcap : 0.f, Q.softcap * LOG2E};
 }
 // tanh(y) = 1 - 2 / (e^2y + 1); near 0, where that cancels, y times a polynomial in y^2
-__device__ __forceinline__ float capped_logit(const Scaling &c, float dot) {
+__device__ __forceinline__ float capped_small(const Scaling &c, float dot) {         // |y| < 1/4
   const float y = dot * c.to_y, z = y * y;
-  const float far = c.cap2 - 2.f * c.cap2 * __builtin_amdgcn_rcpf(exp2_(y * (2.f * LOG2E)) + 1.f);
   const float slope = fmaf(z, fmaf(z, fmaf(z, fmaf(z, 62.f / 2835.f, -17.f / 315.f), 2.f / 15.f), -1.f / 3.f), 1.f);
-  return z < 1.f / 16.f ? dot * c.to_base2 * slope : far;
+  return dot * c.to_base2 * slope;
+}
+__device__ __forceinline__ float capped_logit(const Scaling &c, float dot) {
+  const float y = dot * c.to_y;
+  const float far = c.cap2 - 2.f * c.cap2 * __builtin_amdgcn_rcpf(exp2_(y * (2.f * LOG2E)) + 1.f);
+  return y * y < 1.f / 16.f ? capped_small(c, dot) : far;
 }
 
 // Where the maximum is -inf the sum is 0 (nothing was seen) or NaN (only logits that are none), which stays.
@@ -460,8 +477,10 @@ __device__ __forceinline__ void weights_to_mass(const CacheView &C, const Querie
 struct AttendKernels {
   void (*attend)(const CacheView &C, const Queries &Q, bool row16, unsigned blocks, hipStream_t st);
   void (*mass)(const CacheView &C, const Queries &Q, bool row16, unsigned blocks, hipStream_t st);
+  int again_rows;              // weights of more rows, with logits of more bytes, are found from K
+  size_t again_bytes;
 };
-int attend_workspace(const CacheView &C, const compactor_cache_query_t *query, size_t *bytes);
+int attend_workspace(const CacheView &C, const compactor_cache_query_t *query, const AttendKernels &kernels, size_t *bytes);
 int attend_call(const CacheView &C, const compactor_cache_query_t *query, const AttendKernels &kernels, bool row16, void *workspace,
                 size_t workspace_bytes, void *stream);
 

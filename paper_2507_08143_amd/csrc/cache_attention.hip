@@ -526,7 +526,7 @@ struct AttendPlan {
   size_t bytes() const { return frags + head_frags + partial + stats + logits; }
 };
 
-static AttendPlan attend_plan(const CacheView &C, const compactor_cache_query_t *q) {
+static AttendPlan attend_plan(const CacheView &C, const compactor_cache_query_t *q, const AttendKernels &kernels) {
   int dev = 0, cus = 0;
   if (hipGetDevice(&dev) != hipSuccess ||
       hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess || cus <= 0)
@@ -548,7 +548,7 @@ static AttendPlan attend_plan(const CacheView &C, const compactor_cache_query_t 
   A.joined = A.frags_most > 0;
   A.pitch = (int)((most + ATT_TILE - 1) / ATT_TILE * ATT_TILE);
   const size_t a_row = (size_t)heads * A.pitch * sizeof(float);
-  A.again = q->accumulate && A.rows > AGAIN_ROWS && a_row * A.rows > AGAIN_BYTES;
+  A.again = q->accumulate && A.rows > kernels.again_rows && a_row * A.rows > kernels.again_bytes;
   if (A.again && A.frags_most == 0) A.frags_most = (int)heads;        // one each, for what is known of them
   auto up = [](size_t x) { return (x + 255) / 256 * 256; };
   const size_t n = A.frags_most;
@@ -577,11 +577,11 @@ static void launch_mass(const CacheView &C, const Queries &Q, unsigned blocks, h
   hipLaunchKernelGGL(kernel, dim3(blocks), dim3(256), 0, st, C, Q);
 }
 
-int attend_workspace(const CacheView &C, const compactor_cache_query_t *query, size_t *bytes) {
+int attend_workspace(const CacheView &C, const compactor_cache_query_t *query, const AttendKernels &kernels, size_t *bytes) {
   const int rc = query_check(query, C);
   if (rc) return rc;
   if (!bytes) return COMPACTOR_EINVAL;
-  *bytes = attend_plan(C, query).bytes();
+  *bytes = attend_plan(C, query, kernels).bytes();
   return COMPACTOR_OK;
 }
 
@@ -598,7 +598,7 @@ int attend_call(const CacheView &C, const compactor_cache_query_t *query, const 
         query->out_stride_l | query->out_stride_t | query->out_stride_h) & 7) ||
       ((reinterpret_cast<uintptr_t>(query->lse) | reinterpret_cast<uintptr_t>(query->new_tokens)) & 3u))
     return COMPACTOR_EALIGN;
-  const AttendPlan A = attend_plan(C, query);
+  const AttendPlan A = attend_plan(C, query, kernels);
   const size_t need = A.bytes();
   if (need > 0 && (!workspace || workspace_bytes < need)) return COMPACTOR_EWORKSPACE;
   if (need > 0 && (reinterpret_cast<uintptr_t>(workspace) & 255u)) return COMPACTOR_EALIGN;
@@ -646,6 +646,18 @@ int attend_call(const CacheView &C, const compactor_cache_query_t *query, const 
   return hipGetLastError() == hipSuccess ? COMPACTOR_OK : COMPACTOR_EHIP;
 }
 
+static const AttendKernels &attend_kernels() {
+  static const AttendKernels kernels = {
+      [](const CacheView &C, const Queries &Q, bool row16, unsigned blocks, hipStream_t st) {
+        row16 ? launch_attend<true>(C, Q, blocks, st) : launch_attend<false>(C, Q, blocks, st);
+      },
+      [](const CacheView &C, const Queries &Q, bool row16, unsigned blocks, hipStream_t st) {
+        row16 ? launch_mass<true>(C, Q, blocks, st) : launch_mass<false>(C, Q, blocks, st);
+      },
+      AGAIN_ROWS, AGAIN_BYTES};
+  return kernels;
+}
+
 }  // namespace cmp
 
 using namespace cmp;
@@ -657,7 +669,7 @@ int compactor_cache_attention_workspace_size(const compactor_cache_t *cache, con
                                              size_t *bytes) {
   CacheView C;
   const int rc = cache_view(cache, CACHE_SIZES, &C);
-  return rc ? rc : attend_workspace(C, query, bytes);
+  return rc ? rc : attend_workspace(C, query, attend_kernels(), bytes);
 }
 
 int compactor_cache_attention(const compactor_cache_t *cache, const compactor_cache_query_t *query, void *workspace,
@@ -665,15 +677,8 @@ int compactor_cache_attention(const compactor_cache_t *cache, const compactor_ca
   CacheView C;
   const int rc = cache_view(cache, query && query->accumulate ? CACHE_STATE : CACHE_ROWS, &C);
   if (rc) return rc;
-  static const AttendKernels kernels = {
-      [](const CacheView &C, const Queries &Q, bool row16, unsigned blocks, hipStream_t st) {
-        row16 ? launch_attend<true>(C, Q, blocks, st) : launch_attend<false>(C, Q, blocks, st);
-      },
-      [](const CacheView &C, const Queries &Q, bool row16, unsigned blocks, hipStream_t st) {
-        row16 ? launch_mass<true>(C, Q, blocks, st) : launch_mass<false>(C, Q, blocks, st);
-      }};
   // halves of tiles with one origin, and offsets inside one that fit 32 bits
-  return attend_call(C, query, kernels, C.page_size % 16 == 0 && C.slot_stride <= (1 << 24), workspace, workspace_bytes, stream);
+  return attend_call(C, query, attend_kernels(), C.page_size % 16 == 0 && C.slot_stride <= (1 << 24), workspace, workspace_bytes, stream);
 }
 
 #pragma GCC visibility pop

@@ -143,15 +143,24 @@ __device__ __forceinline__ void product_v(const VRows &v, const float (&scale)[8
   }
 }
 
-// Logits in base 2 of a tile; whole: all of its slots are there and seen by every query, else there_at has bit 16 (i >> 2) + (i & 3) for the lane's
-// i-th slot and `upto` says what its query sees of them.
+// Logits of a tile over `unit`, which makes them of base 2 (capped ones are of base 2 as they are: unit_of()).  whole: all of its slots are there and
+// seen by every query, else there_at has bit 16 (i >> 2) + (i & 3) for the lane's i-th slot and `upto` says what its query sees of them.
+__device__ __forceinline__ float unit_of(const Scaling &scaling) { return scaling.capped ? 1.f : scaling.to_base2; }
 __device__ __forceinline__ void tile_logits(const Scaling &scaling, const f32x4 (&s)[2], bool whole, unsigned there_at, int upto, float (&x)[8]) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) x[i] = s[i >> 2][i & 3];
   if (scaling.capped) {
+    // most logits are in the middle of the cap, where the series does
+    float top = 0.f;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = capped_logit(scaling, s[i >> 2][i & 3]);
-  } else {
+    for (int i = 0; i < 8; ++i) top = fmaxf(top, fabsf(x[i]));
+    if (__any(!(top * scaling.to_y < 0.25f))) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) x[i] = s[i >> 2][i & 3] * scaling.to_base2;
+      for (int i = 0; i < 8; ++i) x[i] = capped_logit(scaling, x[i]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) x[i] = capped_small(scaling, x[i]);
+    }
   }
   if (__builtin_expect(!whole, 0)) {
 #pragma unroll
@@ -178,14 +187,16 @@ struct Attend4Lds {
   int none;
 };
 
+// Workgroups a unit: three of up to 16 rows (with four, 128 registers, 384 heads of 8192 to 32000, 4 rows: 242 us instead of 210), one of more than 48 (two of
+// 256 registers: 192 heads of 16000 to 32000, 64 rows, 939 us instead of 424; of 40 rows, 330 with two and 500 with one).
 template <int NT, bool PAGE16>
-__global__ __launch_bounds__(256, NT == 1 ? 3 : NT == 2 ? 2 : 1) void attend4_kernel(const CacheView C, const Queries Q) {
+__global__ __launch_bounds__(256, NT == 1 ? 3 : NT <= 3 ? 2 : 1) void attend4_kernel(const CacheView C, const Queries Q) {
   __shared__ Attend4Lds<NT, PAGE16> L;
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63, n16 = lane & 15, j = lane >> 4;
   const int R = Q.tokens * Q.group;
   Fragment part;
   int fragment = (int)blockIdx.x;
-  if (!(Q.target > 0 ? scan_part(C, Q, fragment, part) : split_part(C, Q, part, fragment))) {
+  if (!(Q.target > 0 ? scan_part<true>(C, Q, fragment, part) : split_part<true>(C, Q, part, fragment))) {
     if (tid == 0) Q.frags[fragment].head = -1;
     return;
   }
@@ -227,6 +238,7 @@ __global__ __launch_bounds__(256, NT == 1 ? 3 : NT == 2 ? 2 : 1) void attend4_ke
     for (int c = 0; c < 8; ++c) acc[nt][c] = f32x4{0.f, 0.f, 0.f, 0.f};
   }
   const Scaling scaling = scaling_of(Q);
+  const float unit = unit_of(scaling);
   const bool store = Q.logits != nullptr && count <= Q.most;
   float *logits = Q.logits + (long long)part.head * R * Q.pitch;
 
@@ -286,16 +298,15 @@ __global__ __launch_bounds__(256, NT == 1 ? 3 : NT == 2 ? 2 : 1) void attend4_ke
       tile_logits(scaling, s[nt], whole, there_at, see[nt] - s0 - 4 * j, x);
       if (store && 16 * nt + n16 < R) {
         float *to = logits + (long long)(16 * nt + n16) * Q.pitch + s0 + 4 * j;
-        *reinterpret_cast<f32x4 *>(to) = f32x4{x[0], x[1], x[2], x[3]};
-        *reinterpret_cast<f32x4 *>(to + 16) = f32x4{x[4], x[5], x[6], x[7]};
+        *reinterpret_cast<f32x4 *>(to) = f32x4{x[0], x[1], x[2], x[3]} * unit;
+        *reinterpret_cast<f32x4 *>(to + 16) = f32x4{x[4], x[5], x[6], x[7]} * unit;
       }
       float top = x[0];
 #pragma unroll
       for (int i = 1; i < 8; ++i) top = fmaxf(top, x[i]);
-      top = quarters_max(top);
       // the reference moves only when it has fallen 2^8 behind: weights up to 2^8 keep their precision
-      if (__any(top > m[nt] + 8.f)) {
-        const float to = fmaxf(m[nt], top), f = to == -INFINITY ? 1.f : exp2_(m[nt] - to);
+      if (__any(top * unit > m[nt] + 8.f)) {
+        const float to = fmaxf(m[nt], quarters_max(top) * unit), f = to == -INFINITY ? 1.f : exp2_(m[nt] - to);
         m[nt] = to;
         l[nt] *= f;
 #pragma unroll
@@ -305,7 +316,7 @@ __global__ __launch_bounds__(256, NT == 1 ? 3 : NT == 2 ? 2 : 1) void attend4_ke
       float sum = 0.f;
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        x[i] = exp2_(x[i] - ref);
+        x[i] = exp2_(fmaf(x[i], unit, -ref));
         sum += x[i];
       }
       l[nt] += sum;
@@ -383,6 +394,7 @@ __global__ __launch_bounds__(256) void attend4_mass_kernel(const CacheView C, co
 #pragma unroll
   for (int nt = 0; nt < NT; ++nt) z[nt] = see[nt] > 0 ? lse2[16 * nt + n16] : INFINITY;
   const Scaling scaling = scaling_of(Q);
+  const float unit = unit_of(scaling);
   float *weights = Q.weights + (long long)part.head * Q.pitch;
 
   auto one_tile = [&](int tile, auto another) {
@@ -411,7 +423,7 @@ __global__ __launch_bounds__(256) void attend4_mass_kernel(const CacheView C, co
       float x[8];
       tile_logits(scaling, s[nt], whole, there >> (4 * j), see[nt] - s0 - 4 * j, x);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) sum[i] += z[nt] == INFINITY ? 0.f : exp2_(x[i] - z[nt]);
+      for (int i = 0; i < 8; ++i) sum[i] += z[nt] == INFINITY ? 0.f : exp2_(fmaf(x[i], unit, -z[nt]));
     }
     const float mine = lanes_sum(sum, n16);
     if (n16 < 8) weights[s0 + 16 * (n16 >> 2) + 4 * j + (n16 & 3)] = mine;
@@ -425,6 +437,12 @@ __global__ __launch_bounds__(256) void attend4_mass_kernel(const CacheView C, co
   weights_to_mass(C, Q, hp, weights, run, &none);
 }
 
+// Weights from K, read again: 64 bytes a slot against 8 for every row, which pays where the last cache does not hold the logits.  us with K / logits: 192 heads of
+// 4000 to 8000, 40 rows (logits of 183 MB) 136 / 173, 2000 to 4000 (46 MB) 67 / 60; 96 of 16000 to 32000, 20 rows (183 MB) 157 / 169, 16 rows (146 MB) 125 / 140; 96 of
+// 5000 to 9831, 20 rows (57 MB) 64 / 55; 384 of 8000 to 16000, 10 rows (184 MB) 249 / 242.
+constexpr int AGAIN4_ROWS = 12;
+constexpr size_t AGAIN4_BYTES = 128u << 20;
+
 template <bool PAGE16>
 static void launch_attend4(const CacheView &C, const Queries &Q, unsigned blocks, hipStream_t st) {
   const int rows = Q.tokens * Q.group;
@@ -436,8 +454,24 @@ static void launch_attend4(const CacheView &C, const Queries &Q, unsigned blocks
 }
 template <bool PAGE16>
 static void launch_mass4(const CacheView &C, const Queries &Q, unsigned blocks, hipStream_t st) {
-  const auto kernel = Q.tokens * Q.group <= 48 ? attend4_mass_kernel<3, PAGE16> : attend4_mass_kernel<4, PAGE16>;
+  const int rows = Q.tokens * Q.group;
+  const auto kernel = rows <= 16   ? attend4_mass_kernel<1, PAGE16>
+                      : rows <= 32 ? attend4_mass_kernel<2, PAGE16>
+                      : rows <= 48 ? attend4_mass_kernel<3, PAGE16>
+                                   : attend4_mass_kernel<4, PAGE16>;
   hipLaunchKernelGGL(kernel, dim3(blocks), dim3(256), 0, st, C, Q);
+}
+
+static const AttendKernels &attend4_kernels() {
+  static const AttendKernels kernels = {
+      [](const CacheView &C, const Queries &Q, bool row16, unsigned blocks, hipStream_t st) {
+        row16 ? launch_attend4<true>(C, Q, blocks, st) : launch_attend4<false>(C, Q, blocks, st);
+      },
+      [](const CacheView &C, const Queries &Q, bool row16, unsigned blocks, hipStream_t st) {
+        row16 ? launch_mass4<true>(C, Q, blocks, st) : launch_mass4<false>(C, Q, blocks, st);
+      },
+      AGAIN4_ROWS, AGAIN4_BYTES};
+  return kernels;
 }
 
 }  // namespace cmp
@@ -450,7 +484,7 @@ extern "C" {
 int compactor_mx_attention_workspace_size(const compactor_mx_cache_t *cache, const compactor_cache_query_t *query, size_t *bytes) {
   CacheView C;
   const int rc = cache_view(cache, CACHE_SIZES, &C);
-  return rc ? rc : attend_workspace(C, query, bytes);
+  return rc ? rc : attend_workspace(C, query, attend4_kernels(), bytes);
 }
 
 int compactor_mx_attention(const compactor_mx_cache_t *cache, const compactor_cache_query_t *query, void *workspace,
@@ -458,15 +492,8 @@ int compactor_mx_attention(const compactor_mx_cache_t *cache, const compactor_ca
   CacheView C;
   const int rc = cache_view(cache, query && query->accumulate ? CACHE_STATE : CACHE_ROWS, &C);
   if (rc) return rc;
-  static const AttendKernels kernels = {
-      [](const CacheView &C, const Queries &Q, bool row16, unsigned blocks, hipStream_t st) {
-        row16 ? launch_attend4<true>(C, Q, blocks, st) : launch_attend4<false>(C, Q, blocks, st);
-      },
-      [](const CacheView &C, const Queries &Q, bool row16, unsigned blocks, hipStream_t st) {
-        row16 ? launch_mass4<true>(C, Q, blocks, st) : launch_mass4<false>(C, Q, blocks, st);
-      }};
   // halves of tiles with one origin, and offsets inside one that fit 32 bits
-  return attend_call(C, query, kernels, C.page_size % 16 == 0 && C.slot_stride <= (1 << 24), workspace, workspace_bytes, stream);
+  return attend_call(C, query, attend4_kernels(), C.page_size % 16 == 0 && C.slot_stride <= (1 << 24), workspace, workspace_bytes, stream);
 }
 
 #pragma GCC visibility pop
