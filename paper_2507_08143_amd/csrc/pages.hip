@@ -78,33 +78,64 @@ struct Reserve {
 };
 enum EntryKind { WANTS_NONE, WANTS_PAGE, WANTS_COPY };
 
+// Entries of a request from .. to, those from `holds` on are for new tokens.
+__device__ __forceinline__ int4 span_of(const CacheView &C, const Reserve &R, int b, const Most &m) {
+  const int n = tokens_new(R.new_tokens, b, R.tokens), holds = pages_of(C, m.top);
+  const int need = pages_of(C, n < C.capacity - m.top ? m.top + n : C.capacity);
+  const int first = R.own_all ? 0 : n > 0 ? invariant_quotient((unsigned)m.low, C.div_mul, C.div_shift) : holds;
+  return make_int4(min(first, need), need, holds, 0);
+}
+__device__ __forceinline__ void reserve_done(const Reserve &R, int copies, int wants, int found) {
+  if (threadIdx.x != 0) return;
+  R.done[0] = copies;
+  R.done[1] = max(wants - found, 0);
+}
+// Which of the pages p .. p + 3 are free.
+__device__ __forceinline__ void four_free(const CacheView &C, const Reserve &R, int p, int (&is_free)[4]) {
+#pragma unroll
+  for (int i = 0; i < 4; ++i) is_free[i] = p + i < C.num_pages && R.refs[min(p + i, C.num_pages - 1)] == 0;
+}
+// The first `wants` free pages, in order, or as many as there are; -> how many.  first: four_free(4 * threadIdx.x).
+__device__ __forceinline__ int find_free(const CacheView &C, const Reserve &R, int wants, const int (&first)[4], int *pages, int *part) {
+  int found = 0;
+  for (int p0 = 0; p0 < C.num_pages && found < wants; p0 += 4 * PLAN_THREADS) {
+    const int p = p0 + 4 * (int)threadIdx.x;
+    int is_free[4] = {first[0], first[1], first[2], first[3]}, all;
+    if (p0 > 0) four_free(C, R, p, is_free);
+    const int mine = is_free[0] + is_free[1] + is_free[2] + is_free[3];
+    int at = found + plan_scan(mine, part, &all) - mine;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      if (is_free[i] && at < wants) pages[at] = p + i;
+      at += is_free[i];
+    }
+    found += all;
+  }
+  __syncthreads();                           // they are listed, and no count of references is looked at any more
+  return found;
+}
+__device__ __forceinline__ void give_page(const Reserve &R, int32_t *entry, int kind, int old, int page, int pair) {
+  *entry = page;
+  R.refs[page] = 1;
+  if (kind == WANTS_COPY) {
+    atomicAdd(&R.refs[old], -1);
+    R.pairs[pair] = make_int2(old, page);
+  }
+}
+
 __global__ __launch_bounds__(256) void reserve_spans_kernel(const CacheView C, const Reserve R) {
   __shared__ int2 part[4];
   const int b = (int)blockIdx.x;
   const Most m = most_of(C, b, part);
-  if (threadIdx.x != 0) return;
-  const int n = tokens_new(R.new_tokens, b, R.tokens), holds = pages_of(C, m.top);
-  const int need = pages_of(C, n < C.capacity - m.top ? m.top + n : C.capacity);
-  const int first = R.own_all ? 0 : n > 0 ? invariant_quotient((unsigned)m.low, C.div_mul, C.div_shift) : holds;
-  R.spans[b] = make_int4(min(first, need), need, holds, 0);
+  if (threadIdx.x == 0) R.spans[b] = span_of(C, R, b, m);
 }
 
 // Numbers that atomics have made, past the cache of the compute unit.
 __device__ __forceinline__ int atomic_read(const int *p) { return __hip_atomic_load(p, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT); }
 
-__global__ __launch_bounds__(PLAN_THREADS) void reserve_plan_kernel(const CacheView C, const Reserve R) {
-  __shared__ int part[PLAN_WAVES];
+// Any number of entries, by way of the workspace; the spans are there, with their numbers.
+__device__ __forceinline__ void reserve_many(const CacheView &C, const Reserve &R, int entries, const int (&first)[4], int *part) {
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
-  int entries = 0;
-  for (int b0 = 0; b0 < C.nreq; b0 += PLAN_THREADS) {
-    const int b = b0 + tid;
-    const int4 s = b < C.nreq ? R.spans[b] : make_int4(0, 0, 0, 0);
-    int all;
-    const int upto = plan_scan(s.y - s.x, part, &all);
-    if (b < C.nreq) R.spans[b].w = entries + upto - (s.y - s.x);
-    entries += all;
-  }
-  __syncthreads();
   for (int b = wave; b < C.nreq; b += PLAN_WAVES) {
     const int4 s = R.spans[b];
     for (int i = s.x + lane; i < s.y; i += 64) {
@@ -147,45 +178,123 @@ __global__ __launch_bounds__(PLAN_THREADS) void reserve_plan_kernel(const CacheV
     }
     wants += kind != WANTS_NONE;
   }
-  int found = 0;
   plan_scan(wants, part, &wants);
-  for (int p0 = 0; p0 < C.num_pages && found < wants; p0 += 4 * PLAN_THREADS) {
-    const int p = p0 + 4 * tid;
-    int is_free[4], all;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) is_free[i] = p + i < C.num_pages && R.refs[min(p + i, C.num_pages - 1)] == 0;
-    const int mine = is_free[0] + is_free[1] + is_free[2] + is_free[3];
-    int at = found + plan_scan(mine, part, &all) - mine;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      if (is_free[i] && at < wants) R.free_pages[at] = p + i;
-      at += is_free[i];
-    }
-    found += all;
-  }
-  __syncthreads();                           // the free pages are listed, and no count of references is looked at any more
+  const int found = find_free(C, R, wants, first, R.free_pages, part);
   int given = 0, copies = 0;
   for (int e0 = 0; e0 < entries && found >= wants && wants > 0; e0 += PLAN_THREADS) {
     const int e = e0 + tid, kind = e < entries ? R.kinds[e] : WANTS_NONE;
     int all;
-    const int mine = (kind != WANTS_NONE) + ((kind == WANTS_COPY) << 16), upto = plan_scan(mine, part, &all) - mine;
-    if (kind != WANTS_NONE) {
-      const int page = R.free_pages[given + (upto & 0xffff)];
-      *entry_of(e) = page;
-      R.refs[page] = 1;
-      if (kind == WANTS_COPY) {
-        const int old = R.pages[e];
-        atomicAdd(&R.refs[old], -1);
-        R.pairs[copies + (upto >> 16)] = make_int2(old, page);
-      }
-    }
+    const int mine = (kind != WANTS_NONE) + ((kind == WANTS_COPY) << 16), before = plan_scan(mine, part, &all) - mine;
+    if (kind != WANTS_NONE) give_page(R, entry_of(e), kind, R.pages[e], R.free_pages[given + (before & 0xffff)], copies + (before >> 16));
     given += all & 0xffff;
     copies += all >> 16;
   }
-  if (tid == 0) {
-    R.done[0] = copies;
-    R.done[1] = max(wants - found, 0);
+  reserve_done(R, copies, wants, found);
+}
+
+__global__ __launch_bounds__(PLAN_THREADS) void reserve_plan_kernel(const CacheView C, const Reserve R) {
+  __shared__ int part[PLAN_WAVES];
+  int first[4];
+  four_free(C, R, 4 * (int)threadIdx.x, first);
+  int entries = 0;
+  for (int b0 = 0; b0 < C.nreq; b0 += PLAN_THREADS) {
+    const int b = b0 + (int)threadIdx.x;
+    const int4 s = b < C.nreq ? R.spans[b] : make_int4(0, 0, 0, 0);
+    int all;
+    const int upto = plan_scan(s.y - s.x, part, &all);
+    if (b < C.nreq) R.spans[b].w = entries + upto - (s.y - s.x);
+    entries += all;
   }
+  __syncthreads();
+  reserve_many(C, R, entries, first, part);
+}
+
+// Up to an entry a thread, which is a step of nearly any program: all in registers and LDS, one launch, and three loads that wait for each other (counts,
+// entry, references).  64 requests of which some need a page: 14.2 and 3.1 us in two launches by way of the workspace, FEW_TIME in this one.
+// More entries go the other way.
+constexpr int FEW_REQUESTS = PLAN_THREADS;
+constexpr long long FEW_COUNTS = 65536;
+__global__ __launch_bounds__(PLAN_THREADS) void reserve_few_kernel(const CacheView C, const Reserve R) {
+  __shared__ int part[PLAN_WAVES];
+  __shared__ int4 spans[FEW_REQUESTS];
+  __shared__ int4 named4[PLAN_THREADS / 4];              // pages that entries would have copies of, else -1
+  __shared__ int free_pages[PLAN_THREADS];
+  int *named = reinterpret_cast<int *>(named4);
+  const int tid = threadIdx.x, row = tid >> 4, lane = tid & 15, heads = C.layers * C.kv_heads;
+  int first[4];
+  four_free(C, R, 4 * tid, first);
+  for (int b0 = 0; b0 < C.nreq; b0 += PLAN_THREADS / 16) {
+    const int b = b0 + row;
+    int top = 0, low = C.capacity;
+    if (b < C.nreq) {
+      auto take = [&](int count) {
+        const int n = clamp_to(count, C.capacity);
+        top = max(top, n);
+        low = min(low, n);
+      };
+      if (C.layers == 1 || C.count_stride_l == C.kv_heads) {             // a request's counts lie together
+        const int32_t *counts = C.counts + b * C.count_stride_b;
+#pragma unroll 16
+        for (int i = lane; i < heads; i += 16) take(counts[i]);
+      } else {
+#pragma unroll 4
+        for (int i = lane; i < heads; i += 16) {
+          const int l = invariant_quotient((unsigned)i, C.layer_mul, C.layer_shift);
+          take(C.counts[count_at(C, b, l, i - l * C.kv_heads)]);
+        }
+      }
+    }
+    for (int d = 8; d > 0; d >>= 1) {
+      top = max(top, __shfl_xor(top, d));
+      low = min(low, __shfl_xor(low, d));
+    }
+    if (lane == 0 && b < C.nreq) spans[b] = span_of(C, R, b, Most{top, low});
+  }
+  __syncthreads();
+  int4 s = tid < C.nreq ? spans[tid] : make_int4(0, 0, 0, 0);
+  int entries;
+  const int upto = plan_scan(s.y - s.x, part, &entries);
+  s.w = upto - (s.y - s.x);
+  if (tid < C.nreq) {
+    spans[tid].w = s.w;
+    if (entries > PLAN_THREADS) R.spans[tid] = s;
+  }
+  __syncthreads();
+  if (entries > PLAN_THREADS) {
+    reserve_many(C, R, entries, first, part);
+    return;
+  }
+  // the request of entry `tid`: the last whose first entry is not behind it
+  int b = 0;
+  for (int d = PLAN_THREADS / 2; d > 0; d >>= 1)
+    if (b + d < C.nreq && spans[b + d].w <= tid) b += d;
+  const bool is = tid < entries;
+  s = spans[b];
+  const int i = s.x + tid - s.w;
+  int32_t *entry = R.tables + b * C.table_stride + i;
+  const int page = is ? *entry : -1;
+  const bool there = page_there(C, page);
+  int kind = !is ? WANTS_NONE : !there ? (i >= s.z ? WANTS_PAGE : WANTS_NONE) : WANTS_NONE, refs = 0;
+  if (there && (refs = R.refs[page]) > 1) kind = WANTS_COPY;
+  named[tid] = kind == WANTS_COPY ? page : -1;
+  if (__syncthreads_or(kind == WANTS_COPY)) {
+    if (kind == WANTS_COPY) {
+      int tally = 0, last = 0;
+#pragma unroll 8
+      for (int k = 0; k < (entries + 3) / 4; ++k) {
+        const int4 x = named4[k];
+        tally += (x.x == page) + (x.y == page) + (x.z == page) + (x.w == page);
+        last = x.w == page ? 4 * k + 3 : x.z == page ? 4 * k + 2 : x.y == page ? 4 * k + 1 : x.x == page ? 4 * k : last;
+      }
+      if (tally == refs && last == tid) kind = WANTS_NONE;             // keeps it
+    }
+  }
+  const int mine = (kind != WANTS_NONE) + ((kind == WANTS_COPY) << 16);
+  int all;
+  const int before = plan_scan(mine, part, &all) - mine, wants = all & 0xffff;
+  const int found = find_free(C, R, wants, first, free_pages, part);
+  if (found >= wants && kind != WANTS_NONE) give_page(R, entry, kind, page, free_pages[before & 0xffff], before >> 16);
+  reserve_done(R, found >= wants ? all >> 16 : 0, wants, found);
 }
 
 // ------------------------------------------------------------------------------------------ fork
@@ -339,7 +448,13 @@ struct Copy {
   Runs row, word;
   int row_chunks, chunks;      // of K (V) of a page; of a page
 };
+// Written past the caches: what is read is often shared by several copies, and what is written nobody reads for a while.  us of 112 copies of 16 pages of all layers
+// (477 MB in and out) 65, with plain stores 75 at the same number of workgroups; 3570 pages of 0.27 MB (1.9 GB) 427.  With 8 workgroups a unit 74 and 463, with 32 66 and
+// 427; 8 units a thread 80 and 427.
 constexpr int COPY_AT_ONCE = 4;              // units of a thread
+constexpr int COPY_WORKGROUPS = 4;           // a compute unit
+__device__ __forceinline__ void put(char *p, const uint4 &x) { store_stream16(p, x); }
+__device__ __forceinline__ void put(char *p, unsigned x) { *reinterpret_cast<unsigned *>(p) = x; }
 
 __device__ __forceinline__ long long unit_at(const Runs &R, int u, int bytes) {
   if (R.dims == 0) return (long long)u * bytes;
@@ -367,7 +482,7 @@ __device__ __forceinline__ void copy_chunk(char *base, const Runs &R, int2 pair,
     }
 #pragma unroll
   for (int i = 0; i < COPY_AT_ONCE; ++i)
-    if (u0 + 256 * i < R.units) *reinterpret_cast<T *>(base + pair.y * R.page + at[i]) = x[i];
+    if (u0 + 256 * i < R.units) put(base + pair.y * R.page + at[i], x[i]);
 }
 __global__ __launch_bounds__(256) void copy_kernel(const CacheView C, const Copy P) {
   const long long all = (long long)clamp_to(P.done[0], P.most) * P.chunks;
@@ -437,7 +552,7 @@ static int copy_call(const CacheView &C, const int32_t *pairs, int max_pairs, co
   int dev = 0, cus = 0;
   if (hipGetDevice(&dev) != hipSuccess || hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess || cus <= 0)
     cus = 256;
-  const unsigned blocks = (unsigned)std::min((long long)max_pairs * P.chunks, 8ll * cus);
+  const unsigned blocks = (unsigned)std::min((long long)max_pairs * P.chunks, (long long)COPY_WORKGROUPS * cus);
   (void)hipGetLastError();   // a leftover of earlier, unrelated HIP calls is not this call's error
   hipLaunchKernelGGL(copy_kernel, dim3(blocks), dim3(256), 0, static_cast<hipStream_t>(stream), C, P);
   return hipGetLastError() == hipSuccess ? COMPACTOR_OK : COMPACTOR_EHIP;
@@ -512,9 +627,13 @@ int compactor_pages_reserve(const compactor_cache_t *cache, const compactor_page
   R.done = reserve->done;
   hipStream_t st = static_cast<hipStream_t>(stream);
   (void)hipGetLastError();   // a leftover of earlier, unrelated HIP calls is not this call's error
-  hipLaunchKernelGGL(reserve_spans_kernel, dim3((unsigned)C.nreq), dim3(256), 0, st, C, R);
-  if (hipGetLastError() != hipSuccess) return COMPACTOR_EHIP;
-  hipLaunchKernelGGL(reserve_plan_kernel, dim3(1), dim3(PLAN_THREADS), 0, st, C, R);
+  if (C.nreq <= FEW_REQUESTS && (long long)C.nreq * C.layers * C.kv_heads <= FEW_COUNTS) {
+    hipLaunchKernelGGL(reserve_few_kernel, dim3(1), dim3(PLAN_THREADS), 0, st, C, R);
+  } else {
+    hipLaunchKernelGGL(reserve_spans_kernel, dim3((unsigned)C.nreq), dim3(256), 0, st, C, R);
+    if (hipGetLastError() != hipSuccess) return COMPACTOR_EHIP;
+    hipLaunchKernelGGL(reserve_plan_kernel, dim3(1), dim3(PLAN_THREADS), 0, st, C, R);
+  }
   return hipGetLastError() == hipSuccess ? COMPACTOR_OK : COMPACTOR_EHIP;
 }
 
@@ -537,7 +656,7 @@ int compactor_pages_fork(const compactor_cache_t *cache, int32_t *refs, const in
   if (!refs || !parents) return COMPACTOR_EINVAL;
   if (!on4(refs) || !on4(parents)) return COMPACTOR_EALIGN;
   Fork F{const_cast<int32_t *>(cache->tables), refs, parents, cache->table_len, 6, 0, 0};
-  while (F.width_log > 0 && (C.nreq << F.width_log) > FORK_NUMBERS) --F.width_log;
+  while (F.width_log > 0 && (C.nreq << F.width_log) > FORK_NUMBERS / (F.width_log > 3 ? 16 : 1)) --F.width_log;
   const int width = 1 << F.width_log, heads = C.layers * C.kv_heads;
   F.table_strips = (cache->table_len + width - 1) / width;
   F.head_strips = (heads + width - 1) / width;
