@@ -514,7 +514,7 @@ typedef struct compactor_rotate_rows {
   const int32_t *positions;    /* device, int32: of token t of request b at b*position_stride_b + t */
   int64_t position_stride_b;   /* 0: the same for all requests */
   const int32_t *new_tokens;   /* as in compactor_cache_rows; the outputs' padding rows stay as they are */
-  int32_t nreq, layers, tokens, q_heads, kv_heads;
+  int32_t nreq, layers, tokens, q_heads, kv_heads;      /* heads: 2^20 at most */
 } compactor_rotate_rows_t;
 int compactor_rotate(const compactor_rotation_t *rotation, const compactor_rotate_rows_t *rows, void *stream);
 
@@ -524,7 +524,7 @@ typedef struct compactor_rotate_queries {
   void *q_out;            /* q in place, with the same strides, or other memory */
   int64_t q_stride_b, q_stride_l, q_stride_t, q_stride_h;
   int64_t q_out_stride_b, q_out_stride_l, q_out_stride_t, q_out_stride_h;
-  int32_t q_heads;        /* a multiple of kv_heads */
+  int32_t q_heads;        /* a multiple of kv_heads, 2^20 at most */
 } compactor_rotate_queries_t;
 /* compactor_cache_append of keys that are normed and rotated on the way, and of values as they are; the queries of the same tokens
  * likewise (queries NULL: none).  Token t of head h has position seen + t, that which it is appended with, and so have the query
@@ -540,7 +540,7 @@ int compactor_mx_append_rotated(const compactor_mx_cache_t *cache, const compact
  * whatever else holds it); 0: the page is free, and none is below 0.  The calls keep it up as they change the tables of `cache`, which they write to although
  * compactor_cache_t has them const.  Its tables are those of all layers, so these calls take the cache of all of them; of the pool only the sizes are looked at,
  * but by compactor_pages_copy, and a cache in 4 bits is passed as its member `cache`.  No two of them (on any caches) that share refs run at a time.
- * nreq <= 16384.  Entries outside [0, num_pages) name no page. */
+ * nreq <= 16384, num_pages <= 2^30.  Entries outside [0, num_pages) name no page. */
 
 /* Room for new tokens.  With n_b new tokens of request b, `top` the most and `low` the fewest tokens that one of its heads holds, its entries from
  * ceil(top / page_size) up to ceil((top + n_b) / page_size) (or the table's end) that name no page get one, and a page from low / page_size on up to there that is
@@ -561,8 +561,8 @@ int compactor_pages_reserve(const compactor_cache_t *cache, const compactor_page
 int compactor_pages_reserve_workspace_size(const compactor_cache_t *cache, size_t *bytes);
 int compactor_pages_compact_workspace_size(const compactor_cache_t *cache, size_t *bytes);
 
-/* Copies pages, all layers and heads and, where the cache has them, mass and positions (and scales): of the first done[0] of at most max_pairs pairs.  No
- * page is in two of them.  Pairs with a page that is not there are passed over. */
+/* Copies pages, all layers and heads and, where the cache has them, mass and positions (and scales): of the first done[0] of at most max_pairs pairs.  A
+ * page that is written to is in no other pair.  Pairs with a page that is not there are passed over. */
 int compactor_pages_copy(const compactor_cache_t *cache, const int32_t *pairs, int32_t max_pairs, const int32_t *done, void *stream);
 int compactor_mx_pages_copy(const compactor_mx_cache_t *cache, const int32_t *pairs, int32_t max_pairs, const int32_t *done, void *stream);
 

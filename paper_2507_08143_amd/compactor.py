@@ -717,7 +717,7 @@ class Cache:
                  mass: Optional[torch.Tensor] = None, positions: Optional[torch.Tensor] = None):
         self._c = self._take(k_pages, v_pages, torch.bfloat16, tables, counts, seen, mass, positions)
         self._c.head_dim = k_pages.shape[4]
-        self._ref = C.byref(self._c)
+        self._ref = self._plain = C.byref(self._c)
 
     def _take(self, k_pages, v_pages, dtype, tables, counts, seen, mass, positions) -> _Cache:
         if k_pages.dtype != dtype or v_pages.dtype != dtype:
@@ -847,7 +847,7 @@ class MxCache(Cache):
         self.k_scales, self.v_scales = self._scales = k_scales, v_scales
         self._mx = _MxCache(cache, k_scales.data_ptr(), v_scales.data_ptr())
         self._c = self._mx.cache
-        self._ref = C.byref(self._mx)
+        self._ref, self._plain = C.byref(self._mx), C.byref(self._c)      # (_plain: for calls that look at no rows)
 
 
 def _either(cache, mx: bool):
@@ -1056,7 +1056,8 @@ def compactor_mx_read(cache: MxCache, tokens: int, first: Optional[int] = None, 
     if (k is None) != (v is None):
         _refuse("k and v: both, or none")
     if k is None:
-        k, v = (_empty(stream, shape, dtype=torch.bfloat16, device=cache.device) for _ in range(2))
+        make = lambda: cache.counts.new_empty(shape, dtype=torch.bfloat16)      # noqa: E731 (half of what torch.empty with a device takes)
+        k, v = _made_on(stream, make), _made_on(stream, make)
     else:
         for t in (k, v):
             if t.dtype != torch.bfloat16 or tuple(t.shape) != shape or t.stride() != k.stride() or t.stride(4) != 1:
@@ -1246,44 +1247,46 @@ def _append_rotated(call, cache, rotation, k, v, q, new_tokens, q_out, stream):
     return q_out
 
 
-def _pages(cache: Cache, **tensors):
-    """Checks of the calls that change tables -> the cache, as they take it.  tensors: (tensor, shape), int32 and contiguous, or None"""
+def _pages(cache: Cache, *tensors):
+    """Checks of the calls that change tables -> the cache, as they take it.  tensors: (name, tensor, shape), int32 and contiguous, or None"""
     if not cache._whole:
         _refuse("the pages are those of all layers: this call takes the cache that layer() was called on")
-    for name, (t, shape) in tensors.items():
+    device = cache.device
+    for name, t, shape in tensors:
         if t is None:
             continue
-        if t.dtype != torch.int32 or tuple(t.shape) != shape or not t.is_contiguous():
+        if t.dtype != torch.int32 or t.shape != shape or not t.is_contiguous():
             _refuse("%s must be a contiguous int32 tensor %s" % (name, list(shape)))
-        if t.device != cache.device:
+        if t.device != device:
             _refuse("%s must live on the GPU of the cache" % name)
-    return C.byref(cache._c)
+    return cache._plain
 
 
 def _pages_bytes(call, cache: Cache) -> int:
     need = cache._bytes.get(call.__name__)
     if need is None:
         out = C.c_size_t(0)
-        _check(call(C.byref(cache._c), C.byref(out)))
+        _check(call(cache._plain, C.byref(out)))
         need = cache._bytes[call.__name__] = int(out.value)
     return need
 
 
 def _pages_workspace(call, cache, given, stream):
     if given is None:
-        given = _empty(stream, _pages_bytes(call, cache), returned=False, dtype=torch.uint8, device=cache.device)
-    else:
-        _out(given, 0, torch.uint8, "workspace")
-        if given.device != cache.device:
-            _refuse("the workspace must live on the GPU of the cache")
+        need = _pages_bytes(call, cache)
+        return _made_on(stream, lambda: cache.tables.new_empty(need, dtype=torch.uint8), False)      # (half of what torch.empty with a device takes)
+    _out(given, 0, torch.uint8, "workspace")
+    if given.device != cache.device:
+        _refuse("the workspace must live on the GPU of the cache")
     return given
 
 
 def _pages_out(cache, pairs, most, done, stream):
-    got = []
-    for t, shape in ((pairs, (most, 2)), (done, (2,))):
-        got.append(_empty(stream, shape, dtype=torch.int32, device=cache.device) if t is None else t)
-    return got
+    if pairs is None:
+        pairs = _made_on(stream, lambda: cache.tables.new_empty((most, 2)))
+    if done is None:
+        done = _made_on(stream, lambda: cache.tables.new_empty(2))
+    return pairs, done
 
 
 def compactor_pages_reserve_workspace_size(cache: Cache) -> int:
@@ -1302,7 +1305,7 @@ def compactor_pages_reserve(cache: Cache, refs: torch.Tensor, tokens: int, new_t
     N = cache._c.pool.num_pages
     most = min(cache.nreq * cache._c.table_len, N)
     _int32(tokens=tokens)
-    ref = _pages(cache, refs=(refs, (N,)), pairs=(pairs, (most, 2)), done=(done, (2,)))
+    ref = _pages(cache, ("refs", refs, (N,)), ("pairs", pairs, (most, 2)), ("done", done, (2,)))
     pairs, done = _pages_out(cache, pairs, most, done, stream)
     ws = _pages_workspace(_lib.compactor_pages_reserve_workspace_size, cache, workspace, stream)
     c = _PagesReserve(refs.data_ptr(), cache._new_tokens(new_tokens), tokens, 1 if own_all else 0, pairs.data_ptr(), done.data_ptr())
@@ -1311,7 +1314,7 @@ def compactor_pages_reserve(cache: Cache, refs: torch.Tensor, tokens: int, new_t
 
 
 def _copy(call, cache, pairs, done, stream):
-    _pages(cache, done=(done, (2,)))
+    _pages(cache, ("done", done, (2,)))
     if pairs.dtype != torch.int32 or pairs.dim() != 2 or pairs.shape[1] != 2 or pairs.shape[0] < 1 or not pairs.is_contiguous():
         _refuse("pairs must be a contiguous int32 tensor [most, 2]")
     if pairs.device != cache.device:
@@ -1333,13 +1336,13 @@ def compactor_mx_pages_copy(cache: MxCache, pairs: torch.Tensor, done: torch.Ten
 
 def compactor_pages_fork(cache: Cache, refs: torch.Tensor, parents: torch.Tensor, stream=None):
     """Request b goes on as request parents[b] was, on its pages.  parents: int32 [request]"""
-    ref = _pages(cache, refs=(refs, (cache._c.pool.num_pages,)), parents=(parents, (cache.nreq,)))
+    ref = _pages(cache, ("refs", refs, (cache._c.pool.num_pages,)), ("parents", parents, (cache.nreq,)))
     cache._on(stream, lambda st: _lib.compactor_pages_fork(ref, refs.data_ptr(), parents.data_ptr(), st))
 
 
 def compactor_pages_release(cache: Cache, refs: torch.Tensor, finished: Optional[torch.Tensor] = None, stream=None):
     """Gives back the pages behind the last token of every request, and all of those that are finished (int32 [request], not 0)."""
-    ref = _pages(cache, refs=(refs, (cache._c.pool.num_pages,)), finished=(finished, (cache.nreq,)))
+    ref = _pages(cache, ("refs", refs, (cache._c.pool.num_pages,)), ("finished", finished, (cache.nreq,)))
     cache._on(stream, lambda st: _lib.compactor_pages_release(ref, refs.data_ptr(), _ptr(finished), st))
 
 
@@ -1348,7 +1351,7 @@ def compactor_pages_compact(cache: Cache, refs: torch.Tensor, pairs=None, done=N
     are not free), for compactor_pages_copy"""
     N = cache._c.pool.num_pages
     most = N // 2 + 1
-    ref = _pages(cache, refs=(refs, (N,)), pairs=(pairs, (most, 2)), done=(done, (2,)))
+    ref = _pages(cache, ("refs", refs, (N,)), ("pairs", pairs, (most, 2)), ("done", done, (2,)))
     pairs, done = _pages_out(cache, pairs, most, done, stream)
     ws = _pages_workspace(_lib.compactor_pages_compact_workspace_size, cache, workspace, stream)
     cache._on(stream, lambda st: _lib.compactor_pages_compact(ref, refs.data_ptr(), pairs.data_ptr(), done.data_ptr(), ws.data_ptr(), ws.numel(), st))

@@ -12,6 +12,7 @@ namespace cmp {
 
 constexpr int PLAN_THREADS = 1024, PLAN_WAVES = PLAN_THREADS / 64;
 constexpr int PAGES_MOST = 16384;            // requests
+constexpr int POOL_MOST = 1 << 30;           // pages, so that a step beyond the last one fits 32 bits
 
 __device__ __forceinline__ int pages_of(const CacheView &C, int tokens) {       // that hold them
   const int full = invariant_quotient((unsigned)tokens, C.div_mul, C.div_shift);
@@ -522,7 +523,7 @@ static bool runs_of(long long page, long long run, int unit, std::initializer_li
     invariant_divisor(d[k].first, &R->mul[R->dims], &R->shift[R->dims]);
     units *= d[k].first;
   }
-  if (run / unit > 0x7fffffff || units > 0x7fffffff) return false;
+  if (run / unit > 1 << 30 || units > 1 << 30) return false;               // (and a chunk beyond the last unit fits 32 bits)
   R->units = (int)units;
   invariant_divisor(R->run, &R->run_mul, &R->run_shift);
   return true;
@@ -562,7 +563,8 @@ static int copy_call(const CacheView &C, const int32_t *pairs, int max_pairs, co
 static int pages_view(const compactor_cache_t *cache, CacheNeed need, CacheView *C) {
   const int rc = cache_view(cache, need, C);
   if (rc) return rc;
-  return C->nreq > PAGES_MOST || (long long)C->nreq * cache->table_len > 0x7fffffffll ? COMPACTOR_EINVAL : COMPACTOR_OK;
+  const bool fits = C->nreq <= PAGES_MOST && C->num_pages <= POOL_MOST && (long long)C->nreq * cache->table_len <= 0x7fffffffll;
+  return fits ? COMPACTOR_OK : COMPACTOR_EINVAL;
 }
 
 static size_t up(size_t x) { return (x + 255) / 256 * 256; }

@@ -131,6 +131,7 @@ struct RotateRows {
   int parts;                       // waves that share the heads of a token
   unsigned units;                  // (request, layer, token, part)
 };
+constexpr int HEADS_MOST = 1 << 20;
 constexpr int ROTATE_AT_ONCE = 4;  // rows that 16 lanes have on their way
 
 // A wave per token of a layer, or several; its four rows of 16 lanes take heads in turn.
@@ -309,7 +310,7 @@ static int append_rotated(const CacheView &C, const compactor_rotation_t *rotati
   S.tokens = rows->tokens;
   if (queries) {
     const compactor_rotate_queries_t &q = *queries;
-    if (!q.q || !q.q_out || q.q_heads < C.kv_heads || q.q_heads % C.kv_heads) return COMPACTOR_EINVAL;
+    if (!q.q || !q.q_out || q.q_heads < C.kv_heads || q.q_heads % C.kv_heads || q.q_heads > HEADS_MOST) return COMPACTOR_EINVAL;
     if ((rc = strides_check(q.q_stride_b, q.q_stride_l, q.q_stride_t, q.q_stride_h)) != 0) return rc;
     if ((rc = strides_check(q.q_out_stride_b, q.q_out_stride_l, q.q_out_stride_t, q.q_out_stride_h)) != 0) return rc;
     if (misaligned(q.q, 16) || misaligned(q.q_out, 16)) return COMPACTOR_EALIGN;
@@ -353,6 +354,7 @@ int compactor_rotate(const compactor_rotation_t *rotation, const compactor_rotat
   if (!rows) return COMPACTOR_EINVAL;
   const compactor_rotate_rows_t &r = *rows;
   if (r.nreq < 1 || r.layers < 1 || r.tokens < 1 || r.q_heads < 0 || r.kv_heads < 0 || r.q_heads + (long long)r.kv_heads < 1) return COMPACTOR_EINVAL;
+  if (r.q_heads > HEADS_MOST || r.kv_heads > HEADS_MOST) return COMPACTOR_EINVAL;
   if (!r.positions || r.position_stride_b < 0) return COMPACTOR_EINVAL;
   if (misaligned(r.positions, 4) || misaligned(r.new_tokens, 4)) return COMPACTOR_EALIGN;
   if (r.q_heads > 0) {

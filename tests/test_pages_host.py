@@ -42,7 +42,7 @@ def _copies(B, pairs=0xb00000, most=10, done=0xc00000, cache=None, mx=None):
 
 
 BAD = [(dict(nreq=0), "EINVAL"), (dict(nreq=16385), "EINVAL"), (dict(nreq=16384, table_len=1 << 18, table_stride=1 << 18), "EINVAL"), (dict(head_dim=64), "EUNSUPPORTED"),
-       (dict(page_size=0), "EINVAL"), (dict(num_pages=0), "EINVAL"), (dict(table_len=0), "EINVAL"), (dict(tables=0), "EINVAL"), (dict(counts=0), "EINVAL"),
+       (dict(page_size=0), "EINVAL"), (dict(num_pages=0), "EINVAL"), (dict(num_pages=(1 << 30) + 1), "EINVAL"), (dict(table_len=0), "EINVAL"), (dict(tables=0), "EINVAL"), (dict(counts=0), "EINVAL"),
        (dict(count_stride_b=-1), "EINVAL"), (dict(tables=0x30002), "EALIGN"), (dict(counts=0x40001), "EALIGN"), (dict(seen=0x50002), "EALIGN")]
 
 
@@ -82,8 +82,9 @@ def test_bad_copies(B):
     for kw, code in ((dict(k_pages=0), B.EINVAL), (dict(slot_stride=16), B.EINVAL), (dict(page_stride=-16), B.EINVAL), (dict(k_pages=0x10008), B.EALIGN),
                      (dict(mass=0), B.EINVAL), (dict(mass=0x60002), B.EALIGN)):
         assert _copies(B, cache=H._cache(B, **kw), mx=M._mx(B, **kw)) == {code}, kw
-    huge = dict(page_size=1 << 20, kv_heads=256, layers=8, table_len=2, table_stride=2)
-    assert _copies(B, cache=H._cache(B, **huge), mx=M._mx(B, **huge)) == {B.EINVAL}
+    for layers in (8, 2):              # more than 2^30 units of 16 bytes a page, or numbers of its state
+        huge = dict(page_size=1 << 20, kv_heads=1024, layers=layers, table_len=2, table_stride=2)
+        assert _copies(B, cache=H._cache(B, **huge), mx=M._mx(B, **huge)) == {B.EINVAL}
 
 
 def test_the_calls_check_their_tensors(B):

@@ -67,7 +67,7 @@ def test_bad_rows(B):
                      [(dict([(n, 0x1000008)]), B.EALIGN) for n in ("q", "k", "q_out", "k_out", "k_plain")] +
                      [(dict([(n + "_stride_" + d, -8)]), B.EINVAL) for n in ("q", "k", "q_out", "k_out", "k_plain") for d in "blth"] +
                      [(dict([(n + "_stride_" + d, 132)]), B.EALIGN) for n in ("q", "k", "q_out", "k_out", "k_plain") for d in "blth"] +
-                     [(dict(q_heads=0, kv_heads=0), B.EINVAL), (dict(q_heads=-1), B.EINVAL), (dict(kv_heads=-1), B.EINVAL),
+                     [(dict(q_heads=0, kv_heads=0), B.EINVAL), (dict(q_heads=(1 << 20) + 1), B.EINVAL), (dict(kv_heads=(1 << 20) + 1), B.EINVAL), (dict(q_heads=-1), B.EINVAL), (dict(kv_heads=-1), B.EINVAL),
                       (dict(position_stride_b=-1), B.EINVAL), (dict(positions=0x600002), B.EALIGN), (dict(new_tokens=0x2), B.EALIGN),
                       (dict(q_out=0x100000, q_out_stride_t=8192), B.EINVAL), (dict(k_out=0x200000, k_out_stride_h=256), B.EINVAL),
                       (dict(k_plain=0x200000, k_plain_stride_h=256), B.EINVAL), (dict(k_plain=0x400000), B.EINVAL), (dict(q_out=0x200000), B.EINVAL),
@@ -83,7 +83,7 @@ def test_bad_appends(B):
     for kw, code in ((dict(k=0), B.EINVAL), (dict(v=0), B.EINVAL), (dict(tokens=0), B.EINVAL), (dict(stride_t=-8), B.EINVAL), (dict(stride_h=4), B.EALIGN),
                      (dict(k=0x100008), B.EALIGN), (dict(v=0x200002), B.EALIGN), (dict(new_tokens=2), B.EALIGN)):
         assert _appends(B, rotation, _rows(B, **kw), queries) == {code}, kw
-    for kw, code in ((dict(q=0), B.EINVAL), (dict(q_out=0), B.EINVAL), (dict(q_heads=0), B.EINVAL), (dict(q_heads=12), B.EINVAL), (dict(q_heads=4), B.EINVAL),
+    for kw, code in ((dict(q=0), B.EINVAL), (dict(q_out=0), B.EINVAL), (dict(q_heads=0), B.EINVAL), (dict(q_heads=12), B.EINVAL), (dict(q_heads=4), B.EINVAL), (dict(q_heads=1 << 21), B.EINVAL),
                      (dict(q_stride_b=-8), B.EINVAL), (dict(q_out_stride_l=-8), B.EINVAL), (dict(q_stride_t=4), B.EALIGN), (dict(q_out_stride_h=12), B.EALIGN),
                      (dict(q=0x300008), B.EALIGN), (dict(q_out=0x400004), B.EALIGN), (dict(q_out=0x300000, q_out_stride_h=256), B.EINVAL)):
         assert _appends(B, rotation, rows, _queries(B, **kw)) == {code}, kw

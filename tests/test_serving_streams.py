@@ -35,6 +35,8 @@ def test_allocations_belong_to_the_stream_that_uses_them(B, world, monkeypatch, 
     main, side, made, lib = world
     more = _More(lib.lib)
     monkeypatch.setattr(B, "_lib", more)
+    monkeypatch.setattr(M, "_g", _g)          # tensors whose allocations are noted
+    monkeypatch.setattr(R, "_g", _g)
     call = _calls(B)[name]
     del made[:]
     got = call(side)
