@@ -188,9 +188,9 @@ __device__ __forceinline__ HeadSize head_size(const CacheView &C, const Queries 
 // heads on each is cut into the same few parts (split_part): 1024 heads of 4000, us with a scan / a plan / parts 407 / 384 / 360, of 250 to 8000
 // 249 / 237 / 232, 4096 of 2000 1045 / 786 / 692.  -> false: there is no such fragment.
 constexpr int SCAN_GROUP = 4;                // of 64 heads whose sizes are fetched together; the first stays
-// PAIRS: rows of two heads share the lines of memory; the parts of both with the same slots go to one XCD, which reads a line once (workgroups go round the
-// eight).
-template <bool PAIRS = false>
+// BITS4: of rows of 4 bits.  Where heads lie side by side two of their rows share a line of memory: the parts of both with the same slots go to one XCD,
+// whose cache it then comes into once (workgroups go round the eight).
+template <bool BITS4 = false>
 __device__ __forceinline__ bool scan_part(const CacheView &C, const Queries &Q, int fragment, Fragment &F) {
   const int heads = C.nreq * C.layers * C.kv_heads, lane = threadIdx.x & 63;
   HeadSize size[SCAN_GROUP];
@@ -213,7 +213,7 @@ __device__ __forceinline__ bool scan_part(const CacheView &C, const Queries &Q, 
   }
   const int total = __builtin_amdgcn_readlane(wave_scan(mine), 63);          // the host has seen to it that this fits
   longest = (int)__builtin_amdgcn_readlane(wave_max_up((unsigned)longest), 63);
-  const FragmentRule rule = fragment_rule(total, longest, heads, Q.tokens * Q.group, Q.target);
+  const FragmentRule rule = fragment_rule(total, longest, heads, Q.tokens * Q.group, Q.target, BITS4);
   int before = 0;
   for (int h0 = 0; h0 < heads; h0 += 64 * SCAN_GROUP) {
     if (h0 > 0) fetch(h0);
@@ -232,7 +232,7 @@ __device__ __forceinline__ bool scan_part(const CacheView &C, const Queries &Q, 
         F.parts = __builtin_amdgcn_readlane(parts, at);
         F.first = __builtin_amdgcn_readlane(upto, at) - F.parts;
         int k = fragment - F.first;
-        if (PAIRS && (at & 1)) {             // the parts of the head before take as many workgroups more or less than whole rounds of the XCDs
+        if (BITS4 && (at & 1)) {             // the workgroups of the head before are so many more than whole rounds of the XCDs
           const int turn = __builtin_amdgcn_readlane(parts, at - 1) & 7;
           k += turn < F.parts ? turn : 0;
           k -= k >= F.parts ? F.parts : 0;
@@ -249,11 +249,11 @@ __device__ __forceinline__ bool scan_part(const CacheView &C, const Queries &Q, 
 
 // Part blockIdx.x / heads of a head.  Workgroups go round the eight XCDs, and heads often come in eights: neighbours in a group of eight
 // change places from group to group, or an XCD would have the same kv head of every request, long or short.
-template <bool PAIRS = false>
+template <bool BITS4 = false>
 __device__ __forceinline__ bool split_part(const CacheView &C, const Queries &Q, Fragment &F, int &fragment) {
   const unsigned heads = (unsigned)C.nreq * (unsigned)C.layers * (unsigned)C.kv_heads;
   const unsigned part = Q.split == 1 ? 0u : blockIdx.x / heads, i = blockIdx.x - part * heads;
-  if (PAIRS)
+  if (BITS4)
     F.head = (int)((i | 15u) < heads ? (i & ~15u) | (((i + (i >> 4) + part) & 7u) << 1) | (i >> 3 & 1u) : i);
   else
     F.head = (int)((i | 7u) < heads ? (i & ~7u) | ((i + (i >> 3) + part) & 7u) : i);

@@ -15,17 +15,21 @@ constexpr int ATT_EVEN = 256, EVEN_PARTS = 4;          // units that have equal 
 
 // Steps of a fragment: 1 << log, or `per` where that is not 0.
 struct FragmentRule { int log, per; };
-// total: steps of all heads; rows: query rows of a head; target: fragments that there are to be, beside the last of each head
-__host__ __device__ __forceinline__ FragmentRule fragment_rule(int total, int longest, int heads, int rows, int target) {
+// total: steps of all heads; rows: query rows of a head; target: fragments that there are to be, beside the last of each head; bits4: of rows of 4 bits
+__host__ __device__ __forceinline__ FragmentRule fragment_rule(int total, int longest, int heads, int rows, int target, bool bits4 = false) {
   // More than 16 query rows make a step dearer and a start too, and more than 32 leave room for one workgroup a unit: fewer steps where all
   // find room at once (16 heads of 500 to 1411, 40 rows: 24 us with 4 steps, 19 with 1; one of 20000, 64 rows, 30 and 28; up to 16 rows
   // the join costs as much), and twice as many where there is enough for all (24 heads of 18000, 40 rows: 80 us with 4 steps, 62 with 8,
   // with weights 100 and 87; 96 heads of 18000 or of 900 to 9800: the same within 1 %).
+  // Rows of 4 bits are so little to read that for 16 query rows too a step waits for itself, not for memory (4 heads of 2000 to 4000, 7 rows: 14.0 us with 4 steps, 11.8
+  // with 1 and 2), and starts are dearer beside it: twice as many where four would not all run at once (96 heads of 8000, 4 rows: 31 and 28; of 16000
+  // 53 and 48; of 4000, 768 workgroups with 4 steps, 20 and 22).
   const bool many_rows = rows > 16;
-  FragmentRule r{many_rows ? 0 : ATT_LEAST_LOG, 0};
+  FragmentRule r{many_rows || bits4 ? 0 : ATT_LEAST_LOG, 0};
   while (r.log < ATT_LEAST_LOG && total >> r.log > ATT_EVEN) ++r.log;
   while ((total - 1) >> r.log >= target) ++r.log;
   if (many_rows && r.log == ATT_LEAST_LOG && total >> (r.log + 1) >= ATT_EVEN) ++r.log;
+  if (bits4 && !many_rows && r.log == ATT_LEAST_LOG && total >> r.log > 3 * ATT_EVEN) ++r.log;
   if (10ll * total >= 9ll * longest * heads)
     for (int parts = 1; parts <= EVEN_PARTS && r.per == 0; ++parts) {
       const int wgs = heads * parts, over = wgs % ATT_EVEN;

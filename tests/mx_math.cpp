@@ -1,0 +1,19 @@
+// The rule that cuts heads of rows of 4 bits into fragments, for test_mx_math.py.
+#include "common.h"
+#include "fragments.h"
+
+extern "C" {
+int fragments_launched(int heads, int steps, int rows, int units) {
+  return cmp::fragments_most(heads, cmp::fragment_target(heads, steps, rows, units));
+}
+int fragments_made(const int *steps, int heads, int promised, int rows, int units) {
+  int total = 0, longest = 0, made = 0;
+  for (int h = 0; h < heads; ++h) {
+    total += steps[h];
+    longest = steps[h] > longest ? steps[h] : longest;
+  }
+  const cmp::FragmentRule r = cmp::fragment_rule(total, longest, heads, rows, cmp::fragment_target(heads, promised, rows, units), true);
+  for (int h = 0; h < heads; ++h) made += cmp::fragments_of(steps[h], r);
+  return made;
+}
+}
