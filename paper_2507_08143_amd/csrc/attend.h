@@ -188,10 +188,12 @@ __device__ __forceinline__ HeadSize head_size(const CacheView &C, const Queries 
 // heads on each is cut into the same few parts (split_part): 1024 heads of 4000, us with a scan / a plan / parts 407 / 384 / 360, of 250 to 8000
 // 249 / 237 / 232, 4096 of 2000 1045 / 786 / 692.  -> false: there is no such fragment.
 constexpr int SCAN_GROUP = 4;                // of 64 heads whose sizes are fetched together; the first stays
-// BITS4: of rows of 4 bits.  Where heads lie side by side two of their rows share a line of memory: the parts of both with the same slots go to one XCD,
-// whose cache it then comes into once (workgroups go round the eight).
+// BITS4: of rows of 4 bits.  Where heads lie side by side two of their rows share a line of memory, so the parts of both with the same slots go to one XCD, whose
+// cache it then comes into once: workgroups go round the eight XCDs, those with the same place among eight of two times eight take two parts in turn, and
+// of two neighbours' parts the same of both come one behind the other.  `fragment` becomes the number under which its results are kept.
 template <bool BITS4 = false>
-__device__ __forceinline__ bool scan_part(const CacheView &C, const Queries &Q, int fragment, Fragment &F) {
+__device__ __forceinline__ bool scan_part(const CacheView &C, const Queries &Q, int &fragment, Fragment &F) {
+  if (BITS4 && (blockIdx.x | 15u) < gridDim.x) fragment = (fragment & ~15) | (fragment & 7) << 1 | (fragment >> 3 & 1);
   const int heads = C.nreq * C.layers * C.kv_heads, lane = threadIdx.x & 63;
   HeadSize size[SCAN_GROUP];
   auto fetch = [&](int h0) {
@@ -225,18 +227,24 @@ __device__ __forceinline__ bool scan_part(const CacheView &C, const Queries &Q, 
       const int upto = before + wave_scan(parts);
       const unsigned long long beyond = __ballot(upto > fragment);
       if (beyond != 0) {
-        const int at = __builtin_ctzll(beyond), each = rule.per > 0 ? rule.per : 1 << rule.log;
+        int at = __builtin_ctzll(beyond);
+        const int each = rule.per > 0 ? rule.per : 1 << rule.log;
+        int k = -1;                                  // the part, where it is not the fragment's place
+        if (BITS4) {
+          const int two = at & ~1, p0 = __builtin_amdgcn_readlane(parts, two), p1 = __builtin_amdgcn_readlane(parts, two | 1);
+          const int start = __builtin_amdgcn_readlane(upto, two) - p0, q = fragment - start, both = 2 * min(p0, p1);
+          at = two | (q < both ? q & 1 : p1 > p0 ? 1 : 0);
+          k = q < both ? q >> 1 : q - (both >> 1);
+        }
         F.head = h0 + 64 * i + at;
         F.count = __builtin_amdgcn_readlane(size[i].count, at);
         F.n = __builtin_amdgcn_readlane(size[i].n, at);
         F.parts = __builtin_amdgcn_readlane(parts, at);
         F.first = __builtin_amdgcn_readlane(upto, at) - F.parts;
-        int k = fragment - F.first;
-        if (BITS4 && (at & 1)) {             // the workgroups of the head before are so many more than whole rounds of the XCDs
-          const int turn = __builtin_amdgcn_readlane(parts, at - 1) & 7;
-          k += turn < F.parts ? turn : 0;
-          k -= k >= F.parts ? F.parts : 0;
-        }
+        if (BITS4)
+          fragment = F.first + k;
+        else
+          k = fragment - F.first;
         F.step0 = k * each;
         F.step1 = min(F.step0 + each, __builtin_amdgcn_readlane(steps, at));
         return true;

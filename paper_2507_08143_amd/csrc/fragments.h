@@ -21,15 +21,19 @@ __host__ __device__ __forceinline__ FragmentRule fragment_rule(int total, int lo
   // find room at once (16 heads of 500 to 1411, 40 rows: 24 us with 4 steps, 19 with 1; one of 20000, 64 rows, 30 and 28; up to 16 rows
   // the join costs as much), and twice as many where there is enough for all (24 heads of 18000, 40 rows: 80 us with 4 steps, 62 with 8,
   // with weights 100 and 87; 96 heads of 18000 or of 900 to 9800: the same within 1 %).
-  // Rows of 4 bits are so little to read that for 16 query rows too a step waits for itself, not for memory (4 heads of 2000 to 4000, 7 rows: 14.0 us with 4 steps, 11.8
-  // with 1 and 2), and starts are dearer beside it: twice as many where four would not all run at once (96 heads of 8000, 4 rows: 31 and 28; of 16000
-  // 53 and 48; of 4000, 768 workgroups with 4 steps, 20 and 22).
   const bool many_rows = rows > 16;
   FragmentRule r{many_rows || bits4 ? 0 : ATT_LEAST_LOG, 0};
   while (r.log < ATT_LEAST_LOG && total >> r.log > ATT_EVEN) ++r.log;
   while ((total - 1) >> r.log >= target) ++r.log;
   if (many_rows && r.log == ATT_LEAST_LOG && total >> (r.log + 1) >= ATT_EVEN) ++r.log;
-  if (bits4 && !many_rows && r.log == ATT_LEAST_LOG && total >> r.log > 3 * ATT_EVEN) ++r.log;
+  // Rows of 4 bits are so little to read that for 16 query rows too a step waits for itself, not for memory (4 heads of 2000 to 4000, 7 rows: 14.0 us with 4 steps, 11.8
+  // with 1 and 2), and starts and joins are dearer beside it: no more fragments than run at once, as long as that leaves short ones, or heads are
+  // of (nearly) one length (96 heads of 16000, 4 rows: 52 us with 4 steps, 48 with 8, 43 with 16; of 32000 101, 95 and 92 with 8, 16 and 32, 20 rows 146 and
+  // 125 with 8 and 32; 384 of 4000, 4 rows, 60, 52 and 47 with 4, 8 and 16; but 384 of 8192 to 32000 210 and 240 with 32 and 64).
+  if (bits4 && rows <= 48) {
+    const int most = 10ll * total >= 9ll * longest * heads ? 6 : 4;
+    while (r.log >= ATT_LEAST_LOG && r.log < most && total >> r.log > 3 * ATT_EVEN) ++r.log;
+  }
   if (10ll * total >= 9ll * longest * heads)
     for (int parts = 1; parts <= EVEN_PARTS && r.per == 0; ++parts) {
       const int wgs = heads * parts, over = wgs % ATT_EVEN;

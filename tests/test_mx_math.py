@@ -33,21 +33,36 @@ def test_every_fragment_has_a_workgroup(M, units, rows):
                 assert heads <= made <= launched, (heads, promised, steps)
 
 
-def test_the_parts_of_a_second_head_are_a_turn_of_its_own():
-    """Part k of an odd head of P parts, behind one of Q: (k + Q % 8) % P where Q % 8 < P, else k.  Every part once, and at the XCD of the same part of the
-    head before but for the Q % 8 that come round."""
-    for P in range(1, 70):
-        for Q in range(1, 70):
-            turn = Q & 7
-            parts = []
-            for k in range(P):
-                at = k + (turn if turn < P else 0)
-                at -= P if at >= P else 0
-                parts.append(at)
-            assert sorted(parts) == list(range(P))
-            if turn < P:
-                apart = sum((Q + k) % 8 != p % 8 for k, p in enumerate(parts))
-                assert apart <= turn
+def test_the_parts_of_two_heads_go_to_one_xcd():
+    """Workgroup i takes part e(i) of the heads' parts, those of two neighbours in turn: every part of every head once, and the same parts of both at one XCD
+    wherever the pairs before have an even number of parts."""
+    rng = np.random.default_rng(0)
+    for heads in (1, 2, 5, 8, 31, 64):
+        for same in (True, False):
+            for room in (0, 3, 40):
+                parts = np.repeat(rng.integers(1, 12, (heads + 1) // 2), 2)[:heads] if same else rng.integers(1, 12, heads)
+                total, first = int(parts.sum()), np.concatenate(([0], np.cumsum(parts)))
+                grid = total + room
+                seen, at = {}, {}
+                for i in range(grid):
+                    f = (i & ~15) | (i & 7) << 1 | (i >> 3 & 1) if (i | 15) < grid else i
+                    assert 0 <= f < grid and f not in seen
+                    seen[f] = None
+                    if f >= total:
+                        continue
+                    h = int(np.searchsorted(first, f, side="right")) - 1
+                    two = h & ~1
+                    p0, p1 = int(parts[two]), int(parts[two + 1]) if two + 1 < heads else 0
+                    q, both = f - int(first[two]), 2 * min(p0, p1)
+                    head = two | (q & 1 if q < both else 1 if p1 > p0 else 0)
+                    k = q >> 1 if q < both else q - both // 2
+                    assert k < parts[head] and (head, k) not in at
+                    at[head, k] = i % 8 if (i | 15) < grid else None
+                assert len(at) == total
+                if same:
+                    for h in range(0, heads - 1, 2):
+                        for k in range(int(parts[h])):
+                            assert at[h, k] == at[h + 1, k]
 
 
 def test_pairs_of_heads_among_sixteen():
