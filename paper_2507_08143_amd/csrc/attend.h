@@ -215,7 +215,8 @@ __device__ __forceinline__ bool scan_part(const CacheView &C, const Queries &Q, 
   }
   const int total = __builtin_amdgcn_readlane(wave_scan(mine), 63);          // the host has seen to it that this fits
   longest = (int)__builtin_amdgcn_readlane(wave_max_up((unsigned)longest), 63);
-  const FragmentRule rule = fragment_rule(total, longest, heads, Q.tokens * Q.group, Q.target, BITS4);
+  const FragmentRule rule = BITS4 ? bits4_fragment_rule(total, longest, heads, Q.tokens * Q.group, Q.target)
+                                  : fragment_rule(total, longest, heads, Q.tokens * Q.group, Q.target);
   int before = 0;
   for (int h0 = 0; h0 < heads; h0 += 64 * SCAN_GROUP) {
     if (h0 > 0) fetch(h0);
@@ -485,6 +486,7 @@ __device__ __forceinline__ void weights_to_mass(const CacheView &C, const Querie
 struct AttendKernels {
   void (*attend)(const CacheView &C, const Queries &Q, bool row16, unsigned blocks, hipStream_t st);
   void (*mass)(const CacheView &C, const Queries &Q, bool row16, unsigned blocks, hipStream_t st);
+  bool bits4;                  // fragments by bits4_fragment_rule
   int again_rows;              // weights of more rows, with logits of more bytes, are found from K
   size_t again_bytes;
 };

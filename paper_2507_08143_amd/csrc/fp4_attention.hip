@@ -646,7 +646,7 @@ static const AttendKernels &attend4_kernels() {
       [](const CacheView &C, const Queries &Q, bool row16, unsigned blocks, hipStream_t st) {
         row16 ? launch_mass4<true>(C, Q, blocks, st) : launch_mass4<false>(C, Q, blocks, st);
       },
-      AGAIN4_ROWS, AGAIN4_BYTES};
+      true, AGAIN4_ROWS, AGAIN4_BYTES};
   return kernels;
 }
 

@@ -3,6 +3,7 @@
 #pragma once
 
 #include <algorithm>
+#include <cmath>
 
 #include "common.h"
 
@@ -13,27 +14,19 @@ constexpr int SCAN_HEADS = 512, SCAN_ROUNDS = 6;        // heads that a wave loo
                                              // there is room for on the chip
 constexpr int ATT_EVEN = 256, EVEN_PARTS = 4;          // units that have equal parts of heads of one length, and most parts of a head then
 
-// Steps of a fragment: 1 << log, or `per` where that is not 0.
-struct FragmentRule { int log, per; };
-// total: steps of all heads; rows: query rows of a head; target: fragments that there are to be, beside the last of each head; bits4: of rows of 4 bits
-__host__ __device__ __forceinline__ FragmentRule fragment_rule(int total, int longest, int heads, int rows, int target, bool bits4 = false) {
+// Steps of a fragment: 1 << log, or `per` where that is not 0.  inv: 1 / per, or 0 where heads have EVEN_PARTS at most.
+struct FragmentRule { int log, per; float inv; };
+// total: steps of all heads; rows: query rows of a head; target: fragments that there are to be, beside the last of each head
+__host__ __device__ __forceinline__ FragmentRule fragment_rule(int total, int longest, int heads, int rows, int target) {
   // More than 16 query rows make a step dearer and a start too, and more than 32 leave room for one workgroup a unit: fewer steps where all
   // find room at once (16 heads of 500 to 1411, 40 rows: 24 us with 4 steps, 19 with 1; one of 20000, 64 rows, 30 and 28; up to 16 rows
   // the join costs as much), and twice as many where there is enough for all (24 heads of 18000, 40 rows: 80 us with 4 steps, 62 with 8,
   // with weights 100 and 87; 96 heads of 18000 or of 900 to 9800: the same within 1 %).
   const bool many_rows = rows > 16;
-  FragmentRule r{many_rows || bits4 ? 0 : ATT_LEAST_LOG, 0};
+  FragmentRule r{many_rows ? 0 : ATT_LEAST_LOG, 0, 0.f};
   while (r.log < ATT_LEAST_LOG && total >> r.log > ATT_EVEN) ++r.log;
   while ((total - 1) >> r.log >= target) ++r.log;
   if (many_rows && r.log == ATT_LEAST_LOG && total >> (r.log + 1) >= ATT_EVEN) ++r.log;
-  // Rows of 4 bits are so little to read that for 16 query rows too a step waits for itself, not for memory (4 heads of 2000 to 4000, 7 rows: 14.0 us with 4 steps, 11.8
-  // with 1 and 2), and starts and joins are dearer beside it: no more fragments than run at once, as long as that leaves short ones, or heads are
-  // of (nearly) one length (96 heads of 16000, 4 rows: 52 us with 4 steps, 48 with 8, 43 with 16; of 32000 101, 95 and 92 with 8, 16 and 32, 20 rows 146 and
-  // 125 with 8 and 32; 384 of 4000, 4 rows, 60, 52 and 47 with 4, 8 and 16; but 384 of 8192 to 32000 210 and 240 with 32 and 64).
-  if (bits4 && rows <= 48) {
-    const int most = 10ll * total >= 9ll * longest * heads ? 6 : 4;
-    while (r.log >= ATT_LEAST_LOG && r.log < most && total >> r.log > 3 * ATT_EVEN) ++r.log;
-  }
   if (10ll * total >= 9ll * longest * heads)
     for (int parts = 1; parts <= EVEN_PARTS && r.per == 0; ++parts) {
       const int wgs = heads * parts, over = wgs % ATT_EVEN;
@@ -44,9 +37,34 @@ __host__ __device__ __forceinline__ FragmentRule fragment_rule(int total, int lo
     }
   return r;
 }
+// The same for rows of 4 bits, which are so little to read that starts, ends and joins count for more, and a step waits for itself as much as for memory.
+// Whole rounds of the workgroups that run at a time (slots), with steps of any number: as few rounds as leave fragments of 32 steps, of 64 where heads
+// are of (nearly) one length (where they are not, a head's last fragment counts for five eighths of nothing), and no more than the target has room for.
+// us with powers of two of steps and so: 128 heads of 2000 to 9000, 4 rows with their mass, 38.8 and 33.6, in pages of 7 slots 46.7 and 39.0; 96 of 900 to
+// 9831, 4 rows, 25.6 and 23.7, 40 rows 81.2 and 70.7; 192 of 8192 to 32000, 40 capped rows, 325 and 288; 384 of 4000, 4 rows, 57 and 50; but 96 of 32000, 20
+// rows with their mass, 191 and 205.
+// Few heads: a fragment more costs their join what a step costs a fragment, nearly, so that most fragments of a head go with the root of its steps, in whole
+// numbers of fragments for every unit (8 heads, 7 rows, of 8000 15.5 with one step each and 13.3 with two, of 16000 17.8 with two and 15.8 with four).
+__host__ __device__ __forceinline__ FragmentRule bits4_fragment_rule(int total, int longest, int heads, int rows, int target) {
+  const int slots = rows <= 16 ? 3 * ATT_EVEN : rows <= 48 ? 2 * ATT_EVEN : ATT_EVEN;
+  const bool even = 10ll * total >= 9ll * longest * heads;
+  const int ends = even ? 0 : 5 * heads >> 3, room = std::max(target / slots, 1);
+  const int rounds = even ? (int)(((long long)heads * ((longest + 63) >> 6) + slots - 1) / slots) : ((total >> 5) + ends) / slots + 1;
+  const int joined = total / ((int)(0.375f * sqrtf((float)longest)) + 1) / ATT_EVEN + 1;
+  const int parts = std::max(std::min(std::min(rounds, room) * slots, joined * ATT_EVEN) - ends, 1);
+  const int all = even ? longest : total, cut = even ? std::max(parts / heads, 1) : parts;
+  int per = (int)((unsigned)(all + cut - 1) / (unsigned)cut);
+  if ((long long)per * target < total) per = (int)((unsigned)(total + target - 1) / (unsigned)target);
+  return FragmentRule{0, per, 1.f / (float)per};
+}
 // Fragments of a head of that many steps.
 __host__ __device__ __forceinline__ int fragments_of(int steps, const FragmentRule &r) {
   if (r.per == 0) return (steps + (1 << r.log) - 1) >> r.log;
+  if (r.inv > 0.f) {             // below 2^24, where a quotient by way of fp32 is off by one at most
+    int parts = (int)((float)(steps + r.per - 1) * r.inv);
+    const int rest = steps + r.per - 1 - parts * r.per;
+    return parts + (rest >= r.per) - (rest < 0);
+  }
   int parts = 0;
 #pragma unroll
   for (int k = 0; k < EVEN_PARTS; ++k) parts += steps > k * r.per;
@@ -57,6 +75,10 @@ __host__ __device__ __forceinline__ int fragments_of(int steps, const FragmentRu
 // makes of them or of longer ones.  (An even cut makes no more than 2 * ATT_EVEN, however few the units.)
 inline int fragment_target(long long heads, long long steps, int rows, int units) {
   return (int)std::min((long long)SCAN_ROUNDS * (rows <= 32 ? 2 : 1) * units, std::max(((heads * steps - 1) >> ATT_LEAST_LOG) + 1, 2ll * ATT_EVEN));
+}
+inline int bits4_fragment_target(long long heads, long long steps, int rows, int units) {
+  const long long joined = (heads * std::min(steps, (long long)(sqrtf((float)steps) / 0.375f)) / ATT_EVEN + 1) * ATT_EVEN;
+  return (int)std::min(std::min((long long)SCAN_ROUNDS * (rows <= 32 ? 2 : 1) * units, heads * steps / 32 + heads + 3 * ATT_EVEN), joined);
 }
 inline int fragments_most(int heads, int target) { return std::max(target + heads, 2 * ATT_EVEN); }
 

@@ -4,7 +4,7 @@
 
 extern "C" {
 int fragments_launched(int heads, int steps, int rows, int units) {
-  return cmp::fragments_most(heads, cmp::fragment_target(heads, steps, rows, units));
+  return cmp::fragments_most(heads, cmp::bits4_fragment_target(heads, steps, rows, units));
 }
 int fragments_made(const int *steps, int heads, int promised, int rows, int units) {
   int total = 0, longest = 0, made = 0;
@@ -12,8 +12,9 @@ int fragments_made(const int *steps, int heads, int promised, int rows, int unit
     total += steps[h];
     longest = steps[h] > longest ? steps[h] : longest;
   }
-  const cmp::FragmentRule r = cmp::fragment_rule(total, longest, heads, rows, cmp::fragment_target(heads, promised, rows, units), true);
+  const cmp::FragmentRule r = cmp::bits4_fragment_rule(total, longest, heads, rows, cmp::bits4_fragment_target(heads, promised, rows, units));
   for (int h = 0; h < heads; ++h) made += cmp::fragments_of(steps[h], r);
   return made;
 }
+int fragments_of(int steps, int per) { return cmp::fragments_of(steps, cmp::FragmentRule{0, per, 1.f / (float)per}); }
 }

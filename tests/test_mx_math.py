@@ -33,6 +33,17 @@ def test_every_fragment_has_a_workgroup(M, units, rows):
                 assert heads <= made <= launched, (heads, promised, steps)
 
 
+def test_fragments_of_a_head(M):
+    """The quotient by way of fp32, up to the most steps that a table has."""
+    rng = np.random.default_rng(1)
+    most = 2 ** 23
+    for per in [1, 2, 3, 5, 7, 9, 31, 32, 33, 63, 64, 65, 127, 1000, 4097, 2 ** 20 + 1] + [int(x) for x in rng.integers(1, 10000, 50)]:
+        for steps in [1, 2, per - 1, per, per + 1, most, most - 1] + [int(x) for x in rng.integers(1, most, 200)] + [per * int(k) + d for k in
+                                                                                                                 rng.integers(1, max(2, most // per - 1), 40) for d in (-1, 0, 1)]:
+            if 1 <= steps <= most:
+                assert M.fragments_of(steps, per) == -(-steps // per), (steps, per)
+
+
 def test_the_parts_of_two_heads_go_to_one_xcd():
     """Workgroup i takes part e(i) of the heads' parts, those of two neighbours in turn: every part of every head once, and the same parts of both at one XCD
     wherever the pairs before have an even number of parts."""
