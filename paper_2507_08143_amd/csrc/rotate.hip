@@ -134,7 +134,9 @@ struct RotateRows {
 constexpr int HEADS_MOST = 1 << 20;
 constexpr int ROTATE_AT_ONCE = 4;  // rows that 16 lanes have on their way
 
-// A wave per token of a layer, or several; its four rows of 16 lanes take heads in turn.
+// A wave per token of a layer, or several; its four rows of 16 lanes take heads in turn.  Bound by HBM for a prompt: 32 + 8 heads of 32 768 tokens with norms,
+// keys before the rotation too (738 MB in and out), 131 us or 5.6 TB/s, more than a copy reaches; by the latency of position, frequencies and rows for few
+// tokens, 4.1 us up to 64 of them with 32 + 8 heads.
 __global__ __launch_bounds__(256) void rotate_kernel(const Rotation R, const RotateRows S) {
   const unsigned unit = blockIdx.x * 4u + (threadIdx.x >> 6);
   if (unit >= S.units) return;
@@ -186,12 +188,12 @@ struct RotateAppend {
   int tokens, group;               // query heads a kv head, 0: no queries
   int head_rows;                   // rows of 16 lanes a head has, 16 / that heads a workgroup
   int token_rows;                  // of them a token has
-  int parts;                       // workgroups a head
+  int part, parts;                 // tokens of a head a workgroup takes, workgroups a head
 };
-constexpr int ROTATE_PART = 64;    // tokens of a head a workgroup takes at most
 
-// K, V and the G queries of a token of a head are G + 2 rows with one turn.  Bound by the latency of the chain count, table
-// entry, row in small calls.
+// K, V and the G queries of a token of a head are G + 2 rows with one turn.  Bound by the latency of the chain count, table entry, row in small calls (one
+// token of 512 heads with four queries each, norms: 4.5 us, of which a launch is more than half) and by HBM in large ones (4 prompts of 4096 tokens, 8
+// heads, four queries each, 0.4 GB in and out: 92 us, into 4 bits 83).
 template <bool FP4>
 __global__ __launch_bounds__(256) void rotate_append_kernel(const CacheView C, const Rotation R, const RotateAppend S) {
   __shared__ uint4 exchange[FP4 ? 16 : 1][16];
@@ -211,7 +213,7 @@ __global__ __launch_bounds__(256) void rotate_append_kernel(const CacheView C, c
   Weights qw, kw;
   if (R.q_norm != nullptr && S.group > 0) load_weights(R.q_norm, w.l, p, qw);
   if (R.k_norm != nullptr) load_weights(R.k_norm, w.l, p, kw);
-  const int from = part * ROTATE_PART, to = min(n, from + ROTATE_PART);
+  const int from = part * S.part, to = n - from < S.part ? n : from + S.part;
   for (int t = from + mine / S.token_rows; t < to; t += S.head_rows / S.token_rows) {
     const int position = (int)((unsigned)seen + (unsigned)t);
     Turn turn;
@@ -323,11 +325,16 @@ static int append_rotated(const CacheView &C, const compactor_rotation_t *rotati
     S.qo_b = q.q_out_stride_b; S.qo_l = q.q_out_stride_l; S.qo_t = q.q_out_stride_t; S.qo_h = q.q_out_stride_h;
     S.group = q.q_heads / C.kv_heads;
   }
-  // one token: a head's rows side by side; more: two rows of lanes a token, eight tokens side by side
+  // One token: a head's rows side by side, of as many heads as fit.  A few: two rows of lanes a token, eight tokens side by side; more: one, so that a turn is
+  // found once (us of 4 prompts of 4096 tokens, 8 heads, 4 queries each, with 4, 2 and 1 rows: 168, 107 and 92; 16 of 8 tokens 6.9, 5.1 and 5.8).
+  // Parts of a head are as long as leaves every unit 16 workgroups (4 prompts of 64: 7.4 us with 16 tokens a part, 10 with 32, 14 with 64; 64 of 64 22.6, 26.4, 23.4).
   S.head_rows = S.tokens > 1 ? 16 : S.group <= 2 ? 4 : S.group <= 6 ? 8 : 16;
-  S.token_rows = S.tokens > 1 ? 2 : S.head_rows;
-  S.parts = (int)(((long long)S.tokens + ROTATE_PART - 1) / ROTATE_PART);
-  const long long heads = (long long)C.nreq * C.layers * C.kv_heads, per = 16 / S.head_rows, blocks = (heads + per - 1) / per * S.parts;
+  S.token_rows = S.tokens == 1 ? S.head_rows : S.tokens <= 8 ? 2 : 1;
+  const long long heads = (long long)C.nreq * C.layers * C.kv_heads;
+  auto parts_of = [&](int part) { return ((long long)S.tokens + part - 1) / part; };
+  for (S.part = 64; S.part > 16 && heads * parts_of(S.part) < 4096;) S.part /= 2;
+  S.parts = (int)parts_of(S.part);
+  const long long per = 16 / S.head_rows, blocks = (heads + per - 1) / per * S.parts;
   if (!launchable(blocks, 256) || !launchable((heads + 255) / 256, 256)) return COMPACTOR_EINVAL;
   hipStream_t st = static_cast<hipStream_t>(stream);
   (void)hipGetLastError();   // a leftover of earlier, unrelated HIP calls is not this call's error
@@ -393,9 +400,10 @@ int compactor_rotate(const compactor_rotation_t *rotation, const compactor_rotat
                r.k_out_stride_b, r.k_out_stride_l, r.k_out_stride_t, r.k_out_stride_h,
                r.k_plain_stride_b, r.k_plain_stride_l, r.k_plain_stride_t, r.k_plain_stride_h,
                r.positions, r.position_stride_b, r.new_tokens, r.layers, r.tokens, r.q_heads, r.kv_heads, 1, 0u};
-  // few tokens: their heads over as many waves as have one for every row of lanes
+  // Few tokens: their heads over as many waves as have one for every row of lanes, up to a wave a SIMD of the chip (512 tokens of 32 + 8 heads: 5.7 us, with
+  // four waves a SIMD 6.3; 2000 of 128 + 8 24.8 and 31).
   const int most = (max(r.q_heads, r.kv_heads) + 3) / 4;
-  while (S.parts < most && tokens * S.parts < 4096) S.parts *= 2;
+  while (S.parts < most && tokens * S.parts < 1024) S.parts *= 2;
   const long long units = tokens * S.parts;
   if (units > 0x7fffffffll || !launchable((units + 3) / 4, 256)) return COMPACTOR_EINVAL;
   S.units = (unsigned)units;

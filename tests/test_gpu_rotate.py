@@ -206,9 +206,10 @@ def test_append_rotated(C, mx, T, new, G, rotary, interleaved, page, layout):
 
 
 @pytest.mark.parametrize("mx", [False, True])
-@pytest.mark.parametrize("B,L,H,G,T", [(1, 1, 1, 1, 1), (67, 1, 3, 4, 1), (5, 7, 9, 5, 1), (130, 1, 8, 2, 1), (33, 1, 5, 3, 2), (300, 1, 1, 8, 1)])
+@pytest.mark.parametrize("B,L,H,G,T", [(1, 1, 1, 1, 1), (67, 1, 3, 4, 1), (5, 7, 9, 5, 1), (130, 1, 8, 2, 1), (33, 1, 5, 3, 2), (300, 1, 1, 8, 1),
+                                       (3, 1, 2, 7, 8), (3, 1, 2, 7, 9), (40, 2, 8, 2, 20), (64, 4, 8, 1, 48), (64, 8, 8, 1, 60), (64, 8, 8, 1, 70)])
 def test_append_rotated_shapes(C, mx, B, L, H, G, T):
-    twins = _Twins(C, mx, _counts(B, L, H, 5, 0, 17, 33), page=16, room=8)
+    twins = _Twins(C, mx, _counts(B, L, H, 5, 0, 17, 33), page=16, room=max(8, T - 3))
     rotation = _rotation(C, layers=L)
     q, k, v = _rows((B, L, T, H * G, 128), 1), _rows((B, L, T, H, 128), 2), _rows((B, L, T, H, 128), 3)
     for P in (twins.a, twins.b):
