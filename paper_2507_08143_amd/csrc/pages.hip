@@ -96,20 +96,39 @@ __device__ __forceinline__ void four_free(const CacheView &C, const Reserve &R, 
 #pragma unroll
   for (int i = 0; i < 4; ++i) is_free[i] = p + i < C.num_pages && R.refs[min(p + i, C.num_pages - 1)] == 0;
 }
-// The first `wants` free pages, in order, or as many as there are; -> how many.  first: four_free(4 * threadIdx.x).
-__device__ __forceinline__ int find_free(const CacheView &C, const Reserve &R, int wants, const int (&first)[4], int *pages, int *part) {
-  int found = 0;
-  for (int p0 = 0; p0 < C.num_pages && found < wants; p0 += 4 * PLAN_THREADS) {
-    const int p = p0 + 4 * (int)threadIdx.x;
-    int is_free[4] = {first[0], first[1], first[2], first[3]}, all;
-    if (p0 > 0) four_free(C, R, p, is_free);
-    const int mine = is_free[0] + is_free[1] + is_free[2] + is_free[3];
-    int at = found + plan_scan(mine, part, &all) - mine;
+// Which of the pages p .. p + 15 are free, a bit each.
+__device__ __forceinline__ unsigned sixteen_free(const CacheView &C, const Reserve &R, long long p) {
+  unsigned bits = 0;
+  if (p + 16 <= C.num_pages) {
+    int4 x[4];
+    __builtin_memcpy(x, R.refs + p, sizeof(x));        // on 4 bytes
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      if (is_free[i] && at < wants) pages[at] = p + i;
-      at += is_free[i];
-    }
+    for (int i = 0; i < 4; ++i)
+      bits |= (unsigned)(x[i].x == 0) << (4 * i) | (unsigned)(x[i].y == 0) << (4 * i + 1) | (unsigned)(x[i].z == 0) << (4 * i + 2) |
+              (unsigned)(x[i].w == 0) << (4 * i + 3);
+  } else if (p < C.num_pages) {
+#pragma unroll
+    for (int i = 0; i < 16; ++i) bits |= (unsigned)(p + i < C.num_pages && R.refs[min(p + i, C.num_pages - 1ll)] == 0) << i;
+  }
+  return bits;
+}
+// The first `wants` free pages, in order, or as many as there are; -> how many.  first: four_free(4 * threadIdx.x).  Behind those,
+// which are all of a small pool, 16 a thread, the next ones on their way (us of a reserve where all but the last pages are in use, with 4 and with 16:
+// of 5000 pages 7.6 and 9.1, of 20 000 13.1 and 9.1, of 100 000 48 and 18, of 400 000 180 and 51).
+__device__ __forceinline__ int find_free(const CacheView &C, const Reserve &R, int wants, const int (&first)[4], int *pages, int *part) {
+  unsigned bits = (unsigned)first[0] | (unsigned)first[1] << 1 | (unsigned)first[2] << 2 | (unsigned)first[3] << 3;
+  int found = 0, each = 4;
+  for (long long p0 = 0; p0 < C.num_pages && found < wants;) {
+    const long long p = p0 + each * (int)threadIdx.x;
+    p0 += each * PLAN_THREADS;
+    each = 16;
+    const int mine = __popc(bits);
+    int all;
+    unsigned next = 0;
+    if (p0 < C.num_pages) next = sixteen_free(C, R, p0 + 16 * (int)threadIdx.x);
+    int at = found + plan_scan(mine, part, &all) - mine;
+    for (; bits != 0 && at < wants; bits &= bits - 1) pages[at++] = (int)p + __ffs(bits) - 1;
+    bits = next;
     found += all;
   }
   __syncthreads();                           // they are listed, and no count of references is looked at any more
@@ -211,7 +230,7 @@ __global__ __launch_bounds__(PLAN_THREADS) void reserve_plan_kernel(const CacheV
 }
 
 // Up to an entry a thread, which is a step of nearly any program: all in registers and LDS, one launch, and three loads that wait for each other (counts,
-// entry, references).  64 requests of which some need a page: 14.2 and 3.1 us in two launches by way of the workspace, FEW_TIME in this one.
+// entry, references).  64 requests of which some need a page: 14.2 and 3.1 us in two launches by way of the workspace, 7.4 in this one.
 // More entries go the other way.
 constexpr int FEW_REQUESTS = PLAN_THREADS;
 constexpr long long FEW_COUNTS = 65536;
@@ -299,14 +318,16 @@ __global__ __launch_bounds__(PLAN_THREADS) void reserve_few_kernel(const CacheVi
 }
 
 // ------------------------------------------------------------------------------------------ fork
-// A workgroup has a strip of columns of the tables, of counts or of seen: of all requests, so that it reads all of it before it writes.
+// A workgroup has a strip of columns of the tables, of counts or of seen: of all requests, so that it reads all of it before it writes.  Bound by the
+// latency of its three loads and of the atomics behind them, so strips are of 1024 numbers, but 8 columns at least, part of a cache line: 64 tables of
+// 2000 pages, beams of four, 4.0 us with 16 columns, 10.6 with 64.  Where many requests make even those large, strips get narrower so that they fit LDS.
 struct Fork {
   int32_t *tables, *refs;
   const int32_t *parents;
   int table_len, width_log;    // of a strip
   int table_strips, head_strips;
 };
-constexpr int FORK_NUMBERS = 16384;          // of a strip
+constexpr int FORK_NUMBERS = 16384;          // of a strip, that LDS holds
 
 __global__ __launch_bounds__(256) void fork_kernel(const CacheView C, const Fork F) {
   extern __shared__ int old[];
@@ -374,6 +395,7 @@ struct Compact {
   int *to;                     // scratch, [page]: from the number of pages in use on, where a page goes; behind them that number
 };
 
+// Bound by the latency of a pass over 4096 pages: 5000 pages 6.6 us with the tables' kernel, 100 000 45.
 __global__ __launch_bounds__(PLAN_THREADS) void compact_plan_kernel(const CacheView C, const Compact K) {
   __shared__ int part[PLAN_WAVES];
   const int tid = threadIdx.x, N = C.num_pages;
@@ -450,8 +472,8 @@ struct Copy {
   int row_chunks, chunks;      // of K (V) of a page; of a page
 };
 // Written past the caches: what is read is often shared by several copies, and what is written nobody reads for a while.  us of 112 copies of 16 pages of all layers
-// (477 MB in and out) 65, with plain stores 75 at the same number of workgroups; 3570 pages of 0.27 MB (1.9 GB) 427.  With 8 workgroups a unit 74 and 463, with 32 66 and
-// 427; 8 units a thread 80 and 427.
+// (477 MB in and out) with the reserve before them 65, with plain stores 75 at the same number of workgroups; 3570 pages of 0.27 MB (1.9 GB) with release and
+// plan 427.  With 8 workgroups a unit 74 and 463, with 32 66 and 427; 8 units a thread 80 and 427.  Of the 427 the copy is 390, 4.8 TB/s.
 constexpr int COPY_AT_ONCE = 4;              // units of a thread
 constexpr int COPY_WORKGROUPS = 4;           // a compute unit
 __device__ __forceinline__ void put(char *p, const uint4 &x) { store_stream16(p, x); }

@@ -151,6 +151,26 @@ def test_reserve_many(C, B, L, H, entries, own_all):
     W.reserve(5, rng.integers(-1, 7, B).tolist(), own_all)
 
 
+@pytest.mark.parametrize("N", [70, 4095, 4096, 4097, 4103, 4112, 20011, 20480, 61000])
+@pytest.mark.parametrize("lead", [0, 1])
+@pytest.mark.parametrize("free", ["last", "few", "half", "too few"])
+def test_reserve_pools(C, N, lead, free):
+    """Free pages anywhere in pools of all sizes, counts of references that begin anywhere."""
+    rng = np.random.default_rng(N)
+    wants = 40
+    refs = np.ones(N, np.int64)
+    refs[{"last": np.arange(N - wants, N), "few": rng.permutation(N)[:wants + 3], "half": rng.permutation(N)[:max(N // 2, wants)],
+          "too few": rng.permutation(N)[:wants - 1]}[free]] = 0
+    k = torch.empty(N, 1, 1, 1, 128, dtype=torch.bfloat16, device=DEV)
+    tables = [[-1, -1, -1] for _ in range(wants)]
+    cache = C.Cache(k, k.clone(), torch.tensor(tables, dtype=torch.int32, device=DEV), torch.zeros(wants, 1, 1, dtype=torch.int32, device=DEV))
+    dev = torch.tensor([9] * lead + refs.tolist(), dtype=torch.int32, device=DEV)[lead:]
+    r = refs.tolist()
+    want, lack = O.reserve(tables, r, [[0]] * wants, [1] * wants, 1, False)
+    pairs, done = C.compactor_pages_reserve(cache, dev, 1)
+    assert done.tolist() == [len(want), lack] and cache.tables.tolist() == tables and dev.tolist() == r
+
+
 @pytest.mark.parametrize("B,L,H,entries", [(1, 1, 1, 1), (6, 2, 3, 10), (64, 1, 4, 130), (300, 1, 1, 70), (5, 9, 8, 65), (2000, 1, 2, 5)])
 @pytest.mark.parametrize("state", [True, False])
 def test_fork(C, B, L, H, entries, state):
