@@ -96,19 +96,19 @@ __device__ __forceinline__ void four_free(const CacheView &C, const Reserve &R, 
 #pragma unroll
   for (int i = 0; i < 4; ++i) is_free[i] = p + i < C.num_pages && R.refs[min(p + i, C.num_pages - 1)] == 0;
 }
-// Which of the pages p .. p + 15 are free, a bit each.
-__device__ __forceinline__ unsigned sixteen_free(const CacheView &C, const Reserve &R, long long p) {
+// A bit for each of the references of pages p .. p + 15 that is `so`; none for pages beyond the last.
+template <class So>
+__device__ __forceinline__ unsigned sixteen(const int32_t *refs, int pages, long long p, So so) {
   unsigned bits = 0;
-  if (p + 16 <= C.num_pages) {
+  if (p + 16 <= pages) {
     int4 x[4];
-    __builtin_memcpy(x, R.refs + p, sizeof(x));        // on 4 bytes
+    __builtin_memcpy(x, refs + p, sizeof(x));        // on 4 bytes
 #pragma unroll
     for (int i = 0; i < 4; ++i)
-      bits |= (unsigned)(x[i].x == 0) << (4 * i) | (unsigned)(x[i].y == 0) << (4 * i + 1) | (unsigned)(x[i].z == 0) << (4 * i + 2) |
-              (unsigned)(x[i].w == 0) << (4 * i + 3);
-  } else if (p < C.num_pages) {
+      bits |= (unsigned)so(x[i].x) << (4 * i) | (unsigned)so(x[i].y) << (4 * i + 1) | (unsigned)so(x[i].z) << (4 * i + 2) | (unsigned)so(x[i].w) << (4 * i + 3);
+  } else if (p < pages) {
 #pragma unroll
-    for (int i = 0; i < 16; ++i) bits |= (unsigned)(p + i < C.num_pages && R.refs[min(p + i, C.num_pages - 1ll)] == 0) << i;
+    for (int i = 0; i < 16; ++i) bits |= (unsigned)(p + i < pages && so(refs[min(p + i, pages - 1ll)])) << i;
   }
   return bits;
 }
@@ -121,7 +121,7 @@ __device__ __forceinline__ int find_free(const CacheView &C, const Reserve &R, i
   for (long long p0 = 0; p0 < C.num_pages && found < wants;) {
     if (p0 > 0) {
       each = 16;
-      bits = sixteen_free(C, R, p0 + 16 * (int)threadIdx.x);
+      bits = sixteen(R.refs, C.num_pages, p0 + 16 * (int)threadIdx.x, [](int refs) { return refs == 0; });
     }
     const int mine = __popc(bits);
     int all;
@@ -394,34 +394,43 @@ struct Compact {
   int *to;                     // scratch, [page]: from the number of pages in use on, where a page goes; behind them that number
 };
 
-// Bound by the latency of a pass over 4096 pages: 5000 pages 6.6 us with the tables' kernel, 100 000 45.
+// Bound by the latency of its passes, one over all references and one in steps of 16 384 with the numbers in between (us with the tables' kernel, where nothing
+// has to move; in brackets with 4 pages a thread and step: of 5000 pages 6.7 (6.9), of 20 000 7.7 (12.6), of 100 000 22 (45), of 400 000 77 (167)).
 __global__ __launch_bounds__(PLAN_THREADS) void compact_plan_kernel(const CacheView C, const Compact K) {
   __shared__ int part[PLAN_WAVES];
   const int tid = threadIdx.x, N = C.num_pages;
-  auto used = [&](int p) { return p < N && K.refs[min(p, N - 1)] > 0; };
+  auto used = [&](long long p) { return sixteen(K.refs, N, p, [](int refs) { return refs > 0; }); };
   int n = 0, moves = 0;
-#pragma unroll 8
-  for (int p = tid; p < N; p += PLAN_THREADS) n += used(p);
+#pragma unroll 4
+  for (long long p = 16 * tid; p < N; p += 16 * PLAN_THREADS) n += __popc(used(p));
   plan_scan(n, part, &n);
   int before = 0;                            // pages in use so far
-  for (int p0 = 0; p0 < N; p0 += 4 * PLAN_THREADS) {
-    const int p = p0 + 4 * tid;
-    int is_used[4], all;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) is_used[i] = used(p + i);
-    const int mine = is_used[0] + is_used[1] + is_used[2] + is_used[3];
-    int at = before + plan_scan(mine, part, &all) - mine;
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      if (p + i < n && !is_used[i]) K.pairs[p + i - at].y = p + i;          // p - at free ones are below
-      if (p + i >= n && p + i < N) {
-        K.to[p + i] = p + i;
-        if (is_used[i]) K.pairs[n - 1 - at].x = p + i;
-      }
-      moves += p + i < n && !is_used[i];
-      at += is_used[i];
-    }
+  for (long long p0 = 0; p0 < N; p0 += 16 * PLAN_THREADS) {
+    const long long p = p0 + 16 * tid;
+    const unsigned is_used = used(p);
+    int all;
+    const int at = before + plan_scan(__popc(is_used), part, &all) - __popc(is_used);
     before += all;
+    if (p >= N) continue;
+    const int low = clamp_to(n - p, 16);                                    // of the 16 are below n
+    const unsigned below = (1u << low) - 1u;
+    auto rank = [&](int i) { return at + __popc(is_used & ((1u << i) - 1u)); };             // pages in use before p + i
+    for (unsigned bits = ~is_used & below; bits != 0; bits &= bits - 1, ++moves) {
+      const int i = __ffs(bits) - 1;
+      K.pairs[p + i - rank(i)].y = (int)p + i;
+    }
+    for (unsigned bits = is_used & ~below; bits != 0; bits &= bits - 1) {
+      const int i = __ffs(bits) - 1;
+      K.pairs[n - 1 - rank(i)].x = (int)p + i;
+    }
+    if (low == 16) continue;
+    if (p + 16 <= N) {                       // (those below n are not looked at)
+      const int q = (int)p;
+#pragma unroll
+      for (int i = 0; i < 16; i += 4) reinterpret_cast<int4 *>(K.to + q)[i >> 2] = make_int4(q + i, q + i + 1, q + i + 2, q + i + 3);
+    } else {
+      for (int i = 0; p + i < N; ++i) K.to[p + i] = (int)p + i;
+    }
   }
   plan_scan(moves, part, &moves);
   __syncthreads();

@@ -214,7 +214,7 @@ def test_release_and_compact(C, B, L, H, entries):
         assert all(r > 0 for r in W.refs[:n]) and not any(W.refs[n:]) and (not want or before != W.tables or W.refs)
 
 
-@pytest.mark.parametrize("N", [1, 2, 4095, 4096, 4097, 20011])
+@pytest.mark.parametrize("N", [1, 2, 15, 16, 17, 4095, 4096, 4097, 16384, 16391, 20011, 61000])
 @pytest.mark.parametrize("share", [0.0, 0.02, 0.5, 1.0])
 def test_compact_pools(C, N, share):
     rng = np.random.default_rng(N)
