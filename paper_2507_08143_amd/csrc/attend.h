@@ -177,7 +177,7 @@ __device__ __forceinline__ HeadSize head_size(const CacheView &C, const Queries 
 }
 
 // How long a head is only the device knows, so up to SCAN_HEADS heads every wave finds its workgroup's part by itself, without a
-// barrier: heads are cut into fragments of the same power of two of steps, numbered head after head, at most `target` of them beside
+// barrier: heads are cut into fragments of as many steps each, numbered head after head, at most `target` of them beside
 // the last of each head.  A few rounds of workgroups keep the chip busy to the end whatever the lengths (16 requests of 68
 // to 55778 slots a head, us with fragments of any size in 1 / 2 / 3 / 4 / 6 rounds 212 / 202 / 201 / 202 / 203; 48 of 8192 to 32000 833 / 694 / 657 /
 // 652 / 643; 32 of 500 to 16000 131 / 119 / 116 / 116 / 120; cutting every head into the same number of parts 217 / 645 / -).  Heads of (nearly)

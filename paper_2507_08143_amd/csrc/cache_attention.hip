@@ -333,29 +333,46 @@ __global__ __launch_bounds__(256, NT <= 2 ? 2 : 1) void attend_kernel(const Cach
   if (complete && store && n > 0) mass_here(C, Q, hp, logits, R, count, L.lse2, &L.none);
 }
 
-// Second launch: the fragments of a head meet.  The first heads * R workgroups take a query row each, 16 fragments side by side
-// and 8 channels a thread; the others add a fragment's weights to the mass.
+// A query row of a head's fragments, all of its channels: SIDE fragments side by side, 8 channels a thread.
+template <int SIDE>
+__device__ __forceinline__ void join_fragments(const Queries &Q, int2 f, int R, int r, const float2 &all, int sl, int ch, f32x4 (&o)[2]) {
+  o[0] = o[1] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll SIDE < 16 ? 4 : 1
+  for (int k = sl; k < f.y; k += SIDE) {
+    const long long at = (long long)(f.x + k) * R + r;
+    const float mk = Q.stats[at].x, scale = all.x == -INFINITY ? 0.f : exp2_(mk - all.x);
+    const f32x4 *x = reinterpret_cast<const f32x4 *>(Q.partial + at * D + ch);
+    o[0] += x[0] * scale;
+    o[1] += x[1] * scale;
+  }
+}
 
+// Second launch: the fragments of a head meet.  The first workgroups take a query row each, 16 fragments side by side and 8 channels a thread, or (WAVES)
+// four, a wave each with 4 fragments side by side; the others add a fragment's weights to the mass.
+template <bool WAVES>
 __global__ __launch_bounds__(256) void attend_join_kernel(const CacheView C, const Queries Q) {
-  __shared__ float part_o[16][D + 4], lse2[MOST_ROWS];
+  __shared__ float part_o[WAVES ? 1 : 16][D + 4], lse2[MOST_ROWS];
   __shared__ float2 stats[256];                     // of the groups of more than 16 rows
   __shared__ int none;
   const int tid = threadIdx.x, R = Q.tokens * Q.group;
   const unsigned rows = (unsigned)C.nreq * (unsigned)C.layers * (unsigned)C.kv_heads * (unsigned)R;
-  if (blockIdx.x < rows) {
-    const unsigned g = blockIdx.x / (unsigned)R;
-    const int r = (int)(blockIdx.x - g * (unsigned)R);
+  const unsigned blocks = WAVES ? (rows + 3) / 4 : rows;
+  if (blockIdx.x < blocks) {
+    const unsigned at = WAVES ? 4 * blockIdx.x + (unsigned)__builtin_amdgcn_readfirstlane(tid >> 6) : blockIdx.x;
+    if (at >= rows) return;
+    const unsigned g = at / (unsigned)R;
+    const int r = (int)(at - g * (unsigned)R);
     const int2 f = Q.head_frags[g];
     if (f.y < 2) return;                            // its only workgroup has finished it
     const float2 all = join_stats(Q, f.x, f.y, R, r);      // (every wave)
-    const int sl = tid >> 4, ch = 8 * (tid & 15);
-    f32x4 o[2] = {f32x4{0.f, 0.f, 0.f, 0.f}, f32x4{0.f, 0.f, 0.f, 0.f}};
-    for (int k = sl; k < f.y; k += 16) {
-      const long long at = (long long)(f.x + k) * R + r;
-      const float mk = Q.stats[at].x, scale = all.x == -INFINITY ? 0.f : exp2_(mk - all.x);
-      const f32x4 *x = reinterpret_cast<const f32x4 *>(Q.partial + at * D + ch);
-      o[0] += x[0] * scale;
-      o[1] += x[1] * scale;
+    const int sl = WAVES ? tid >> 4 & 3 : tid >> 4, ch = 8 * (tid & 15);
+    f32x4 o[2];
+    join_fragments<WAVES ? 4 : 16>(Q, f, R, r, all, sl, ch, o);
+    if (WAVES) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) o[i >> 2][i & 3] = quarters_sum(o[i >> 2][i & 3]);
+      if (sl == 0) finish_row(C, Q, head_of(C, g), r, ch, o, all.x, all.y);
+      return;
     }
     *reinterpret_cast<f32x4 *>(&part_o[sl][ch]) = o[0];
     *reinterpret_cast<f32x4 *>(&part_o[sl][ch + 4]) = o[1];
@@ -371,7 +388,7 @@ __global__ __launch_bounds__(256) void attend_join_kernel(const CacheView C, con
     }
     return;
   }
-  const Fragment f = Q.frags[blockIdx.x - rows];
+  const Fragment f = Q.frags[blockIdx.x - blocks];
   if (f.head < 0 || f.parts < 2 || f.count > Q.most) return;
   const HeadPlace hp = head_place(C, head_of(C, (unsigned)f.head));
   const float *logits = Q.logits + (long long)f.head * R * Q.pitch;
@@ -388,6 +405,11 @@ __global__ __launch_bounds__(256) void attend_join_kernel(const CacheView C, con
     mass_add(Q, lse2, none, logits, R, at, M);
   }
 }
+
+// Where there are many rows each has few fragments, and what counts is how many workgroups start: for rows of 4 bits, where that is a larger part of a call, a
+// wave a row from this many on (us with a workgroup a row / a wave: 96 heads of 900 to 9831, 20 rows with their mass 44.3 / 41.9; 1024 of 500 to 4000, 4 rows
+// 89.0 / 83.6; 192 of 8192 to 32000, 40 rows 286 / 278; but 8 of 8000, 7 rows, 13.4 / 15.3, of 32000 20.6 / 26.2).
+constexpr long long JOIN_WAVES = 1024;
 
 // Weights of many rows from K, which is read again: 256 bytes a slot, where the logits' way through the workspace takes 8 for every row.
 // (Third launch.)  A fragment a workgroup; its rows' sums are known.  A lane has 8 slots of query l & 15 as in attend_kernel, and the sum over the
@@ -604,7 +626,8 @@ int attend_call(const CacheView &C, const compactor_cache_query_t *query, const 
   if (need > 0 && (reinterpret_cast<uintptr_t>(workspace) & 255u)) return COMPACTOR_EALIGN;
   const long long heads = (long long)C.nreq * C.layers * C.kv_heads;
   const long long blocks = A.frags_most > 0 ? A.frags_most : heads;
-  const long long join = A.joined ? heads * A.rows + (query->accumulate && !A.again ? A.frags_most : 0) : 0;
+  const bool waves = kernels.bits4 && heads * A.rows >= JOIN_WAVES;
+  const long long join = A.joined ? (waves ? (heads * A.rows + 3) / 4 : heads * A.rows) + (query->accumulate && !A.again ? A.frags_most : 0) : 0;
   if (!launchable(blocks, 256) || !launchable(join, 256)) return COMPACTOR_EINVAL;
   Queries Q;
   Q.q = static_cast<const uint16_t *>(query->q);
@@ -637,7 +660,7 @@ int attend_call(const CacheView &C, const compactor_cache_query_t *query, const 
   kernels.attend(C, Q, row16, (unsigned)blocks, st);
   if (A.joined) {
     if (hipGetLastError() != hipSuccess) return COMPACTOR_EHIP;
-    hipLaunchKernelGGL(attend_join_kernel, dim3((unsigned)join), dim3(256), 0, st, C, Q);
+    hipLaunchKernelGGL(waves ? attend_join_kernel<true> : attend_join_kernel<false>, dim3((unsigned)join), dim3(256), 0, st, C, Q);
   }
   if (A.again) {
     if (hipGetLastError() != hipSuccess) return COMPACTOR_EHIP;

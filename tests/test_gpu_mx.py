@@ -210,7 +210,7 @@ def test_attention_scales_and_caps(C, scale, cap, gain):
 
 
 @pytest.mark.parametrize("B,L,H,n,page", [(1, 1, 4, 9001, 64), (2, 1, 1, 33000, 24), (1, 3, 2, 6007, 32), (1, 1, 2, 70001, 256)])
-@pytest.mark.parametrize("G,T", [(4, 1), (7, 1), (5, 4)])
+@pytest.mark.parametrize("G,T", [(4, 1), (7, 1), (5, 4), (43, 1, 5, 1500, 16, 5, 1), (37, 1, 3, 1400, 24, 3, 5)])
 def test_attention_long(C, B, L, H, n, page, G, T):
     P = X.Paged(C, DEV, _counts(B, L, H, n, n - 3 * page - 1, 5), page=page, layout="head")
     _attend(C, P, _queries(P, T, H * G), cap=20.0 if T > 1 else 0.0)
