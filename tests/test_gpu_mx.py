@@ -210,10 +210,17 @@ def test_attention_scales_and_caps(C, scale, cap, gain):
 
 
 @pytest.mark.parametrize("B,L,H,n,page", [(1, 1, 4, 9001, 64), (2, 1, 1, 33000, 24), (1, 3, 2, 6007, 32), (1, 1, 2, 70001, 256)])
-@pytest.mark.parametrize("G,T", [(4, 1), (7, 1), (5, 4), (43, 1, 5, 1500, 16, 5, 1), (37, 1, 3, 1400, 24, 3, 5)])
+@pytest.mark.parametrize("G,T", [(4, 1), (7, 1), (5, 4)])
 def test_attention_long(C, B, L, H, n, page, G, T):
     P = X.Paged(C, DEV, _counts(B, L, H, n, n - 3 * page - 1, 5), page=page, layout="head")
     _attend(C, P, _queries(P, T, H * G), cap=20.0 if T > 1 else 0.0)
+
+
+@pytest.mark.parametrize("B,L,H,n,page,G,T", [(43, 1, 5, 1500, 16, 5, 1), (37, 1, 3, 1400, 24, 3, 5), (41, 3, 3, 3000, 16, 3, 1)])
+def test_attention_of_many_rows_in_fragments(C, B, L, H, n, page, G, T):
+    """Numbers of rows that are no multiple of four."""
+    P = X.Paged(C, DEV, _counts(B, L, H, n, n - 3 * page - 1, 5), page=page, layout="token")
+    _attend(C, P, _queries(P, T, H * G))
 
 
 @pytest.mark.parametrize("H,lengths,page", [(2, (9001, 300, 0, 1), 64), (1, (20011, 6000, 4500, 31), 24)])
