@@ -215,7 +215,7 @@ __device__ __forceinline__ bool scan_part(const CacheView &C, const Queries &Q, 
   }
   const int total = __builtin_amdgcn_readlane(wave_scan(mine), 63);          // the host has seen to it that this fits
   longest = (int)__builtin_amdgcn_readlane(wave_max_up((unsigned)longest), 63);
-  const FragmentRule rule = BITS4 ? bits4_fragment_rule(total, longest, heads, Q.tokens * Q.group, Q.target)
+  const FragmentRule rule = BITS4 ? bits4_fragment_rule(total, longest, heads, Q.tokens * Q.group, Q.target, C.slot_stride > ROW4)
                                   : fragment_rule(total, longest, heads, Q.tokens * Q.group, Q.target);
   int before = 0;
   for (int h0 = 0; h0 < heads; h0 += 64 * SCAN_GROUP) {

@@ -29,8 +29,9 @@ def test_every_fragment_has_a_workgroup(M, units, rows):
             for steps in (np.full(heads, promised), rng.integers(max(1, promised - promised // 12), promised + 1, heads),
                           rng.integers(1, promised + 1, heads), np.full(heads, 7 * promised), np.ones(heads)):
                 steps = np.ascontiguousarray(steps, dtype=np.int32)
-                made = M.fragments_made(steps.ctypes.data_as(C.POINTER(C.c_int)), heads, promised, rows, units)
-                assert heads <= made <= launched, (heads, promised, steps)
+                for apart in (0, 1):
+                    made = M.fragments_made(steps.ctypes.data_as(C.POINTER(C.c_int)), heads, promised, rows, units, apart)
+                    assert heads <= made <= launched, (heads, promised, apart, steps)
 
 
 def test_fragments_of_a_head(M):
