@@ -561,7 +561,7 @@ static AttendPlan attend_plan(const CacheView &C, const compactor_cache_query_t 
   A.target = A.frags_most = 0;
   // a wave adds up the steps of heads that may hold more than `most`, and their fragments have to fit all the same
   if (steps > ATT_ALONE && heads <= SCAN_HEADS && heads * (((long long)C.capacity + ATT_STEP - 1) / ATT_STEP) <= 0x7fffffffll) {
-    A.target = kernels.bits4 ? bits4_fragment_target(heads, steps, A.rows, cus) : fragment_target(heads, steps, A.rows, cus);
+    A.target = kernels.bits4 ? bits4_fragment_target(heads, steps, A.rows, cus, C.slot_stride > ROW4) : fragment_target(heads, steps, A.rows, cus);
     A.frags_most = fragments_most((int)heads, A.target);
   } else if (steps > ATT_ALONE) {
     A.split = (int)std::max(std::min(std::min(SPLIT_ALL / heads, (long long)SPLIT_MOST), ((steps - 1) >> ATT_LEAST_LOG) + 1), 1ll);

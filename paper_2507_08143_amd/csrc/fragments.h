@@ -39,20 +39,23 @@ __host__ __device__ __forceinline__ FragmentRule fragment_rule(int total, int lo
 }
 // The same for rows of 4 bits, which are so little to read that starts, ends and joins count for more, and a step waits for itself as much as for memory.
 // Whole rounds of the workgroups that run at a time (slots), with steps of any number: as few rounds as leave fragments of 32 steps (a head's last
-// one counts for five eighths of nothing), or where heads are of (nearly) one length of 64, of 16 where slots of a head lie apart and there are up to 16
-// rows, and no more than the target has room for (us with 64 and 16: 384 heads of 16000, 4 rows, slots apart 199 and 185, together 164 and 167; 96 of 32000 105 and 102, 87
+// one counts for five eighths of nothing), or where heads are of (nearly) one length of 64, of 24 where slots of a head lie apart and there are up to 16
+// rows, and no more than the target has room for (us with 64 and 24: 384 heads of 16000, 4 rows, slots apart 199 and 185, together 164 and 167; 96 of 32000 105 and 102, 87
 // and 90; 96 of 16000, 20 rows with their mass, apart 110 and 117).
 // us with powers of two of steps and so: 128 heads of 2000 to 9000, 4 rows with their mass, 38.8 and 33.6, in pages of 7 slots 46.7 and 39.0; 96 of 900 to
-// 9831, 4 rows, 25.6 and 23.7, 40 rows 81.2 and 70.7; 192 of 8192 to 32000, 40 capped rows, 325 and 288; 384 of 4000, 4 rows, 57 and 50; but 96 of 32000, 20
-// rows with their mass, 191 and 205.
+// 9831, 4 rows, 25.6 and 23.5, 40 rows 81 and 66; 192 of 8192 to 32000, 40 capped rows, 325 and 280; 384 of 4000, 4 rows, 57 and 44; but 96 of 32000, 20
+// rows with their mass, 191 and 200.
 // Few heads: a fragment more costs their join what a step costs a fragment, nearly, so that most fragments of a head go with the root of its steps, in whole
 // numbers of fragments for every unit (8 heads, 7 rows, of 8000 15.5 with one step each and 13.3 with two, of 16000 17.8 with two and 15.8 with four).
+__host__ __device__ __forceinline__ int bits4_slots(int rows) { return rows <= 16 ? 3 * ATT_EVEN : rows <= 48 ? 2 * ATT_EVEN : ATT_EVEN; }
+__host__ __device__ __forceinline__ long long bits4_rounds(long long total, long long longest, long long heads, int rows, bool apart, bool even) {
+  const int slots = bits4_slots(rows), even_steps = rows <= 16 && apart ? 24 : 64;
+  return even ? (heads * ((longest + even_steps - 1) / even_steps) + slots - 1) / slots : ((total >> 5) + (5 * heads >> 3)) / slots + 1;
+}
 __host__ __device__ __forceinline__ FragmentRule bits4_fragment_rule(int total, int longest, int heads, int rows, int target, bool apart) {
-  const int slots = rows <= 16 ? 3 * ATT_EVEN : rows <= 48 ? 2 * ATT_EVEN : ATT_EVEN;
+  const int slots = bits4_slots(rows);
   const bool even = 10ll * total >= 9ll * longest * heads;
-  const int even_steps = rows <= 16 && apart ? 16 : 64;
-  const int ends = even ? 0 : 5 * heads >> 3, room = std::max(target / slots, 1);
-  const int rounds = even ? (int)(((long long)heads * ((longest + even_steps - 1) / even_steps) + slots - 1) / slots) : ((total >> 5) + ends) / slots + 1;
+  const int ends = even ? 0 : 5 * heads >> 3, room = std::max(target / slots, 1), rounds = (int)bits4_rounds(total, longest, heads, rows, apart, even);
   const int joined = total / ((int)(0.375f * sqrtf((float)longest)) + 1) / ATT_EVEN + 1;
   const int parts = std::max(std::min(std::min(rounds, room) * slots, joined * ATT_EVEN) - ends, 1);
   const int all = even ? longest : total, cut = even ? std::max(parts / heads, 1) : parts;
@@ -79,9 +82,12 @@ __host__ __device__ __forceinline__ int fragments_of(int steps, const FragmentRu
 inline int fragment_target(long long heads, long long steps, int rows, int units) {
   return (int)std::min((long long)SCAN_ROUNDS * (rows <= 32 ? 2 : 1) * units, std::max(((heads * steps - 1) >> ATT_LEAST_LOG) + 1, 2ll * ATT_EVEN));
 }
-inline int bits4_fragment_target(long long heads, long long steps, int rows, int units) {
+// Workgroups that find no fragment cost their start, so no more rounds than the rule can want where heads hold no more than `steps` (us with a round or
+// more to spare and so: 384 heads of 4000, 4 rows, 46.2 and 42.3, of 2000 32.1 and 29.3).
+inline int bits4_fragment_target(long long heads, long long steps, int rows, int units, bool apart) {
   const long long joined = (heads * std::min(steps, (long long)(sqrtf((float)steps) / 0.375f)) / ATT_EVEN + 1) * ATT_EVEN;
-  return (int)std::min(std::min((long long)SCAN_ROUNDS * (rows <= 32 ? 2 : 1) * units, heads * steps / 32 + heads + 3 * ATT_EVEN), joined);
+  const long long rounds = std::max(bits4_rounds(heads * steps, steps, heads, rows, apart, true), bits4_rounds(heads * steps, steps, heads, rows, apart, false));
+  return (int)std::min(std::min((long long)SCAN_ROUNDS * (rows <= 32 ? 2 : 1) * units, rounds * bits4_slots(rows)), joined);
 }
 inline int fragments_most(int heads, int target) { return std::max(target + heads, 2 * ATT_EVEN); }
 
