@@ -1,8 +1,9 @@
 """Thin ctypes binding of libcompactor.so (argument marshalling only).
 
 Every function here has the name of the C entry point it calls
-(include/compactor.h) and does nothing but turn torch tensors into raw device
-pointers, allocate the outputs with torch, and check the return code.  All of
+(include/compactor.h; those of the cache in 4 bits a second one) and does
+nothing but turn torch tensors into raw device pointers, allocate the outputs
+with torch, and check the return code.  All of
 the method's arithmetic runs in the HIP kernels; there is no CPU fallback: if
 the shared library is missing the import of this module fails.
 """
@@ -1356,3 +1357,16 @@ def compactor_pages_compact(cache: Cache, refs: torch.Tensor, pairs=None, done=N
     ws = _pages_workspace(_lib.compactor_pages_compact_workspace_size, cache, workspace, stream)
     cache._on(stream, lambda st: _lib.compactor_pages_compact(ref, refs.data_ptr(), pairs.data_ptr(), done.data_ptr(), ws.data_ptr(), ws.numel(), st))
     return pairs, done
+
+
+# The cache in 4 bits by the name of its numbers too: E2M1 codes are commonly called fp4, rows of them with E8M0 scales mx.
+Fp4Cache = MxCache
+compactor_fp4_append = compactor_mx_append
+compactor_fp4_store = compactor_mx_store
+compactor_fp4_read = compactor_mx_read
+compactor_fp4_attention = compactor_mx_attention
+compactor_fp4_attention_workspace_size = compactor_mx_attention_workspace_size
+compactor_fp4_evict = compactor_mx_evict
+compactor_fp4_evict_workspace_size = compactor_mx_evict_workspace_size
+compactor_fp4_append_rotated = compactor_mx_append_rotated
+compactor_fp4_pages_copy = compactor_mx_pages_copy
