@@ -279,7 +279,7 @@ def prepare(case, seed):
         if op != "rotate":
             state = s["tables"], s["counts"], s["seen"], s["mass"], s["positions"]
             if op in ("attention", "append", "store"):
-                s["cache"] = C.MxCache(s["k4"], s["v4"], s["k_scales"], s["v_scales"], *state)
+                s["cache"] = C.Fp4Cache(s["k4"], s["v4"], s["k_scales"], s["v_scales"], *state)
             if op == "store":
                 s["source"] = C.Cache(s["k_pages"], s["v_pages"], s["source_tables"], s["source_counts"], s["source_seen"],
                                       s["source_mass"], s["source_positions"])
@@ -527,12 +527,12 @@ def _plain_reserve(s):
     i = torch.arange(P, device=dev)
     there = (tables >= 0) & (tables < N)
     named = torch.where(there, tables, 0).long()
-    shared = (i >= first.unsqueeze(1)) & (i < need.unsqueeze(1)) & there & (refs[named] > 1)
+    shared = (i >= first.unsqueeze(1)) & (i < holds.unsqueeze(1)) & there & (refs[named] > 1)
     fresh = (i >= holds.unsqueeze(1)) & (i < need.unsqueeze(1)) & ~there
-    entry = torch.arange(B * P, device=dev).view(B, P)
+    b = torch.arange(B, device=dev).unsqueeze(1).expand(B, P)
     tally = torch.zeros(N, dtype=torch.int64, device=dev).scatter_add_(0, named.flatten(), shared.flatten().long())
-    last = torch.full((N,), -1, device=dev).scatter_reduce_(0, named.flatten(), torch.where(shared, entry, -1).flatten(), "amax")
-    copied = shared & ~((tally[named] == refs[named]) & (last[named] == entry))  # the last entry of all that name a page keeps it
+    last = torch.full((N,), -1, device=dev).scatter_reduce_(0, named.flatten(), torch.where(shared, b, -1).flatten(), "amax")
+    copied = shared & ~((tally[named] == refs[named]) & (last[named] == b))      # the last of all that name a page keeps it
     wants = (copied | fresh).flatten()
     rank = wants.cumsum(0) - 1
     free = (refs != 0).to(torch.int8).sort(stable=True).indices
@@ -606,7 +606,7 @@ def run(s):
     C, cache, new = s.get("C"), s.get("cache"), s["new_tokens"]
     if op == "attention":
         if own:
-            out, lse = C.compactor_mx_attention(cache, s["q"], new_tokens=new, softcap=case["cap"],
+            out, lse = C.compactor_fp4_attention(cache, s["q"], new_tokens=new, softcap=case["cap"],
                                                  accumulate=case["accumulate"], want_lse=True)
         else:
             out, lse = _plain_attention(s)
@@ -614,15 +614,15 @@ def run(s):
     if op == "append":
         s["state"].copy_(s["start"])          # the rows are rewritten on every pass
         if own:
-            C.compactor_mx_append(cache, s["k"], s["v"], new_tokens=new)
-            k, v = C.compactor_mx_read(cache, case["new"], new_tokens=new)
+            C.compactor_fp4_append(cache, s["k"], s["v"], new_tokens=new)
+            k, v = C.compactor_fp4_read(cache, case["new"], new_tokens=new)
         else:
             k, v = _plain_append(s)
         return {"k": k, "v": v, "mass": s["mass"], "positions": s["positions"], "counts": s["counts"], "seen": s["seen"]}
     if op == "store":
         if own:
-            C.compactor_mx_store(cache, s["source"])
-            k, v = C.compactor_mx_read(cache, s["max_tokens"], first=0)
+            C.compactor_fp4_store(cache, s["source"])
+            k, v = C.compactor_fp4_read(cache, s["max_tokens"], first=0)
         else:
             k, v = _plain_store(s)
         return {"k": k, "v": v, "mass": s["mass"], "positions": s["positions"], "counts": s["counts"], "seen": s["seen"]}
