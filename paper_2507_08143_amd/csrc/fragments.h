@@ -47,6 +47,10 @@ __host__ __device__ __forceinline__ FragmentRule fragment_rule(int total, int lo
 // rows with their mass, 191 and 200.
 // Few heads: a fragment more costs their join what a step costs a fragment, nearly, so that most fragments of a head go with the root of its steps, in whole
 // numbers of fragments for every unit (8 heads, 7 rows, of 8000 15.5 with one step each and 13.3 with two, of 16000 17.8 with two and 15.8 with four).
+// What the ends of hundreds of short heads take must not leave a long one among them in one piece (us of 512 heads, one of 131072 and the others of 100 or 500, 4 rows,
+// 4 with their mass, 20 with it, 40, with one part at least 791, 1030, 2156, 1520; 772, 1005, 2181, 1529; with 64 43, 45, 87, 57; 57, 65, 144, 108; with 96 43, 45, 82, 50; 46, 51,
+// 112, 86; with ends taken off the rounds only 55, 58, 82, 56; 50, 51, 90, 66, but then of 256 heads, the others of 100, 45, 48, 72, 53 instead of 30, 32, 62, 44).
+constexpr int LEAST_PARTS = 96;
 __host__ __device__ __forceinline__ int bits4_slots(int rows) { return rows <= 16 ? 3 * ATT_EVEN : rows <= 48 ? 2 * ATT_EVEN : ATT_EVEN; }
 __host__ __device__ __forceinline__ long long bits4_rounds(long long total, long long longest, long long heads, int rows, bool apart, bool even) {
   const int slots = bits4_slots(rows), even_steps = rows <= 16 && apart ? 24 : 64;
@@ -57,7 +61,7 @@ __host__ __device__ __forceinline__ FragmentRule bits4_fragment_rule(int total, 
   const bool even = 10ll * total >= 9ll * longest * heads;
   const int ends = even ? 0 : 5 * heads >> 3, room = std::max(target / slots, 1), rounds = (int)bits4_rounds(total, longest, heads, rows, apart, even);
   const int joined = total / ((int)(0.375f * sqrtf((float)longest)) + 1) / ATT_EVEN + 1;
-  const int parts = std::max(std::min(std::min(rounds, room) * slots, joined * ATT_EVEN) - ends, 1);
+  const int parts = std::max(std::min(std::min(rounds, room) * slots, joined * ATT_EVEN) - ends, LEAST_PARTS);
   const int all = even ? longest : total, cut = even ? std::max(parts / heads, 1) : parts;
   int per = (int)((unsigned)(all + cut - 1) / (unsigned)cut);
   if ((long long)per * target < total) per = (int)((unsigned)(total + target - 1) / (unsigned)target);
