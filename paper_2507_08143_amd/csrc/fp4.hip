@@ -7,7 +7,10 @@ namespace cmp {
 // ------------------------------------------------------------------------------------------ store
 // 16 lanes take a row of K and of V, 8 channels a lane.  Bound by HBM: 512 bytes a token in, 136 out, 16 of mass and position; 2.5 M tokens of 12
 // requests in 336 us, 4.9 TB/s, which is what a copy reaches.
-constexpr int STORE_ROWS = 64;       // of a head per workgroup
+constexpr int STORE_ROWS = 64;       // of a head per workgroup and step
+// Workgroups, beside one a head.  How many rows there are only the device knows, and tables often have room for many more, so a head's workgroups step through its rows
+// (16 requests of 256 heads that hold 1000 tokens, tables for 131 072 each: 8905 us with a workgroup for every 64 that there is room for, 556 with these).
+constexpr long long STORE_MOST = 65536;
 
 __global__ __launch_bounds__(256) void store_kernel(const CacheView T, const CacheView S, int parts) {
   const unsigned g = blockIdx.x / (unsigned)parts;
@@ -19,25 +22,27 @@ __global__ __launch_bounds__(256) void store_kernel(const CacheView T, const Cac
     if (T.seen != nullptr) T.seen[count_at(T, w.b, w.l, w.h)] = S.seen[count_at(S, w.b, w.l, w.h)];
   }
   const HeadPlace from = head_place(S, w), to = head_place(T, w);
+  for (int slot0 = part * STORE_ROWS; slot0 < room; slot0 += parts * STORE_ROWS) {
 #pragma unroll
-  for (int i = 0; i < STORE_ROWS / 16; ++i) {
-    const int slot = part * STORE_ROWS + 16 * i + (int)(threadIdx.x >> 4);
-    if (slot >= room) return;
-    const SlotPlace a = slot_place(S, from, slot), z = slot_place(T, to, slot);
-    if (!page_there(S, a.page) || !page_there(T, z.page)) continue;      // (the same for the 16 lanes)
-    const long long src = row_at(S, from, a) + 8 * lane, dst = row_at(T, to, z) + 2 * lane;
-    const uint4 k = load_stream16(S.k + src), v = load_stream16(S.v + src);
-    uint32_t k_scales, v_scales;
-    *reinterpret_cast<unsigned *>(T.k + dst) = fp4_encode_row(k, lane, k_scales);
-    *reinterpret_cast<unsigned *>(T.v + dst) = fp4_encode_row(v, lane, v_scales);
-    if (lane == 0) {
-      const long long y = state_at(T, to, z);
-      T.k_scales[y] = k_scales;
-      T.v_scales[y] = v_scales;
-      if (T.mass != nullptr) {
-        const long long x = state_at(S, from, a);
-        T.mass[y] = S.mass[x];
-        T.positions[y] = S.positions[x];
+    for (int i = 0; i < STORE_ROWS / 16; ++i) {
+      const int slot = slot0 + 16 * i + (int)(threadIdx.x >> 4);
+      if (slot >= room) break;
+      const SlotPlace a = slot_place(S, from, slot), z = slot_place(T, to, slot);
+      if (!page_there(S, a.page) || !page_there(T, z.page)) continue;      // (the same for the 16 lanes)
+      const long long src = row_at(S, from, a) + 8 * lane, dst = row_at(T, to, z) + 2 * lane;
+      const uint4 k = load_stream16(S.k + src), v = load_stream16(S.v + src);
+      uint32_t k_scales, v_scales;
+      *reinterpret_cast<unsigned *>(T.k + dst) = fp4_encode_row(k, lane, k_scales);
+      *reinterpret_cast<unsigned *>(T.v + dst) = fp4_encode_row(v, lane, v_scales);
+      if (lane == 0) {
+        const long long y = state_at(T, to, z);
+        T.k_scales[y] = k_scales;
+        T.v_scales[y] = v_scales;
+        if (T.mass != nullptr) {
+          const long long x = state_at(S, from, a);
+          T.mass[y] = S.mass[x];
+          T.positions[y] = S.positions[x];
+        }
       }
     }
   }
@@ -95,7 +100,7 @@ int compactor_mx_store(const compactor_mx_cache_t *cache, const compactor_cache_
   if (T.nreq != S.nreq || T.layers != S.layers || T.kv_heads != S.kv_heads) return COMPACTOR_EINVAL;
   if (T.counts == S.counts || T.k == S.k || T.v == S.v || T.k == S.v || T.v == S.k) return COMPACTOR_EINVAL;
   const long long heads = (long long)T.nreq * T.layers * T.kv_heads;
-  const int parts = (min(T.capacity, S.capacity) + STORE_ROWS - 1) / STORE_ROWS;
+  const int parts = (int)min((min(T.capacity, S.capacity) + STORE_ROWS - 1ll) / STORE_ROWS, max(STORE_MOST / heads, 1ll));
   if (!launchable(heads * parts, 256)) return COMPACTOR_EINVAL;
   (void)hipGetLastError();   // a leftover of earlier, unrelated HIP calls is not this call's error
   hipLaunchKernelGGL(store_kernel, dim3((unsigned)(heads * parts)), dim3(256), 0, static_cast<hipStream_t>(stream), T, S, parts);
