@@ -49,7 +49,8 @@ __device__ __forceinline__ void turn_freqs(const Rotation &R, int lane, double (
 // Weights of a norm, the lane's 8 channels.
 struct Weights { float w[8]; };
 __device__ __forceinline__ void load_weights(const float *norm, int layer, const RowPieces &p, Weights &W) {
-  const float4 a = *reinterpret_cast<const float4 *>(norm + layer * D + p.lo), b = *reinterpret_cast<const float4 *>(norm + layer * D + p.hi);
+  const float *w = norm + (long long)layer * D;
+  const float4 a = *reinterpret_cast<const float4 *>(w + p.lo), b = *reinterpret_cast<const float4 *>(w + p.hi);
   W = Weights{{a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w}};
 }
 
