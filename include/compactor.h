@@ -394,7 +394,8 @@ typedef struct compactor_cache_query {
   int32_t accumulate;     /* not 0: adds the weights to the cache's mass */
   int32_t max_tokens;     /* tokens that no head holds more of, 0 = what the tables hold.  Launches and
                              workspace go by it (accumulate: 4 bytes a token, head and query row, or without the query
-                             rows where there are more than 32 and that is more than 256 MB), so it pays where
+                             rows where there are more than 32 and that is more than 256 MB, of a cache in 4 bits
+                             more than 12 and 128 MB), so it pays where
                              tables have much more room than heads hold.  A head that holds more all the same is attended to in
                              full, but its weights are not accumulated. */
 } compactor_cache_query_t;
@@ -445,7 +446,9 @@ int compactor_cache_evict_workspace_size(const compactor_cache_t *cache,
 /* ---- the cache in 4 bits ------------------------------------------------------------------ */
 /* The same cache with rows of 64 bytes: channels in groups of 32, a channel a 4-bit floating point number (E2M1: 0, 0.5, 1, 1.5, 2, 3, 4, 6 and
  * a sign; channel 2i is the low half of byte i), a group a scale that is a power of two (E8M0: byte s stands for 2^(s - 127), 255 for
- * NaN), the OCP microscaling format MXFP4.  136 bytes a token of a head instead of 512.  The value of a number is exact in bf16.
+ * NaN), the OCP microscaling format MXFP4.  136 bytes a token of a head instead of 512.  The value of a number is exact in bf16, but for the larger ones
+ * of scale bytes 253 and 254 (from 2^128 on), which read as infinities.  No call here writes these bytes; rows of other programs that have them are no V to
+ * attend to: an infinity times a weight may come out as NaN, for queries too that do not see the row.
  * What is written: of a group whose largest magnitude is m 2^k (1 <= m < 2) the scale is 2^(k - 2), or 2^(k - 1) where m >= 1.75, so that
  * every number is off by half a step at most; between 2^-125 and 2^125; numbers are rounded to the nearest, ties to the even code, and to 6
  * beyond it.  A group with an infinity or a NaN becomes NaN, all 32 of it. */
@@ -476,7 +479,7 @@ typedef struct compactor_cache_rows_out {
  * is not there. */
 int compactor_mx_read(const compactor_mx_cache_t *cache, const compactor_cache_rows_out_t *rows, void *stream);
 
-/* compactor_cache_attention, to it.  Weights go into the product with V in 16 bits, their sums in fp32. */
+/* compactor_cache_attention, to it.  Weights go into the product with V in 16 bits, their sums in fp32.  The workspace goes by the pool's slot_stride too. */
 int compactor_mx_attention(const compactor_mx_cache_t *cache, const compactor_cache_query_t *query, void *workspace,
                             size_t workspace_bytes, void *stream);
 int compactor_mx_attention_workspace_size(const compactor_mx_cache_t *cache, const compactor_cache_query_t *query, size_t *bytes);

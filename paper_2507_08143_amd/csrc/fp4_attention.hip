@@ -151,7 +151,7 @@ __device__ __forceinline__ void product_v(const VRows &v, const float (&scale)[8
       acc[nt][2 * d + c] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(a[c].v, lo[nt].v, acc[nt][2 * d + c], 0, 0, 0);
     }
 }
-// Two weights as sums of two bf16 numbers: 2^-17 of them is lost.  (V holds no infinities, whose product with a lower part of the other sign would be none.)
+// Two weights as sums of two bf16 numbers: 2^-17 of them is lost.  (V that is written here holds no infinities, whose product with a lower part of the other sign would be none.)
 __device__ __forceinline__ void split4(float x0, float x1, unsigned &hi, unsigned &lo) {
   hi = pack_bf16(x0, x1);
   lo = pack_bf16(x0 - __uint_as_float(hi << 16), x1 - __uint_as_float(hi & 0xffff0000u));

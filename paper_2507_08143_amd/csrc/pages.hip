@@ -228,9 +228,10 @@ __global__ __launch_bounds__(PLAN_THREADS) void reserve_plan_kernel(const CacheV
   reserve_many(C, R, entries, first, part);
 }
 
-// Up to an entry a thread, which is a step of nearly any program: all in registers and LDS, one launch, and three loads that wait for each other (counts,
+// Up to an entry a thread, which is a step that does not ask for the pages of whole contexts: all in registers and LDS, one launch, and three loads that wait for each other (counts,
 // entry, references).  64 requests of which some need a page: 14.2 and 3.1 us in two launches by way of the workspace, 7.4 in this one.
-// More entries go the other way.
+// More entries go the other way, in time that grows with them (us of own_all, no page shared / eight contexts on the same pages: 48 contexts of 1640 pages 174 / 833, 64 of
+// 2000 276 / 1353).
 constexpr int FEW_REQUESTS = PLAN_THREADS;
 constexpr long long FEW_COUNTS = 65536;
 __global__ __launch_bounds__(PLAN_THREADS) void reserve_few_kernel(const CacheView C, const Reserve R) {
