@@ -543,7 +543,7 @@ int compactor_mx_append_rotated(const compactor_mx_cache_t *cache, const compact
  * whatever else holds it); 0: the page is free, and none is below 0.  The calls keep it up as they change the tables of `cache`, which they write to although
  * compactor_cache_t has them const.  Its tables are those of all layers, so these calls take the cache of all of them; of the pool only the sizes are looked at,
  * but by compactor_pages_copy, and a cache in 4 bits is passed as its member `cache`.  No two of them (on any caches) that share refs run at a time.
- * nreq <= 16384, num_pages <= 2^30.  Entries outside [0, num_pages) name no page. */
+ * nreq <= 16384, num_pages <= 2^30, nreq * table_len < 2^31 - 1024.  Entries outside [0, num_pages) name no page. */
 
 /* Room for new tokens.  With n_b new tokens of request b, `top` the most and `low` the fewest tokens that one of its heads holds, its entries from
  * ceil(top / page_size) up to ceil((top + n_b) / page_size) (or the table's end) that name no page get one, and a page from low / page_size on up to there that is

@@ -13,6 +13,7 @@ namespace cmp {
 constexpr int PLAN_THREADS = 1024, PLAN_WAVES = PLAN_THREADS / 64;
 constexpr int PAGES_MOST = 16384;            // requests
 constexpr int POOL_MOST = 1 << 30;           // pages, so that a step beyond the last one fits 32 bits
+constexpr long long ENTRIES_MOST = 0x7fffffffll - PLAN_THREADS;        // of all tables, likewise
 
 __device__ __forceinline__ int pages_of(const CacheView &C, int tokens) {       // that hold them
   const int full = invariant_quotient((unsigned)tokens, C.div_mul, C.div_shift);
@@ -594,7 +595,7 @@ static int copy_call(const CacheView &C, const int32_t *pairs, int max_pairs, co
 static int pages_view(const compactor_cache_t *cache, CacheNeed need, CacheView *C) {
   const int rc = cache_view(cache, need, C);
   if (rc) return rc;
-  const bool fits = C->nreq <= PAGES_MOST && C->num_pages <= POOL_MOST && (long long)C->nreq * cache->table_len <= 0x7fffffffll;
+  const bool fits = C->nreq <= PAGES_MOST && C->num_pages <= POOL_MOST && (long long)C->nreq * cache->table_len <= ENTRIES_MOST;
   return fits ? COMPACTOR_OK : COMPACTOR_EINVAL;
 }
 
